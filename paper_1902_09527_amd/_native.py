@@ -41,6 +41,18 @@ EXPORTS = (
     "kmeans_pp_workspace_bytes", "kmeans_pp_seed", "kmeans_pp_seed_noalloc", "kmeans_pp_run_best",
 )
 
+#: Types of rows (include/kmeans_ops.h).
+KM_F32 = 0
+KM_BF16 = 1
+KM_F16 = 2
+
+#: Every symbol include/kmeans_ops.h declares.
+OPS_EXPORTS = (
+    "kmeans_sort_workspace_bytes", "kmeans_sort_plan", "kmeans_sort_gather", "kmeans_sort_combine",
+    "kmeans_sort_combine_backward",
+    "kmeans_norm_forward", "kmeans_norm_workspace_bytes", "kmeans_norm_backward",
+)
+
 #: Size of the static workspace of kmeans_pp_seed_noalloc (KMEANS_PP_STATIC_WORKSPACE_BYTES).
 KMEANS_PP_STATIC_WORKSPACE_BYTES = 64 << 20
 
@@ -132,6 +144,23 @@ def load() -> C.CDLL:
     lib.kmeans_pp_run_best.argtypes = [P, i64, i32, i32, P, i32, i32, f64, P, P, P, u32, P, P,
                                        C.POINTER(KmStats)]
     lib.kmeans_pp_run_best.restype = C.c_int
+    f32, sz = C.c_float, C.c_size_t
+    lib.kmeans_sort_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.kmeans_sort_workspace_bytes.restype = sz
+    lib.kmeans_sort_plan.argtypes = [P, i64, i32, i32, P, P, P, P, P, sz, P]
+    lib.kmeans_sort_plan.restype = C.c_int
+    lib.kmeans_sort_gather.argtypes = [P, i64, i64, i32, i32, i32, i32, P, P, P, P]
+    lib.kmeans_sort_gather.restype = C.c_int
+    lib.kmeans_sort_combine.argtypes = [P, i64, i64, i32, i32, i32, i32, P, P, P, P, P]
+    lib.kmeans_sort_combine.restype = C.c_int
+    lib.kmeans_sort_combine_backward.argtypes = [P, i64, P, i64, i64, i32, i32, i32, i32, P, P, P, P, P, P]
+    lib.kmeans_sort_combine_backward.restype = C.c_int
+    lib.kmeans_norm_forward.argtypes = [P, i64, i64, i32, i32, P, P, i32, f32, P, P, P, P]
+    lib.kmeans_norm_forward.restype = C.c_int
+    lib.kmeans_norm_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.kmeans_norm_workspace_bytes.restype = sz
+    lib.kmeans_norm_backward.argtypes = [P, i64, P, i64, i64, i32, i32, P, P, P, i32, P, P, P, P, sz, P]
+    lib.kmeans_norm_backward.restype = C.c_int
     lib.kmeans_mti_last_hip_error.argtypes = []
     lib.kmeans_mti_last_hip_error.restype = C.c_char_p
     _lib = lib

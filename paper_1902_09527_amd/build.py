@@ -20,6 +20,8 @@ LIB = os.path.join(HERE, "libkmeans_mti.so")
 SOURCES = [os.path.join(CSRC, "km_kernels.hip"), os.path.join(CSRC, "km_large.hip"),
            os.path.join(CSRC, "km_small.hip"), os.path.join(CSRC, "km_pp.hip"),
            os.path.join(CSRC, "km_gen.hip"),
+           os.path.join(CSRC, "km_sort.hip"), os.path.join(CSRC, "km_norm.hip"),
+           os.path.join(CSRC, "km_ops.hip"),
            os.path.join(CSRC, "km_capi.hip")]
 ARCH = "gfx950"
 

@@ -1,0 +1,111 @@
+// Shared by the operators of a layer conditioned on clusters (km_sort.hip,
+// km_norm.hip, km_adapter.hip) and their entry points (km_ops.hip).  The
+// public interface is include/kmeans_ops.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace km {
+
+// Row types; the values are KM_F32, KM_BF16, KM_F16 of kmeans_ops.h.
+enum RowType { kF32 = 0, kBF16 = 1, kF16 = 2 };
+
+inline size_t row_type_bytes(int t) { return t == kF32 ? 4 : 2; }
+
+// V elements moved by one load or store.
+template <class T, int V>
+struct alignas(sizeof(T) * V) Vec {
+    T e[V];
+};
+
+template <class T>
+__device__ __forceinline__ float to_f32(T v) {
+    return (float)v;
+}
+// Rounds to nearest even; the only rounding of a result.
+template <class T>
+__device__ __forceinline__ T from_f32(float v) {
+    return (T)v;
+}
+
+// Sum over groups of W consecutive lanes (W a power of two up to 64), the
+// same value in every lane of a group.
+template <int W>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Whether rows at p with row stride ld (elements of es bytes) and width d can
+// be moved 16 bytes at a time.
+inline bool rows_vec16(const void* p, int64_t ld, int64_t d, size_t es) {
+    return ((uintptr_t)p & 15) == 0 && (ld * (int64_t)es) % 16 == 0 && (d * (int64_t)es) % 16 == 0;
+}
+
+// Error text and device checks of km_capi.hip, for the entry points elsewhere.
+int ops_hip_error(hipError_t e, const char* what);
+int ops_error(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+int ops_check_range(const void* p, size_t bytes, int device, const char* what);
+
+// ---- rows sorted by cluster and back (km_sort.hip)
+
+constexpr int64_t kSortRankMax = 1024;   // slots up to which one block ranks them by comparing
+constexpr int kSortBins = 1024;          // most digit values of a counting pass
+constexpr int kSortThreads = 512;
+constexpr int kSortWaves = kSortThreads / 64;
+
+// How N slots with keys 0..k are sorted: passes over digits of `bits` bits,
+// tiles of kSortThreads * rounds slots.  passes = 0: ranked in one block.
+struct SortShape {
+    int passes, bits, rounds;
+    int64_t tiles;
+    size_t off_hist, off_tot, off_idx, bytes;   // workspace segments
+};
+SortShape sort_shape(int64_t N, int32_t k);
+
+struct SortArgs {
+    const int32_t* ids;
+    int32_t N, k;
+    int32_t *order, *pos, *sorted_ids, *offsets;
+};
+hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hipStream_t s);
+
+// Rows to and from their sorted places.  A slot is in use where its place is
+// below offsets[k] (= *used).
+struct MoveArgs {
+    const int32_t* pos;    // n x m places
+    const int32_t* used;   // slots in use
+    int64_t n;
+    int32_t m, d;
+    const void *src, *src2;   // gather: X; combine: Z; backward: dY and Z
+    int64_t ld, ld2;
+    void* dst;                // gather: Xs; combine: Y; backward: dZ (contiguous rows)
+    const float* w;           // n x m weights, or null (ones)
+    float* dw;                // backward: n x m, or null
+};
+hipError_t launch_sort_gather(const MoveArgs& A, int type, hipStream_t s);
+hipError_t launch_sort_combine(const MoveArgs& A, int type, hipStream_t s);
+hipError_t launch_sort_combine_bwd(const MoveArgs& A, int type, hipStream_t s);
+
+// ---- layer norm (km_norm.hip)
+
+struct NormArgs {
+    const void *X, *dY;
+    int64_t ldx, lddy, n;
+    int32_t d;
+    const void *gamma, *beta;   // d values or null (ones, zeros)
+    int32_t param_f32;          // their type: float32, else the rows'
+    float eps;
+    void *Y, *dX;               // contiguous rows
+    float *mean, *rstd;         // written forward, read backward
+    float *dgamma, *dbeta;      // d values or null
+    float* part;                // backward: blocks x 2 x d partial sums
+    int32_t blocks;             // backward: rows of part (set by the launch)
+};
+int norm_bwd_max_blocks(int64_t n, int32_t d, int type);   // most rows of part that the backward pass writes
+hipError_t launch_norm_fwd(NormArgs A, int type, hipStream_t s);
+hipError_t launch_norm_bwd(NormArgs A, int type, hipStream_t s);
+
+}  // namespace km
