@@ -6,7 +6,9 @@
  * (tokens, embeddings) to small experts of their clusters.  The operators:
  *   kmeans_sort_*     rows sorted by cluster and back with weights, and the
  *                     gradients of both;
- *   kmeans_norm_*     layer norm of rows and its gradients.
+ *   kmeans_norm_*     layer norm of rows and its gradients;
+ *   kmeans_adapter_*  a shared projection with one low-rank adapter per
+ *                     cluster, and the gradients of rows and adapters.
  *
  * Common to all.  Status codes and kmeans_mti_last_hip_error() are those of
  * kmeans_mti.h; no entry point throws, allocates device memory or
@@ -98,6 +100,50 @@ int kmeans_norm_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
                          int32_t type, const float* mean, const float* rstd, const void* gamma, int32_t param_f32,
                          void* dX, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
                          void* hip_stream);
+
+/*
+ * A shared projection with one low-rank adapter per cluster: for every row x
+ * of cluster c
+ *   h = A_c x,  y = W x + scale_c B_c h;
+ * a row whose id is outside [0, k) has h = 0 and y = W x.
+ *   X      n rows of din, ldx apart      W  dout x din
+ *   A      k x r x din                   B  k x dout x r
+ *   scale  k float32 or NULL (ones)
+ *   Y      n x dout                      H  n x r (for the backward pass)
+ * all of one type; h and scale_c h are rounded to it once each where they
+ * enter the second product (not for up to 64 rows, where it is formed in
+ * float32).  The clusters come as
+ *   ids    n int32, with sorted_ids = offsets = order = NULL: the rows are
+ *          sorted in the workspace where the form for many rows takes them;
+ *   or a plan of kmeans_sort_plan with n slots (ids is not read): sorted_ids,
+ *          offsets and order (m = 1), or order = NULL for rows that are in
+ *          the plan's order already (the output of kmeans_sort_gather).
+ * Requires n >= 0, din, dout, k >= 1, 1 <= r <= 128 (else
+ * KM_ERR_UNSUPPORTED), n < 2^31.  backward: the workspace of the backward
+ * pass, else of the forward pass.
+ */
+size_t kmeans_adapter_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type,
+                                      int32_t backward);   /* 0 for bad sizes */
+int kmeans_adapter_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r,
+                           int32_t type, const void* W, const void* A, const void* B, const float* scale,
+                           const int32_t* ids, const int32_t* order, const int32_t* sorted_ids,
+                           const int32_t* offsets, void* Y, void* H, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/*
+ * Gradients of kmeans_adapter_forward from dY (n rows of dout), X and H, with
+ * a plan (as above, order or rows in its order):
+ *   g = scale_c B_c^T dy,  dX = W^T dy + A_c^T g  (n x din),
+ *   dA_c = sum g x^T  (k x r x din),  dB_c = scale_c sum dy h^T  (k x dout x r)
+ * over the rows of each cluster (zeros for a cluster with none), all of the
+ * rows' type; g is rounded to it once.  W has no gradient here: it is frozen
+ * where adapters are trained.
+ */
+int kmeans_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* H, int64_t n,
+                            int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type, const void* W,
+                            const void* A, const void* B, const float* scale, const int32_t* order,
+                            const int32_t* sorted_ids, const int32_t* offsets, void* dX, void* dA, void* dB,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -21,7 +21,7 @@ SOURCES = [os.path.join(CSRC, "km_kernels.hip"), os.path.join(CSRC, "km_large.hi
            os.path.join(CSRC, "km_small.hip"), os.path.join(CSRC, "km_pp.hip"),
            os.path.join(CSRC, "km_gen.hip"),
            os.path.join(CSRC, "km_sort.hip"), os.path.join(CSRC, "km_norm.hip"),
-           os.path.join(CSRC, "km_ops.hip"),
+           os.path.join(CSRC, "km_adapter.hip"), os.path.join(CSRC, "km_ops.hip"),
            os.path.join(CSRC, "km_capi.hip")]
 ARCH = "gfx950"
 

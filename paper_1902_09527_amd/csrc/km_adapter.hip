@@ -1,0 +1,938 @@
+// A shared projection with one low-rank adapter per cluster:
+//   h = A_c x,  y = W x + s_c B_c h,
+// and its gradients for rows and adapters (W is frozen):
+//   g = s_c B_c^T dy,  dx = W^T dy + A_c^T g,
+//   dA_c = sum g x^T,  dB_c = s_c sum dy h^T  over the cluster's rows.
+//
+// Rows are taken in cluster order (places), so a tile of rows meets few
+// clusters.  The inner products (h, g) are formed first: they are r wide, and
+// one pass over the rows forms them.  The shared product is a tiled matrix
+// product over the places whose contraction continues past the shared width
+// with the r inner products against each cluster's adapter: the adapter's
+// term costs r more steps of the same accumulators and no pass over the
+// results.  The adapters' gradients contract over a cluster's rows; long
+// clusters are cut into chunks whose float32 sums are joined in order.
+//
+// Sums are float32 (matrix-core accumulators); h and g are rounded to the
+// rows' type, once, as the matrix cores' operands.
+#include "km_ops.h"
+
+namespace km {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+#define KM_LDS __attribute__((address_space(3)))
+#define KM_GLOBAL __attribute__((address_space(1)))
+
+// Where a lane reads past the end of a row or of the rows: 16 zero bytes.
+__device__ __align__(16) const uint32_t ad_zero[4] = {0, 0, 0, 0};
+
+// 16-byte operand chunks: E elements of one row (or column) along the
+// contraction.  A 64-lane operand is 16 rows x 4 chunks; mma adds the product
+// of two, D[m][n] += sum_k first[m][k] second[n][k], lane l holding rows m =
+// 4 (l / 16) + 0..3 of column n = l % 16.  float32 takes four 16x16x4 steps.
+template <class T>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    }
+};
+template <>
+struct Mma<_Float16> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+    }
+};
+template <>
+struct Mma<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <class T>
+__device__ __forceinline__ u32x4 zero_chunk() {
+    return u32x4{0, 0, 0, 0};
+}
+
+// Elements p[0 .. E) at positions k0 .. of a row of K elements, zero past its end.
+template <class T>
+__device__ __forceinline__ u32x4 chunk_guarded(const T* row, int64_t k0, int64_t K, int64_t stride = 1) {
+    constexpr int E = Mma<T>::E;
+    Vec<T, E> v{};
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (k0 + e < K) v.e[e] = row[(k0 + e) * stride];
+    return __builtin_bit_cast(u32x4, v);
+}
+template <class T>
+__device__ __forceinline__ u32x4 chunk(const T* row, int64_t k0, int64_t K, bool aligned) {
+    if (!aligned) return chunk_guarded(row, k0, K);
+    return k0 < K ? *reinterpret_cast<const u32x4*>(row + k0) : zero_chunk<T>();
+}
+
+// Four consecutive results, col0 .. of a row of P.
+template <class T>
+__device__ __forceinline__ void store4(T* row, int64_t col0, int64_t P, f32x4 v, bool aligned) {
+    if (aligned && col0 + 4 <= P) {
+        Vec<T, 4> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.e[i] = from_f32<T>(v[i]);
+        *reinterpret_cast<Vec<T, 4>*>(row + col0) = o;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col0 + i < P) row[col0 + i] = from_f32<T>(v[i]);
+    }
+}
+
+// One asynchronous 16-byte move a lane from `src` to LDS base + 16 lane.
+__device__ __forceinline__ void load_lds16(const void* src, char* wave_base) {
+    __builtin_amdgcn_global_load_lds((const KM_GLOBAL void*)src, (KM_LDS void*)wave_base, 16, 0, 0);
+}
+
+__device__ __forceinline__ int64_t row_of(const int32_t* order, int64_t place) { return order ? order[place] : place; }
+
+// --------------------------------------------------------------------------
+// Inner products: S[place] = s_c Q_c u (rounded to T, rp wide, zero past r)
+// and, if H is not null, H[row] = Q_c u.  16 places a block; its four waves
+// share the contraction, their sums are added in wave order through LDS.
+// TR = false: Q_c is r x K (rows along the contraction); true: K x r.
+struct InnerArgs {
+    const void* U;
+    int64_t ldu;
+    const void* Q;
+    const int32_t *order, *sids, *offsets;
+    const float* scale;
+    void *S, *H;
+    int64_t n;
+    int32_t K, r, rp, u16, q16, h4;   // u16 / q16: rows of U / Q can be read 16 bytes at a time; h4: H written by fours
+};
+
+template <class T, int RF, bool TR>
+__global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E;
+    __shared__ f32x4 s_red[4][RF][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
+    const int64_t p0 = (int64_t)blockIdx.x * 16;
+    const int64_t place = p0 + li;
+    const bool in = place < A.n;
+    const int mine = in ? A.sids[place] : -1;
+    const int64_t row = in ? row_of(A.order, place) : 0;
+    const T* u = static_cast<const T*>(A.U) + row * A.ldu;
+    const int steps = (A.K + KS - 1) / KS;
+    int c = __builtin_amdgcn_readfirstlane(A.sids[p0]);
+    while (c >= 0) {
+        f32x4 acc[RF];
+#pragma unroll
+        for (int j = 0; j < RF; ++j) acc[j] = f32x4{0, 0, 0, 0};
+        const T* q = static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.K;
+        for (int s = wave; s < steps; s += 4) {
+            const int64_t k0 = (int64_t)s * KS + g * E;
+            const u32x4 b = chunk(u, k0, A.K, A.u16);
+#pragma unroll
+            for (int j = 0; j < RF; ++j) {
+                const int rr = j * 16 + li;
+                u32x4 a = zero_chunk<T>();
+                if (rr < A.r)
+                    a = TR ? chunk_guarded(q + rr, k0, A.K, A.r) : chunk(q + (int64_t)rr * A.K, k0, A.K, A.q16);
+                acc[j] = Mma<T>::mma(a, b, acc[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < RF; ++j) s_red[wave][j][lane] = acc[j];
+        __syncthreads();
+        const float sc = A.scale ? A.scale[c] : 1.0f;
+        for (int j = wave; j * 16 < A.rp; j += 4) {
+            f32x4 v{0, 0, 0, 0};
+            if (j < RF) v = (s_red[0][j][lane] + s_red[1][j][lane]) + (s_red[2][j][lane] + s_red[3][j][lane]);
+            const int r0 = j * 16 + g * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r0 + i >= A.r) v[i] = 0.0f;
+            if (mine == c) {
+                if (A.H) store4(static_cast<T*>(A.H) + row * A.r, r0, A.r, v, A.h4);
+                store4(static_cast<T*>(A.S) + place * A.rp, r0, A.rp, v * sc, true);
+            }
+        }
+        __syncthreads();
+        const int64_t next = A.offsets[c + 1];
+        c = next < p0 + 16 && next < A.n ? __builtin_amdgcn_readfirstlane(A.sids[next]) : -1;
+    }
+    if (in && mine < 0)   // rows in no cluster
+        for (int j = wave; j * 16 < A.rp; j += 4) {
+            const int r0 = j * 16 + g * 4;
+            if (A.H) store4(static_cast<T*>(A.H) + row * A.r, r0, A.r, f32x4{0, 0, 0, 0}, A.h4);
+            store4(static_cast<T*>(A.S) + place * A.rp, r0, A.rp, f32x4{0, 0, 0, 0}, true);
+        }
+}
+
+// --------------------------------------------------------------------------
+// The shared product over places with the adapters' term:
+//   Y[row] = V u + Q_c S[place],  V = W (P x K) forward, W^T (W is K x P) with TR.
+// A tile is TM places x TN columns, WR x WC waves; the contraction goes in
+// stages of 128 bytes a row, loaded to LDS while the stage before is used.
+struct MainArgs {
+    const void* U;
+    int64_t ldu;
+    const void *W, *Q, *S;
+    const int32_t *order, *sids, *offsets;
+    void* Y;
+    int64_t n;
+    int32_t K, P, r, rp, q16, y4;
+    int32_t tm, tn;   // tiles
+};
+
+// Chunk position of a stage's rows in LDS: rows are 128 bytes, so 16 rows read
+// at one chunk index fall on all 64 banks once.
+__device__ __forceinline__ int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
+
+// The same for tiles that hold the contraction along their rows (TR): 16-bit
+// tiles are read 4 rows x 16 columns at a time, float32 by columns.
+template <class T, int CPR>
+__device__ __forceinline__ int swz_tr(int k, int c) {
+    const int m = sizeof(T) == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2;
+    return c ^ (m & (CPR - 1));
+}
+
+// Operand of 16 columns c0 .. along rows k0 + 0 .. KS of a tile whose rows
+// are the contraction (CPR chunks a row).
+template <class T, int CPR>
+__device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int c0, int lane) {
+    if constexpr (sizeof(T) == 2) {
+        const int li = lane & 15, k = k0 + (lane >> 4) * 8 + (li >> 2), ch = c0 / 8 + ((li & 3) >> 1);
+        s16x4 v[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (KM_LDS s16x4*)(tile + ((k + 4 * t) * CPR + swz_tr<T, CPR>(k + 4 * t, ch)) * 16 + (li & 1) * 8));
+        struct Two { s16x4 a, b; } w{v[0], v[1]};
+        return __builtin_bit_cast(u32x4, w);
+    } else {
+        const int c = c0 + (lane & 15), k = k0 + (lane >> 4) * 4;
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = *reinterpret_cast<const uint32_t*>(tile + ((k + j) * CPR + swz_tr<T, CPR>(k + j, c / 4)) * 16 +
+                                                      (c & 3) * 4);
+        return v;
+    }
+}
+
+template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
+__global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
+    constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
+    constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
+    constexpr int kStage = (TM + TN) * 128;
+    extern __shared__ __align__(16) char s_tiles[];   // two stages: TM rows of U, then TN rows (TR: BK rows) of W
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, li = lane & 15;
+    const int wr = wave / WC, wc = wave % WC;
+
+    // Consecutive tiles go to one XCD (blocks are dealt over 8), down 4 tiles
+    // of places before the next columns.
+    const int64_t tiles = (int64_t)A.tm * A.tn, per = (tiles + 7) / 8;
+    const int64_t t = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= per || t >= tiles) return;
+    const int64_t grp = t / (4 * (int64_t)A.tn), m0 = grp * 4;
+    const int gm = A.tm - m0 < 4 ? (int)(A.tm - m0) : 4;
+    const int64_t in_grp = t - grp * 4 * A.tn;
+    const int64_t bm = (m0 + in_grp % gm) * TM, bn = in_grp / gm * TN;
+
+    const T* up[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        int64_t place = bm + (i * NT + tid) / 8;
+        if (place >= A.n) place = A.n - 1;   // not stored
+        up[i] = static_cast<const T*>(A.U) + row_of(A.order, place) * A.ldu;
+    }
+    const int nk = (A.K + BK - 1) / BK;
+
+    auto load = [&](int kt, char* buf) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int q = i * NT + tid, row = q / 8;
+            const int64_t k0 = (int64_t)kt * BK + swz(row, q % 8) * E;
+            if constexpr (AL)
+                load_lds16(k0 < A.K ? (const void*)(up[i] + k0) : (const void*)ad_zero, buf + (i * NT + wave * 64) * 16);
+            else
+                *reinterpret_cast<u32x4*>(buf + q * 16) = chunk_guarded(up[i], k0, A.K);
+        }
+        char* wb = buf + TM * 128;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const int q = i * NT + tid;
+            if constexpr (TR) {
+                const int kk = q / CPR;
+                const int64_t k = (int64_t)kt * BK + kk, col = bn + swz_tr<T, CPR>(kk, q % CPR) * E;
+                const T* src = static_cast<const T*>(A.W) + k * A.P;
+                if constexpr (AL)
+                    load_lds16(k < A.K && col < A.P ? (const void*)(src + col) : (const void*)ad_zero,
+                               wb + (i * NT + wave * 64) * 16);
+                else
+                    *reinterpret_cast<u32x4*>(wb + q * 16) =
+                        k < A.K ? chunk_guarded(src, col, A.P) : zero_chunk<T>();
+            } else {
+                const int row = q / 8;
+                int64_t col = bn + row;
+                if (col >= A.P) col = A.P - 1;   // not stored
+                const int64_t k0 = (int64_t)kt * BK + swz(row, q % 8) * E;
+                const T* src = static_cast<const T*>(A.W) + col * A.K;
+                if constexpr (AL)
+                    load_lds16(k0 < A.K ? (const void*)(src + k0) : (const void*)ad_zero,
+                               wb + (i * NT + wave * 64) * 16);
+                else
+                    *reinterpret_cast<u32x4*>(wb + q * 16) = chunk_guarded(src, k0, A.K);
+            }
+        }
+    };
+
+    f32x4 acc[FR][FC];
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+        for (int h = 0; h < FC; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
+
+    load(0, s_tiles);
+    for (int kt = 0; kt < nk; ++kt) {
+        // The stage's loads have landed, and every wave is done with the other buffer.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const char* ub = s_tiles + (kt & 1) * kStage;
+        const char* wb = ub + TM * 128;
+        if (kt + 1 < nk) load(kt + 1, s_tiles + ((kt + 1) & 1) * kStage);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            u32x4 b[FR], a[FC];
+#pragma unroll
+            for (int f = 0; f < FR; ++f) {
+                const int row = wr * (TM / WR) + f * 16 + li;
+                b[f] = *reinterpret_cast<const u32x4*>(ub + row * 128 + swz(row, s * 4 + g) * 16);
+            }
+#pragma unroll
+            for (int h = 0; h < FC; ++h) {
+                const int c0 = wc * (TN / WC) + h * 16;
+                if constexpr (TR)
+                    a[h] = read_tr<T, CPR>(wb, s * KS, c0, lane);
+                else
+                    a[h] = *reinterpret_cast<const u32x4*>(wb + (c0 + li) * 128 + swz(c0 + li, s * 4 + g) * 16);
+            }
+#pragma unroll
+            for (int f = 0; f < FR; ++f)
+#pragma unroll
+                for (int h = 0; h < FC; ++h) acc[f][h] = Mma<T>::mma(a[h], b[f], acc[f][h]);
+        }
+    }
+
+    // The adapters' term, cluster by cluster of the wave's places: a lane
+    // keeps the sum only where its place is of the cluster, so that nothing of
+    // one cluster's adapter reaches another's rows.
+    const int64_t w0 = bm + wr * (TM / WR), w1 = w0 + TM / WR < A.n ? w0 + TM / WR : A.n;
+    const int64_t cb = bn + wc * (TN / WC);
+    int c = w0 < w1 ? __builtin_amdgcn_readfirstlane(A.sids[w0]) : -1;
+    while (c >= 0) {
+        const int64_t c0 = A.offsets[c], c1 = A.offsets[c + 1];
+        for (int k0 = 0; k0 < A.rp; k0 += KS) {
+            u32x4 a[FC];
+#pragma unroll
+            for (int h = 0; h < FC; ++h) {
+                const int64_t col = cb + h * 16 + li;
+                const int rr = k0 + g * E;
+                a[h] = zero_chunk<T>();
+                if (col < A.P) {
+                    if constexpr (TR)
+                        a[h] = chunk_guarded(static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.P + col, rr, A.r, A.P);
+                    else
+                        a[h] = chunk(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r, rr, A.r, A.q16);
+                }
+            }
+#pragma unroll
+            for (int f = 0; f < FR; ++f) {
+                const int64_t f0 = w0 + f * 16, place = f0 + li;
+                if (f0 >= c1 || f0 + 16 <= c0) continue;
+                const bool is = place >= c0 && place < c1;
+                const u32x4 b = is ? *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) + place * A.rp + k0 +
+                                                                     g * E)
+                                   : zero_chunk<T>();
+#pragma unroll
+                for (int h = 0; h < FC; ++h) {
+                    const f32x4 d = Mma<T>::mma(a[h], b, acc[f][h]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
+                }
+            }
+        }
+        c = c1 < w1 ? __builtin_amdgcn_readfirstlane(A.sids[c1]) : -1;
+    }
+
+#pragma unroll
+    for (int f = 0; f < FR; ++f) {
+        const int64_t place = w0 + f * 16 + li;
+        if (place >= A.n) continue;
+        T* y = static_cast<T*>(A.Y) + row_of(A.order, place) * A.P;
+#pragma unroll
+        for (int h = 0; h < FC; ++h) store4(y, cb + h * 16 + g * 4, A.P, acc[f][h], A.y4);
+    }
+}
+
+// --------------------------------------------------------------------------
+// Few rows, forward: the time is that of reading W (and the adapters) once.
+
+// h: a wave a (place, index), its lanes along the row.  S is float32 here.
+struct FewArgs {
+    const void* X;
+    int64_t ldx;
+    const void *W, *A, *B;
+    const int32_t *order, *cl;   // cl: the cluster of every place (a plan's), or of every row (order null)
+    const float* scale;
+    float* S;
+    void *H, *Y;
+    int32_t n, K, P, r, k, x16, y4;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
+    constexpr int E = Mma<T>::E;
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= (int64_t)A.n * A.r) return;
+    const int p = (int)(w / A.r), j = (int)(w % A.r);
+    const int c = A.cl[p];
+    const int64_t row = row_of(A.order, p);
+    float sum = 0.0f;
+    const bool in = (unsigned)c < (unsigned)A.k;
+    if (in) {
+        const T* x = static_cast<const T*>(A.X) + row * A.ldx;
+        const T* a = static_cast<const T*>(A.A) + ((int64_t)c * A.r + j) * A.K;
+        if (A.x16) {
+#pragma unroll 4
+            for (int k0 = lane * E; k0 < A.K; k0 += 64 * E) {
+                const Vec<T, E> u = *reinterpret_cast<const Vec<T, E>*>(x + k0);
+                const Vec<T, E> v = *reinterpret_cast<const Vec<T, E>*>(a + k0);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum = fmaf(to_f32(u.e[e]), to_f32(v.e[e]), sum);
+            }
+        } else {
+#pragma unroll 4
+            for (int k0 = lane; k0 < A.K; k0 += 64) sum = fmaf(to_f32(x[k0]), to_f32(a[k0]), sum);
+        }
+    }
+    sum = group_sum<64>(sum);
+    if (lane == 0) {
+        static_cast<T*>(A.H)[row * A.r + j] = from_f32<T>(sum);
+        A.S[(int64_t)p * A.r + j] = in ? sum * (A.scale ? A.scale[c] : 1.0f) : 0.0f;
+    }
+}
+
+// y: 16 columns a block, its 8 waves share the contraction; RF x 16 places.
+template <class T, int RF>
+__global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E;
+    __shared__ f32x4 s_red[8][RF][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
+    const int64_t col0 = (int64_t)blockIdx.x * 16;
+    const int64_t col = col0 + li < A.P ? col0 + li : A.P - 1;
+    const T* w = static_cast<const T*>(A.W) + col * A.K;
+    const T* x[RF];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+        const int p = f * 16 + li < A.n ? f * 16 + li : A.n - 1;
+        x[f] = static_cast<const T*>(A.X) + row_of(A.order, p) * A.ldx;
+    }
+    f32x4 acc[RF];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) acc[f] = f32x4{0, 0, 0, 0};
+    const int steps = (A.K + KS - 1) / KS;
+    for (int s = wave; s < steps; s += 8) {
+        const int64_t k0 = (int64_t)s * KS + g * E;
+        const u32x4 a = chunk(w, k0, A.K, A.x16);
+#pragma unroll
+        for (int f = 0; f < RF; ++f) acc[f] = Mma<T>::mma(a, chunk(x[f], k0, A.K, A.x16), acc[f]);
+    }
+#pragma unroll
+    for (int f = 0; f < RF; ++f) s_red[wave][f][lane] = acc[f];
+    __syncthreads();
+    for (int f = wave; f < RF; f += 8) {
+        const int p = f * 16 + li;
+        if (p >= A.n) continue;
+        f32x4 v{0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v += s_red[q][f][lane];
+        const int c = A.cl[p];
+        const int64_t o0 = col0 + g * 4;
+        if ((unsigned)c < (unsigned)A.k) {
+            const float* s = A.S + (int64_t)p * A.r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (o0 + i >= A.P) continue;
+                const T* b = static_cast<const T*>(A.B) + ((int64_t)c * A.P + o0 + i) * A.r;
+                float d = 0.0f;
+                for (int j = 0; j < A.r; ++j) d = fmaf(s[j], to_f32(b[j]), d);
+                v[i] += d;
+            }
+        }
+        store4(static_cast<T*>(A.Y) + row_of(A.order, p) * A.P, o0, A.P, v, A.y4);
+    }
+}
+
+// --------------------------------------------------------------------------
+// Gradients of the adapters: out_c = sum over the cluster's places of
+// U[row] V[place or row]^T, U wide (P), V r wide.
+
+struct Item {
+    int32_t c, p0, p1, slot;   // places p0 .. p1 of cluster c; slot: partial sum to write, -1: the result itself
+};
+
+// Chunks of every cluster, in order.  One block; lists[0] = number of items.
+struct ListArgs {
+    const int32_t* offsets;
+    int32_t k, chunk;
+    int32_t* count;      // items
+    Item* items;
+    int32_t *first, *num;   // per cluster: first partial slot, chunks (0: empty)
+};
+
+__global__ __launch_bounds__(1024) void k_ad_list(ListArgs A) {
+    __shared__ int s_i[16], s_s[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int items = 0, slots = 0;   // so far
+    for (int c0 = 0; c0 < A.k; c0 += 1024) {
+        const int c = c0 + tid;
+        const int a = c < A.k ? A.offsets[c] : 0, b = c < A.k ? A.offsets[c + 1] : 0;
+        const int ni = (b - a + A.chunk - 1) / A.chunk, ns = ni > 1 ? ni : 0;
+        int xi = ni, xs = ns;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int ui = __shfl_up(xi, o), us = __shfl_up(xs, o);
+            if (lane >= o) xi += ui, xs += us;
+        }
+        if (lane == 63) s_i[wave] = xi, s_s[wave] = xs;
+        __syncthreads();
+        int bi = items, bs = slots;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) bi += s_i[w], bs += s_s[w];
+            items += s_i[w];
+            slots += s_s[w];
+        }
+        bi += xi - ni;
+        bs += xs - ns;
+        if (c < A.k) {
+            A.first[c] = bs;
+            A.num[c] = ni;
+            for (int q = 0; q < ni; ++q) {
+                const int p = a + q * A.chunk;
+                A.items[bi + q] = Item{c, p, b - p < A.chunk ? b : p + A.chunk, ni > 1 ? bs + q : -1};
+            }
+        }
+        __syncthreads();
+    }
+    if (tid == 0) A.count[0] = items;
+}
+
+struct GradArgs {
+    const void* U;
+    int64_t ldu;
+    const void* V;
+    int64_t ldv;
+    int32_t v_by_row;        // V's rows are rows (H), else places (S)
+    const int32_t* order;
+    const float* scale;      // per cluster, or null
+    const int32_t* count;
+    const Item* items;
+    const int32_t *first, *num;
+    void* out;               // WF: k x r x P, else k x P x r
+    float* part;             // slots x r x P, each as out
+    int32_t k, P, r, v16, o4, tiles;   // o4: out written by fours
+};
+
+// 128 columns a block, 32 a wave; stages of 2 KS places.  WF: the wide operand
+// comes first (lanes hold four consecutive columns: dA), else second (four
+// consecutive indexes of r: dB).
+template <class T, int RF, bool WF, bool AL>
+__global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, TC = 128, CPR = TC / E, VPR = RF * 16 / E;
+    constexpr int NU = BK * CPR / 256;
+    __shared__ __align__(16) char s_u[2][BK * TC * sizeof(T)];
+    __shared__ __align__(16) char s_v[2][BK * RF * 16 * sizeof(T)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, li = lane & 15;
+    const int64_t total = (int64_t)A.count[0] * A.tiles;
+    for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+        const Item it = A.items[w / A.tiles];
+        const int64_t bc = (w % A.tiles) * TC;
+        auto load = [&](int64_t p0, int buf) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int q = i * 256 + tid, kk = q / CPR;
+                const int64_t p = p0 + kk, col = bc + swz_tr<T, CPR>(kk, q % CPR) * E;
+                const bool in = p < it.p1;
+                const T* src = static_cast<const T*>(A.U) + (in ? row_of(A.order, p) : 0) * A.ldu;
+                if constexpr (AL)
+                    load_lds16(in && col < A.P ? (const void*)(src + col) : (const void*)ad_zero,
+                               s_u[buf] + (i * 256 + wave * 64) * 16);
+                else
+                    *reinterpret_cast<u32x4*>(s_u[buf] + q * 16) =
+                        in ? chunk_guarded(src, col, A.P) : zero_chunk<T>();
+            }
+            for (int q = tid; q < BK * VPR; q += 256) {
+                const int kk = q / VPR;
+                const int64_t p = p0 + kk;
+                u32x4 v = zero_chunk<T>();
+                if (p < it.p1) {
+                    const T* src = static_cast<const T*>(A.V) + (A.v_by_row ? row_of(A.order, p) : p) * A.ldv;
+                    v = chunk(src, (q % VPR) * E, A.r, A.v16);
+                }
+                *reinterpret_cast<u32x4*>(s_v[buf] + (kk * VPR + swz_tr<T, VPR>(kk, q % VPR)) * 16) = v;
+            }
+        };
+        f32x4 acc[2][RF];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < RF; ++j) acc[h][j] = f32x4{0, 0, 0, 0};
+        int buf = 0;
+        load(it.p0, 0);
+        for (int64_t p = it.p0; p < it.p1; p += BK, buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (p + BK < it.p1) load(p + BK, buf ^ 1);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 a[2], b[RF];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) a[h] = read_tr<T, CPR>(s_u[buf], s * KS, wave * 32 + h * 16, lane);
+#pragma unroll
+                for (int j = 0; j < RF; ++j) b[j] = read_tr<T, VPR>(s_v[buf], s * KS, j * 16, lane);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < RF; ++j)
+                        acc[h][j] = WF ? Mma<T>::mma(a[h], b[j], acc[h][j]) : Mma<T>::mma(b[j], a[h], acc[h][j]);
+            }
+        }
+        __syncthreads();   // both buffers are free for the next item
+        const float sc = A.scale ? A.scale[it.c] : 1.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < RF; ++j) {
+                const int64_t cw = bc + wave * 32 + h * 16;
+                const int64_t slot = it.slot < 0 ? it.c : it.slot;
+                // WF: row rr of r, columns 4 g ..;  else row = column li, indexes 4 g ..
+                const int64_t rr = WF ? j * 16 + li : cw + li, x0 = WF ? cw + g * 4 : j * 16 + g * 4;
+                const int64_t rows = WF ? A.r : A.P, width = WF ? A.P : A.r;
+                if (rr >= rows) continue;
+                const int64_t at = (slot * rows + rr) * width;
+                if (it.slot < 0)
+                    store4(static_cast<T*>(A.out) + at, x0, width, acc[h][j] * sc, A.o4);
+                else
+                    store4(A.part + at, x0, width, acc[h][j] * sc, width % 4 == 0);
+            }
+    }
+}
+
+// Clusters of no chunk: zeros; of several: the sum of their parts in order.
+template <class T>
+__global__ __launch_bounds__(256) void k_ad_join(GradArgs A) {
+    const int64_t size = (int64_t)A.r * A.P;
+    for (int c = blockIdx.y; c < A.k; c += gridDim.y) {
+        const int num = A.num[c];
+        if (num == 1) continue;
+        const float* part = A.part + A.first[c] * size;
+        T* out = static_cast<T*>(A.out) + c * size;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+            float sum = 0.0f;
+            for (int q = 0; q < num; ++q) sum += part[q * size + i];
+            out[i] = from_f32<T>(sum);
+        }
+    }
+}
+
+// --------------------------------------------------------------------------
+// Launches
+
+template <class T, bool TR>
+hipError_t inner_go(const InnerArgs& A, hipStream_t s) {
+    const dim3 g((unsigned)((A.n + 15) / 16)), b(256);
+    const int rf = (A.r + 15) / 16;
+    if (rf == 1) hipLaunchKernelGGL((k_ad_inner<T, 1, TR>), g, b, 0, s, A);
+    else if (rf == 2) hipLaunchKernelGGL((k_ad_inner<T, 2, TR>), g, b, 0, s, A);
+    else if (rf <= 4) hipLaunchKernelGGL((k_ad_inner<T, 4, TR>), g, b, 0, s, A);
+    else hipLaunchKernelGGL((k_ad_inner<T, 8, TR>), g, b, 0, s, A);
+    return hipGetLastError();
+}
+
+template <class K>
+hipError_t raise_lds(K* kernel, int bytes) {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
+hipError_t main_tile(MainArgs A, hipStream_t s) {
+    A.tm = (int)((A.n + TM - 1) / TM);
+    A.tn = (A.P + TN - 1) / TN;
+    constexpr int lds = 2 * (TM + TN) * 128;
+    if (lds > 65536) {
+        const hipError_t e = raise_lds(k_ad_main<T, TM, TN, WR, WC, TR, AL>, lds);
+        if (e != hipSuccess) return e;
+    }
+    const int64_t tiles = (int64_t)A.tm * A.tn;
+    hipLaunchKernelGGL((k_ad_main<T, TM, TN, WR, WC, TR, AL>), dim3((unsigned)((tiles + 7) / 8 * 8)),
+                       dim3(64 * WR * WC), lds, s, A);
+    return hipGetLastError();
+}
+
+template <class T, bool TR>
+hipError_t main_go(const MainArgs& A, bool al, hipStream_t s) {
+    if (!al) return main_tile<T, 64, 64, 2, 2, TR, false>(A, s);
+    auto tiles = [&](int64_t m, int64_t n) { return (A.n + m - 1) / m * ((A.P + n - 1) / n); };
+    if (tiles(256, 256) >= 256) return main_tile<T, 256, 256, 2, 4, TR, true>(A, s);
+    if (tiles(128, 128) >= 256) return main_tile<T, 128, 128, 2, 2, TR, true>(A, s);
+    return main_tile<T, 64, 64, 2, 2, TR, true>(A, s);
+}
+
+template <class T, bool WF>
+hipError_t grad_go(const GradArgs& A, bool al, int64_t max_items, hipStream_t s) {
+    int64_t blocks = max_items * A.tiles;
+    if (blocks > 65536) blocks = 65536;
+    if (blocks < 1) blocks = 1;
+    const dim3 g((unsigned)blocks), b(256);
+    const int rf = (A.r + 15) / 16;
+#define KM_GRAD(RF)                                                                 \
+    do {                                                                            \
+        if (al) hipLaunchKernelGGL((k_ad_grad<T, RF, WF, true>), g, b, 0, s, A);    \
+        else hipLaunchKernelGGL((k_ad_grad<T, RF, WF, false>), g, b, 0, s, A);      \
+    } while (0)
+    if (rf == 1) KM_GRAD(1);
+    else if (rf == 2) KM_GRAD(2);
+    else if (rf <= 4) KM_GRAD(4);
+    else KM_GRAD(8);
+#undef KM_GRAD
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t size = (int64_t)A.r * A.P, gx = (size + 1023) / 1024;
+    hipLaunchKernelGGL((k_ad_join<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(A.k < 128 ? A.k : 128)),
+                       dim3(256), 0, s, A);
+    return hipGetLastError();
+}
+
+bool a16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+template <class T>
+hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipStream_t s) {
+    constexpr int E = Mma<T>::E;
+    const bool x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T)) && a16(D.W) && a16(D.A);
+    const bool y4 = D.dout % 4 == 0 && a16(D.Y);
+    hipError_t e;
+    if (L.few) {
+        FewArgs F{};
+        F.X = D.X;
+        F.ldx = D.ldx;
+        F.W = D.W;
+        F.A = D.A;
+        F.B = D.B;
+        F.order = D.order;
+        F.cl = D.sids ? D.sids : D.ids;
+        F.scale = D.scale;
+        F.S = reinterpret_cast<float*>(ws + L.off_s);
+        F.H = D.H;
+        F.Y = D.Y;
+        F.n = (int32_t)D.n;
+        F.K = D.di;
+        F.P = D.dout;
+        F.r = D.r;
+        F.k = D.k;
+        F.x16 = x16;
+        F.y4 = y4;
+        hipLaunchKernelGGL((k_ad_few_inner<T>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        const dim3 g((unsigned)((D.dout + 15) / 16)), b(512);
+        if (D.n <= 16) hipLaunchKernelGGL((k_ad_few_main<T, 1>), g, b, 0, s, F);
+        else if (D.n <= 32) hipLaunchKernelGGL((k_ad_few_main<T, 2>), g, b, 0, s, F);
+        else hipLaunchKernelGGL((k_ad_few_main<T, 4>), g, b, 0, s, F);
+        return hipGetLastError();
+    }
+    InnerArgs I{};
+    I.U = D.X;
+    I.ldu = D.ldx;
+    I.Q = D.A;
+    I.order = D.order;
+    I.sids = D.sids;
+    I.offsets = D.offsets;
+    I.scale = D.scale;
+    I.S = ws + L.off_s;
+    I.H = D.H;
+    I.n = D.n;
+    I.K = D.di;
+    I.r = D.r;
+    I.rp = L.rp;
+    I.u16 = I.q16 = x16;
+    I.h4 = D.r % 4 == 0 && a16(D.H);
+    if ((e = inner_go<T, false>(I, s)) != hipSuccess) return e;
+    MainArgs M{};
+    M.U = D.X;
+    M.ldu = D.ldx;
+    M.W = D.W;
+    M.Q = D.B;
+    M.S = I.S;
+    M.order = D.order;
+    M.sids = D.sids;
+    M.offsets = D.offsets;
+    M.Y = D.Y;
+    M.n = D.n;
+    M.K = D.di;
+    M.P = D.dout;
+    M.r = D.r;
+    M.rp = L.rp;
+    M.q16 = D.r % E == 0 && a16(D.B);
+    M.y4 = y4;
+    return main_go<T, false>(M, x16, s);
+}
+
+template <class T>
+hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipStream_t s) {
+    constexpr int E = Mma<T>::E;
+    const bool dy16 = rows_vec16(D.dY, D.lddy, D.dout, sizeof(T)), x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T));
+    hipError_t e;
+    char* S = ws + L.off_s;
+    if (D.n > 0) {
+        InnerArgs I{};
+        I.U = D.dY;
+        I.ldu = D.lddy;
+        I.Q = D.B;
+        I.order = D.order;
+        I.sids = D.sids;
+        I.offsets = D.offsets;
+        I.scale = D.scale;
+        I.S = S;
+        I.n = D.n;
+        I.K = D.dout;
+        I.r = D.r;
+        I.rp = L.rp;
+        I.u16 = dy16;
+        if ((e = inner_go<T, true>(I, s)) != hipSuccess) return e;
+        MainArgs M{};
+        M.U = D.dY;
+        M.ldu = D.lddy;
+        M.W = D.W;
+        M.Q = D.A;
+        M.S = S;
+        M.order = D.order;
+        M.sids = D.sids;
+        M.offsets = D.offsets;
+        M.Y = D.dX;
+        M.n = D.n;
+        M.K = D.dout;
+        M.P = D.di;
+        M.r = D.r;
+        M.rp = L.rp;
+        M.y4 = D.di % 4 == 0 && a16(D.dX);
+        if ((e = main_go<T, true>(M, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
+    }
+    ListArgs Q{};
+    Q.offsets = D.offsets;
+    Q.k = D.k;
+    Q.chunk = L.chunk;
+    Q.count = reinterpret_cast<int32_t*>(ws + L.off_count);
+    Q.items = reinterpret_cast<Item*>(ws + L.off_items);
+    Q.first = reinterpret_cast<int32_t*>(ws + L.off_first);
+    Q.num = Q.first + D.k;
+    hipLaunchKernelGGL(k_ad_list, dim3(1), dim3(1024), 0, s, Q);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    GradArgs G{};
+    G.order = D.order;
+    G.count = Q.count;
+    G.items = Q.items;
+    G.first = Q.first;
+    G.num = Q.num;
+    G.k = D.k;
+    G.r = D.r;
+    G.part = reinterpret_cast<float*>(ws + L.off_part);
+    G.U = D.X;
+    G.ldu = D.ldx;
+    G.V = S;
+    G.ldv = L.rp;
+    G.v16 = 1;
+    G.out = D.dA;
+    G.P = D.di;
+    G.tiles = (D.di + 127) / 128;
+    G.o4 = D.di % 4 == 0 && a16(D.dA);
+    GradArgs B = G;
+    B.U = D.dY;
+    B.ldu = D.lddy;
+    B.V = D.H;
+    B.ldv = D.r;
+    B.v_by_row = 1;
+    B.v16 = D.r % E == 0 && a16(D.H);
+    B.scale = D.scale;
+    B.out = D.dB;
+    B.P = D.dout;
+    B.tiles = (D.dout + 127) / 128;
+    B.o4 = D.r % 4 == 0 && a16(D.dB);
+    if ((e = grad_go<T, true>(G, x16, L.max_items, s)) != hipSuccess) return e;
+    return grad_go<T, false>(B, dy16, L.max_items, s);
+}
+
+}  // namespace
+
+AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward) {
+    AdapterShape L{};
+    const int ks = type == kF32 ? 16 : 32;
+    L.rp = (r + ks - 1) / ks * ks;
+    L.few = !backward && n <= kAdapterFew;
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    size_t o = 0;
+    auto take = [&](size_t b) {
+        const size_t at = o;
+        o += up(b);
+        return at;
+    };
+    L.off_s = take(L.few ? (size_t)n * r * 4 : (size_t)n * L.rp * row_type_bytes(type));
+    if (backward) {
+        // Chunks long enough that their float32 sums are a small part of the
+        // rows read, and at most 256 or so of them.
+        const int64_t part = (n / 256 + 63) / 64 * 64;
+        L.chunk = 16 * r > 512 ? 16 * r : 512;
+        if (part > L.chunk) L.chunk = (int32_t)part;
+        const int64_t cuts = n / L.chunk;
+        L.max_items = cuts + (k < n ? k : n);
+        // A cluster of several chunks has one that is not full: at most 2 cuts partial sums.
+        const int64_t slots = 2 * cuts;
+        L.off_count = take(4);
+        L.off_items = take((size_t)L.max_items * sizeof(Item));
+        L.off_first = take((size_t)k * 8);
+        L.off_part = take((size_t)slots * r * (di > dout ? di : dout) * 4);
+    }
+    L.bytes = o > 0 ? o : 256;
+    return L;
+}
+
+hipError_t launch_adapter_forward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s) {
+    if (D.n == 0) return hipSuccess;
+    if (type == kF32) return forward_t<float>(D, ws, L, s);
+    if (type == kBF16) return forward_t<__bf16>(D, ws, L, s);
+    return forward_t<_Float16>(D, ws, L, s);
+}
+
+hipError_t launch_adapter_backward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s) {
+    if (type == kF32) return backward_t<float>(D, ws, L, s);
+    if (type == kBF16) return backward_t<__bf16>(D, ws, L, s);
+    return backward_t<_Float16>(D, ws, L, s);
+}
+
+}  // namespace km

@@ -108,4 +108,31 @@ int norm_bwd_max_blocks(int64_t n, int32_t d, int type);   // most rows of part 
 hipError_t launch_norm_fwd(NormArgs A, int type, hipStream_t s);
 hipError_t launch_norm_bwd(NormArgs A, int type, hipStream_t s);
 
+// ---- shared projection with cluster adapters (km_adapter.hip)
+
+constexpr int kAdapterFew = 64;       // rows up to which the forward pass takes the form for few rows
+constexpr int kAdapterMaxRank = 128;
+
+struct AdapterArgs {
+    const void *X, *dY;
+    int64_t ldx, lddy, n;
+    int32_t di, dout, k, r;
+    const void *W, *A, *B;
+    const int32_t* ids;                         // clusters of the rows (forward, few rows, no plan)
+    const int32_t *order, *sids, *offsets;      // the plan; order null: rows are in its order
+    const float* scale;                         // k, or null (ones)
+    void *Y, *H;                                // H: read backward
+    void *dX, *dA, *dB;
+};
+struct AdapterShape {
+    int32_t rp;          // r padded to a step of the matrix cores
+    int32_t few;         // forward: few rows
+    int32_t chunk;       // backward: rows a chunk
+    int64_t max_items;
+    size_t off_s, off_count, off_items, off_first, off_part, bytes;   // workspace segments
+};
+AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward);
+hipError_t launch_adapter_forward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s);
+hipError_t launch_adapter_backward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s);
+
 }  // namespace km

@@ -246,4 +246,166 @@ int kmeans_norm_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
     return done(km::launch_norm_bwd(A, type, static_cast<hipStream_t>(hip_stream)), "kmeans_norm_backward");
 }
 
+// Forward workspace: the operator's own, then a plan where none is given.
+struct AdapterPlan {
+    km::SortShape sort;
+    size_t order, pos, sids, offsets, ws, bytes;
+};
+static AdapterPlan adapter_plan(int64_t n, int32_t k, size_t at) {
+    AdapterPlan P{};
+    auto take = [&](size_t b) {
+        const size_t here = at;
+        at += (b + 255) / 256 * 256;
+        return here;
+    };
+    P.sort = km::sort_shape(n, k);
+    P.order = take((size_t)n * 4);
+    P.pos = take((size_t)n * 4);
+    P.sids = take((size_t)n * 4);
+    P.offsets = take(((size_t)k + 1) * 4);
+    P.ws = take(P.sort.bytes);
+    P.bytes = at;
+    return P;
+}
+
+static int adapter_sizes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type) {
+    if (!slots_ok(n, 1, k) || din < 1 || dout < 1 || r < 1 || !type_ok(type))
+        return bad("n, din, dout, k, r or type out of range");
+    if (r > km::kAdapterMaxRank)
+        return km::ops_error(KM_ERR_UNSUPPORTED, "adapters have a rank of at most %d", km::kAdapterMaxRank);
+    if (!rows_ok(n, din, din) || !rows_ok(n, dout, dout) || !rows_ok(dout, din, din) ||
+        !rows_ok((int64_t)k * r, din, din) || !rows_ok((int64_t)k * r, dout, dout))
+        return bad("sizes within 63 bits needed");
+    return KM_OK;
+}
+
+size_t kmeans_adapter_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type,
+                                      int32_t backward) {
+    if (adapter_sizes(n, din, dout, k, r, type) != KM_OK) return 0;
+    const km::AdapterShape L = km::adapter_shape(n, din, dout, k, r, type, backward != 0);
+    return backward || L.few ? L.bytes : adapter_plan(n, k, L.bytes).bytes;
+}
+
+int kmeans_adapter_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r,
+                           int32_t type, const void* W, const void* A, const void* B, const float* scale,
+                           const int32_t* ids, const int32_t* order, const int32_t* sorted_ids,
+                           const int32_t* offsets, void* Y, void* H, void* workspace, size_t workspace_bytes,
+                           void* hip_stream) {
+    int rc = adapter_sizes(n, din, dout, k, r, type);
+    if (rc != KM_OK) return rc;
+    if (!rows_ok(n, din, ldx)) return bad("ldx >= din needed, and sizes within 63 bits");
+    if (!W || !A || !B) return bad("W, A or B is null");
+    if (n > 0 && (!X || !Y || !H)) return bad("X, Y or H is null");
+    const bool plan = sorted_ids || offsets || order;
+    if (n > 0 && (plan ? (!sorted_ids || !offsets) : !ids)) return bad("ids, or sorted_ids and offsets, needed");
+    const km::AdapterShape L = km::adapter_shape(n, din, dout, k, r, type, false);
+    const AdapterPlan P = adapter_plan(n, k, L.bytes);
+    const size_t need = plan || L.few ? L.bytes : P.bytes;
+    if ((rc = workspace_ok(workspace, workspace_bytes, need)) != KM_OK) return rc;
+    if (n == 0) return KM_OK;
+    const size_t es = km::row_type_bytes(type);
+    Checks C;
+    C.rows(X, n, din, ldx, type, "X");
+    C.array(W, (size_t)din * dout * es, "W");
+    C.array(A, (size_t)k * r * din * es, "A");
+    C.array(B, (size_t)k * r * dout * es, "B");
+    if (scale) C.array(scale, (size_t)k * 4, "scale");
+    if (plan) {
+        if (order) C.array(order, (size_t)n * 4, "order");
+        C.array(sorted_ids, (size_t)n * 4, "sorted_ids");
+        C.array(offsets, ((size_t)k + 1) * 4, "offsets");
+    } else {
+        C.array(ids, (size_t)n * 4, "ids");
+    }
+    C.array(Y, (size_t)n * dout * es, "Y");
+    C.array(H, (size_t)n * r * es, "H");
+    C.array(workspace, need, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    char* ws = static_cast<char*>(workspace);
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    km::AdapterArgs D{};
+    D.X = X;
+    D.ldx = ldx;
+    D.n = n;
+    D.di = din;
+    D.dout = dout;
+    D.k = k;
+    D.r = r;
+    D.W = W;
+    D.A = A;
+    D.B = B;
+    D.ids = ids;
+    D.order = order;
+    D.sids = sorted_ids;
+    D.offsets = offsets;
+    D.scale = scale;
+    D.Y = Y;
+    D.H = H;
+    if (!plan && !L.few) {
+        auto at = [&](size_t o) { return reinterpret_cast<int32_t*>(ws + o); };
+        const km::SortArgs S{ids, (int32_t)n, k, at(P.order), at(P.pos), at(P.sids), at(P.offsets)};
+        const hipError_t e = km::launch_sort_plan(S, P.sort, ws + P.ws, st);
+        if (e != hipSuccess) return km::ops_hip_error(e, "kmeans_adapter_forward");
+        D.order = S.order;
+        D.sids = S.sorted_ids;
+        D.offsets = S.offsets;
+    }
+    return done(km::launch_adapter_forward(D, ws, L, type, st), "kmeans_adapter_forward");
+}
+
+int kmeans_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* H, int64_t n,
+                            int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type, const void* W,
+                            const void* A, const void* B, const float* scale, const int32_t* order,
+                            const int32_t* sorted_ids, const int32_t* offsets, void* dX, void* dA, void* dB,
+                            void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = adapter_sizes(n, din, dout, k, r, type);
+    if (rc != KM_OK) return rc;
+    if (!rows_ok(n, din, ldx) || !rows_ok(n, dout, lddy)) return bad("ldx >= din and lddy >= dout needed");
+    if (!W || !A || !B || !offsets || !dA || !dB) return bad("W, A, B, offsets, dA or dB is null");
+    if (n > 0 && (!dY || !X || !H || !dX || !sorted_ids)) return bad("dY, X, H, dX or sorted_ids is null");
+    const km::AdapterShape L = km::adapter_shape(n, din, dout, k, r, type, true);
+    if ((rc = workspace_ok(workspace, workspace_bytes, L.bytes)) != KM_OK) return rc;
+    const size_t es = km::row_type_bytes(type);
+    Checks C;
+    C.rows(dY, n, dout, lddy, type, "dY");
+    C.rows(X, n, din, ldx, type, "X");
+    C.array(H, (size_t)n * r * es, "H");
+    C.array(W, (size_t)din * dout * es, "W");
+    C.array(A, (size_t)k * r * din * es, "A");
+    C.array(B, (size_t)k * r * dout * es, "B");
+    if (scale) C.array(scale, (size_t)k * 4, "scale");
+    if (order) C.array(order, (size_t)n * 4, "order");
+    C.array(sorted_ids, (size_t)n * 4, "sorted_ids");
+    C.array(offsets, ((size_t)k + 1) * 4, "offsets");
+    C.array(dX, (size_t)n * din * es, "dX");
+    C.array(dA, (size_t)k * r * din * es, "dA");
+    C.array(dB, (size_t)k * r * dout * es, "dB");
+    C.array(workspace, L.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    km::AdapterArgs D{};
+    D.dY = dY;
+    D.lddy = lddy;
+    D.X = X;
+    D.ldx = ldx;
+    D.H = const_cast<void*>(H);
+    D.n = n;
+    D.di = din;
+    D.dout = dout;
+    D.k = k;
+    D.r = r;
+    D.W = W;
+    D.A = A;
+    D.B = B;
+    D.scale = scale;
+    D.order = order;
+    D.sids = sorted_ids;
+    D.offsets = offsets;
+    D.dX = dX;
+    D.dA = dA;
+    D.dB = dB;
+    return done(km::launch_adapter_backward(D, static_cast<char*>(workspace), L, type,
+                                            static_cast<hipStream_t>(hip_stream)),
+                "kmeans_adapter_backward");
+}
+
 }  // extern "C"

@@ -6,7 +6,9 @@ tokens of a model, embeddings -- to small experts of their clusters:
   cluster_sort, cluster_gather, cluster_combine, cluster_combine_backward
       rows sorted by cluster and back with weights, and the gradients;
   layernorm, layernorm_backward
-      the normalisation in front of them.
+      the normalisation in front of them;
+  adapter_linear, adapter_linear_backward
+      a shared projection with one low-rank adapter per cluster.
 
 As in :mod:`.kmeans`, this is argument marshalling only: tensors are checked
 and handed to the kernels of ``libkmeans_mti.so``.  Rows are float32, bfloat16
@@ -278,3 +280,100 @@ def layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rs
                                       _p(weight), f32, _p(dx), _p(dg), _p(db), _p(ws), ws.numel(), s)
     N.check(st, "kmeans_norm_backward")
     return dx, dg, db
+
+
+def _adapters(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+              scale: Optional[torch.Tensor]) -> Tuple[int, int, int, int]:
+    """Check the weights of an adapter projection; (din, dout, k, r)."""
+    for t, name, dims in ((W, "W", 2), (A, "A", 3), (B, "B", 3)):
+        _gpu(t, name, X.device)
+        if t.dim() != dims or 0 in t.shape:
+            raise ValueError("%s must be a non-empty %d-D tensor" % (name, dims))
+    (dout, din), (k, r) = W.shape, A.shape[:2]
+    if X.shape[1] != din:
+        raise ValueError("X must have %d columns" % din)
+    _array(W, "W", X.dtype, (dout, din), X.device)
+    _array(A, "A", X.dtype, (k, r, din), X.device)
+    _array(B, "B", X.dtype, (k, dout, r), X.device)
+    if scale is not None:
+        _array(scale, "scale", torch.float32, (k,), X.device)
+    return din, dout, k, r
+
+
+def _places(plan: ClusterPlan, n: int, k: int, device: torch.device, sorted_rows: bool) -> Optional[torch.Tensor]:
+    """Check a plan for n rows; its order, or None where the rows are in it already."""
+    _plan(plan, device)
+    if plan.k != k:
+        raise ValueError("plan has %d clusters, A has %d" % (plan.k, k))
+    if plan.m != 1 and not sorted_rows:
+        raise ValueError("a plan of m = %d slots a row needs sorted rows (cluster_gather)" % plan.m)
+    if plan.n * plan.m != n:
+        raise ValueError("plan has %d places, X %d rows" % (plan.n * plan.m, n))
+    return None if sorted_rows else plan.order
+
+
+def adapter_linear(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor, clusters,
+                   scale: Optional[torch.Tensor] = None, sorted_rows: bool = False,
+                   stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A shared projection with one low-rank adapter per cluster
+    (kmeans_adapter_forward): for a row x of cluster c, h = A[c] x and
+    y = W x + scale[c] B[c] h; a row in no cluster has h = 0, y = W x.
+
+    W [dout, din], A [k, r, din], B [k, dout, r] (r up to 128) and X are of
+    one type; scale is float32 [k] or None (ones).  ``clusters``: int32 ids
+    [n], or a :class:`ClusterPlan` (with ``sorted_rows``, X is in the plan's
+    order: the output of :func:`cluster_gather`).  Returns (Y [n, dout],
+    H [n, r]); :func:`adapter_linear_backward` reads H.
+    """
+    ld = _rows(X, "X")
+    din, dout, k, r = _adapters(X, W, A, B, scale)
+    n, dev = X.shape[0], X.device
+    ids = order = sids = offsets = None
+    if isinstance(clusters, ClusterPlan):
+        order = _places(clusters, n, k, dev, sorted_rows)
+        sids, offsets = clusters.sorted_ids, clusters.offsets
+    else:
+        if sorted_rows:
+            raise ValueError("sorted rows need a plan")
+        _array(clusters, "clusters", torch.int32, (n,), dev)
+        ids = clusters
+    lib = N.load()
+    need = lib.kmeans_adapter_workspace_bytes(n, din, dout, k, r, _TYPES[X.dtype], 0)
+    if need == 0 and r > 128:
+        raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_adapter_forward", "adapters have a rank of at most 128")
+    with _On(dev, stream, X, W, A, B, ids, order, sids, offsets, scale) as s:
+        y = torch.empty(n, dout, dtype=X.dtype, device=dev)
+        h = torch.empty(n, r, dtype=X.dtype, device=dev)
+        ws = _workspace(need, dev, "kmeans_adapter_workspace_bytes")
+        st = lib.kmeans_adapter_forward(_p(X), ld, n, din, dout, k, r, _TYPES[X.dtype], _p(W), _p(A), _p(B),
+                                        _p(scale), _p(ids), _p(order), _p(sids), _p(offsets), _p(y), _p(h),
+                                        _p(ws), ws.numel(), s)
+    N.check(st, "kmeans_adapter_forward")
+    return y, h
+
+
+def adapter_linear_backward(dY: torch.Tensor, X: torch.Tensor, H: torch.Tensor, W: torch.Tensor, A: torch.Tensor,
+                            B: torch.Tensor, plan: ClusterPlan, scale: Optional[torch.Tensor] = None,
+                            sorted_rows: bool = False, stream: Optional[torch.cuda.Stream] = None
+                            ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients of :func:`adapter_linear` (kmeans_adapter_backward): (dX, dA,
+    dB), of the rows' type; W is frozen."""
+    ld = _rows(X, "X")
+    din, dout, k, r = _adapters(X, W, A, B, scale)
+    n, dev = X.shape[0], X.device
+    ldy = _rows(dY, "dY", like=X, n=n, d=dout)
+    _array(H, "H", X.dtype, (n, r), dev)
+    order = _places(plan, n, k, dev, sorted_rows)
+    lib = N.load()
+    need = lib.kmeans_adapter_workspace_bytes(n, din, dout, k, r, _TYPES[X.dtype], 1)
+    if need == 0 and r > 128:
+        raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_adapter_backward", "adapters have a rank of at most 128")
+    with _On(dev, stream, dY, X, H, W, A, B, order, plan.sorted_ids, plan.offsets, scale) as s:
+        dx = torch.empty(n, din, dtype=X.dtype, device=dev)
+        da, db = torch.empty_like(A), torch.empty_like(B)
+        ws = _workspace(need, dev, "kmeans_adapter_workspace_bytes")
+        st = lib.kmeans_adapter_backward(_p(dY), ldy, _p(X), ld, _p(H), n, din, dout, k, r, _TYPES[X.dtype], _p(W),
+                                         _p(A), _p(B), _p(scale), _p(order), _p(plan.sorted_ids),
+                                         _p(plan.offsets), _p(dx), _p(da), _p(db), _p(ws), ws.numel(), s)
+    N.check(st, "kmeans_adapter_backward")
+    return dx, da, db

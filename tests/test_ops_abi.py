@@ -58,6 +58,26 @@ def test_norm_refusals():
     assert [bwd(ws=None), bwd(wsb=need - 1), bwd(ws=C.c_void_p(0x1010)), bwd(dy=None), bwd(ld=63)] == [BAD] * 5
 
 
+def test_adapter_refusals():
+    lib = N.load()
+    size = lambda n=100, di=64, do=32, k=4, r=8, t=1, b=0: lib.kmeans_adapter_workspace_bytes(n, di, do, k, r, t, b)
+    assert size() > 0 and size(b=1) > 0 and size(n=0) > 0
+    assert [size(n=-1), size(n=2 ** 31), size(di=0), size(do=0), size(k=0), size(r=0), size(t=3), size(r=129)] == [0] * 8
+
+    def fwd(X=FAKE, ldx=64, n=100, r=8, W=FAKE, ids=FAKE, order=None, sids=None, off=None, ws=FAKE, wsb=size()):
+        return lib.kmeans_adapter_forward(X, ldx, n, 64, 32, 4, r, 1, W, FAKE, FAKE, None, ids, order, sids, off, FAKE,
+                                          FAKE, ws, wsb, None)
+    assert [fwd(X=None), fwd(ldx=63), fwd(n=-1), fwd(W=None), fwd(ids=None), fwd(ids=None, order=FAKE),
+            fwd(ids=None, sids=FAKE), fwd(ws=None), fwd(wsb=size() - 1), fwd(ws=C.c_void_p(0x1010))] == [BAD] * 10
+    assert fwd(r=129) == N.KM_ERR_UNSUPPORTED
+
+    def bwd(dY=FAKE, H=FAKE, n=100, sids=FAKE, off=FAKE, dA=FAKE, wsb=size(b=1)):
+        return lib.kmeans_adapter_backward(dY, 32, FAKE, 64, H, n, 64, 32, 4, 8, 1, FAKE, FAKE, FAKE, None, None, sids,
+                                           off, FAKE, dA, FAKE, FAKE, wsb, None)
+    assert [bwd(dY=None), bwd(H=None), bwd(n=-1), bwd(sids=None), bwd(off=None), bwd(dA=None),
+            bwd(wsb=size(b=1) - 1)] == [BAD] * 7
+
+
 def test_binding_rejects_cpu_tensors():
     import torch
     import paper_1902_09527_amd as km
