@@ -33,38 +33,61 @@ __device__ __forceinline__ float row_sum(float v, float (*s)[4], int slot) {
     }
 }
 
-__device__ __forceinline__ float param_at(const void* p, int f32, int type, int64_t i) {
-    if (f32 || type == kF32) return static_cast<const float*>(p)[i];
-    if (type == kBF16) return (float)static_cast<const __bf16*>(p)[i];
-    return (float)static_cast<const _Float16*>(p)[i];
-}
-
-template <class T>
-constexpr int type_of() {
-    return sizeof(T) == 4 ? kF32 : __is_same(T, __bf16) ? kBF16 : kF16;
+// V consecutive parameters (of type P) from column c; `fill` where there are
+// none.  V > 1: c is a multiple of V and p 16-byte aligned.
+template <class P, int V>
+__device__ __forceinline__ void params(const void* p, int64_t c, float fill, float* out) {
+    constexpr int S = V * sizeof(P) > 16 ? 16 / (int)sizeof(P) : V;
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = fill;
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < V / S; ++q) {
+        const Vec<P, S> v = *reinterpret_cast<const Vec<P, S>*>(static_cast<const P*>(p) + c + q * S);
+#pragma unroll
+        for (int e = 0; e < S; ++e) out[q * S + e] = to_f32(v.e[e]);
+    }
 }
 
 // R steps of V elements a lane: d <= L R V.
-template <class T, int V, int L, int R>
+template <class T, class P, int V, int L, int R>
 __global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs A) {
     using W = Vec<T, V>;
     __shared__ float s_red[2][4];
     const int l = threadIdx.x % L, nv = A.d / V;
     const float dim = (float)A.d;
-    constexpr int TY = type_of<T>();
+    float g[R][V], b[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool in = l + r * L < nv;
+        params<P, V>(in ? A.gamma : nullptr, (int64_t)(l + r * L) * V, 1.0f, g[r]);
+        params<P, V>(in ? A.beta : nullptr, (int64_t)(l + r * L) * V, 0.0f, b[r]);
+    }
     const int64_t step = (int64_t)gridDim.x * (kNormThreads / L);
-    for (int64_t i = (int64_t)blockIdx.x * (kNormThreads / L) + threadIdx.x / L; i < A.n; i += step) {
-        const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx);
+    int64_t i = (int64_t)blockIdx.x * (kNormThreads / L) + threadIdx.x / L;
+    // The next row's loads are in flight while a row is worked on.
+    W nx[R];
+    auto fetch = [&](int64_t q) {
+        const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + q * A.ldx);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (l + r * L < nv) nx[r] = x[l + r * L];
+    };
+    if (i < A.n) fetch(i);
+    for (; i < A.n; i += step) {
         W* y = reinterpret_cast<W*>(static_cast<T*>(A.Y) + i * A.d);
         W v[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) v[r] = nx[r];
+        if (i + step < A.n) fetch(i + step);
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (l + r * L < nv) {
-                v[r] = x[l + r * L];
+            if (l + r * L < nv)
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum += to_f32(v[r].e[e]);
-            }
         const float mu = row_sum<L>(sum, s_red, 0) / dim;
         float sq = 0.0f;
 #pragma unroll
@@ -84,26 +107,21 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs A) {
         for (int r = 0; r < R; ++r)
             if (l + r * L < nv) {
                 W o;
-                const int64_t c = (int64_t)(l + r * L) * V;
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float g = A.gamma ? param_at(A.gamma, A.param_f32, TY, c + e) : 1.0f;
-                    const float b = A.beta ? param_at(A.beta, A.param_f32, TY, c + e) : 0.0f;
-                    o.e[e] = from_f32<T>(fmaf((to_f32(v[r].e[e]) - mu) * rs, g, b));
-                }
+                for (int e = 0; e < V; ++e)
+                    o.e[e] = from_f32<T>(fmaf((to_f32(v[r].e[e]) - mu) * rs, g[r][e], b[r][e]));
                 y[l + r * L] = o;
             }
     }
 }
 
 // Rows wider than the registers: a block a row, read three times (twice from cache).
-template <class T, int V>
+template <class T, class P, int V>
 __global__ __launch_bounds__(kNormThreads) void k_norm_fwd_wide(NormArgs A) {
     using W = Vec<T, V>;
     __shared__ float s_red[2][4];
     const int nv = A.d / V;
     const float dim = (float)A.d;
-    constexpr int TY = type_of<T>();
     for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
         const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx);
         W* y = reinterpret_cast<W*>(static_cast<T*>(A.Y) + i * A.d);
@@ -133,47 +151,58 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd_wide(NormArgs A) {
         for (int c = threadIdx.x; c < nv; c += kNormThreads) {
             const W v = x[c];
             W o;
+            float g[V], b[V];
+            params<P, V>(A.gamma, (int64_t)c * V, 1.0f, g);
+            params<P, V>(A.beta, (int64_t)c * V, 0.0f, b);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int64_t q = (int64_t)c * V + e;
-                const float g = A.gamma ? param_at(A.gamma, A.param_f32, TY, q) : 1.0f;
-                const float b = A.beta ? param_at(A.beta, A.param_f32, TY, q) : 0.0f;
-                o.e[e] = from_f32<T>(fmaf((to_f32(v.e[e]) - mu) * rs, g, b));
-            }
+            for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(fmaf((to_f32(v.e[e]) - mu) * rs, g[e], b[e]));
             y[c] = o;
         }
     }
 }
 
-template <class T, int V, int L, int R>
+template <class T, class P, int V, int L, int R>
 __global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs A) {
     using W = Vec<T, V>;
     __shared__ float s_red[2][4];
-    constexpr int TY = type_of<T>(), kGroups = kNormThreads / L;
+    constexpr int kGroups = kNormThreads / L;
     const int l = threadIdx.x % L, nv = A.d / V;
     const float dim = (float)A.d;
     float g[R][V], dg[R][V], db[R][V];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        params<P, V>(l + r * L < nv ? A.gamma : nullptr, (int64_t)(l + r * L) * V, 1.0f, g[r]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            dg[r][e] = db[r][e] = 0.0f;
-            const int64_t c = (int64_t)(l + r * L) * V + e;
-            g[r][e] = A.gamma && l + r * L < nv ? param_at(A.gamma, A.param_f32, TY, c) : 1.0f;
-        }
+        for (int e = 0; e < V; ++e) dg[r][e] = db[r][e] = 0.0f;
+    }
     const int64_t step = (int64_t)gridDim.x * kGroups;
-    for (int64_t i = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; i < A.n; i += step) {
-        const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx);
-        const W* __restrict__ y = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + i * A.lddy);
-        W* dx = reinterpret_cast<W*>(static_cast<T*>(A.dX) + i * A.d);
-        const float mu = A.mean[i], rs = A.rstd[i];
-        W vx[R], vy[R];
+    int64_t i = (int64_t)blockIdx.x * kGroups + threadIdx.x / L;
+    // The next row's loads are in flight while a row is worked on.
+    W nx[R], ny[R];
+    float nmu = 0.0f, nrs = 0.0f;
+    auto fetch = [&](int64_t q) {
+        const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + q * A.ldx);
+        const W* __restrict__ y = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + q * A.lddy);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (l + r * L < nv) {
-                vx[r] = x[l + r * L];
-                vy[r] = y[l + r * L];
+                nx[r] = x[l + r * L];
+                ny[r] = y[l + r * L];
             }
+        nmu = A.mean[q];
+        nrs = A.rstd[q];
+    };
+    if (i < A.n) fetch(i);
+    for (; i < A.n; i += step) {
+        W* dx = reinterpret_cast<W*>(static_cast<T*>(A.dX) + i * A.d);
+        const float mu = nmu, rs = nrs;
+        W vx[R], vy[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            vx[r] = nx[r];
+            vy[r] = ny[r];
+        }
+        if (i + step < A.n) fetch(i + step);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -246,11 +275,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs A) {
 
 // Wide rows: a block a row; its sums of dg and db stay in its own row of
 // part, each column owned by one lane.
-template <class T, int V>
+template <class T, class P, int V>
 __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
     using W = Vec<T, V>;
     __shared__ float s_red[2][4];
-    constexpr int TY = type_of<T>();
     const int nv = A.d / V;
     const float dim = (float)A.d;
     float* out = A.part ? A.part + (int64_t)blockIdx.x * 2 * A.d : nullptr;
@@ -264,11 +292,12 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
 #pragma unroll 2
         for (int c = threadIdx.x; c < nv; c += kNormThreads) {
             const W vx = x[c], vy = y[c];
+            float g[V];
+            params<P, V>(A.gamma, (int64_t)c * V, 1.0f, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const int64_t q = (int64_t)c * V + e;
-                const float g = A.gamma ? param_at(A.gamma, A.param_f32, TY, q) : 1.0f;
-                const float xh = (to_f32(vx.e[e]) - mu) * rs, dy = to_f32(vy.e[e]), h = dy * g;
+                const float xh = (to_f32(vx.e[e]) - mu) * rs, dy = to_f32(vy.e[e]), h = dy * g[e];
                 s1 += h;
                 s2 = fmaf(h, xh, s2);
                 if (out) {
@@ -283,11 +312,11 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
         for (int c = threadIdx.x; c < nv; c += kNormThreads) {
             const W vx = x[c], vy = y[c];
             W o;
+            float g[V];
+            params<P, V>(A.gamma, (int64_t)c * V, 1.0f, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const int64_t q = (int64_t)c * V + e;
-                const float g = A.gamma ? param_at(A.gamma, A.param_f32, TY, q) : 1.0f;
-                const float xh = (to_f32(vx.e[e]) - mu) * rs, h = to_f32(vy.e[e]) * g;
+                const float xh = (to_f32(vx.e[e]) - mu) * rs, h = to_f32(vy.e[e]) * g[e];
                 o.e[e] = from_f32<T>(rs * (h - s1 - xh * s2));
             }
             dx[c] = o;
@@ -295,25 +324,27 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
     }
 }
 
-// dg and db: 64 columns a block, 4 waves take every fourth row of part.
-__global__ __launch_bounds__(256) void k_norm_sums(NormArgs A) {
-    __shared__ float s[2][4][64];
+// dg (blockIdx.y = 0) and db: 64 columns a block, 16 waves take every 16th
+// row of part; their sums are added in wave order.
+__global__ __launch_bounds__(1024) void k_norm_sums(NormArgs A) {
+    __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + lane;
-    float g = 0.0f, b = 0.0f;
+    float* out = blockIdx.y ? A.dbeta : A.dgamma;
+    if (!out) return;
+    float sum = 0.0f;
     if (c < A.d) {
-#pragma unroll 4
-        for (int r = wave; r < A.blocks; r += 4) {
-            g += A.part[(int64_t)r * 2 * A.d + c];
-            b += A.part[(int64_t)r * 2 * A.d + A.d + c];
-        }
+        const float* p = A.part + (blockIdx.y ? A.d : 0) + c;
+#pragma unroll 8
+        for (int r = wave; r < A.blocks; r += 16) sum += p[(int64_t)r * 2 * A.d];
     }
-    s[0][wave][lane] = g;
-    s[1][wave][lane] = b;
+    s[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && c < A.d) {
-        if (A.dgamma) A.dgamma[c] = (s[0][0][lane] + s[0][1][lane]) + (s[0][2][lane] + s[0][3][lane]);
-        if (A.dbeta) A.dbeta[c] = (s[1][0][lane] + s[1][1][lane]) + (s[1][2][lane] + s[1][3][lane]);
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) sum += s[w][lane];
+        out[c] = sum;
     }
 }
 
@@ -332,70 +363,76 @@ Shape norm_shape(int nv) {
     return {256, 0};
 }
 
+// Blocks of the backward pass: two rows a group of lanes where the rows are
+// few, and at most 512 (each writes its sums of dg and db). Fewer vectors a
+// row never make more blocks.
 int bwd_blocks(int64_t n, int nv) {
-    const int64_t groups = kNormThreads / norm_shape(nv).L, b = (n + 8 * groups - 1) / (8 * groups);
+    const int64_t groups = kNormThreads / norm_shape(nv).L, b = (n + 2 * groups - 1) / (2 * groups);
     return (int)(b < 1 ? 1 : b > 512 ? 512 : b);
 }
 
-template <class T, int V, int L, int R>
+template <class T, class P, int V, int L, int R>
 hipError_t norm_go(const NormArgs& A, bool bwd, hipStream_t s) {
     const int groups = kNormThreads / L;
     if (bwd) {
         const size_t lds = A.part && groups > 1 ? (size_t)(groups - 1) * 2 * R * V * L * 4 : 0;
-        hipLaunchKernelGGL((k_norm_bwd<T, V, L, R>), dim3((unsigned)A.blocks), dim3(kNormThreads), lds, s, A);
+        hipLaunchKernelGGL((k_norm_bwd<T, P, V, L, R>), dim3((unsigned)A.blocks), dim3(kNormThreads), lds, s, A);
     } else {
+        // At most 2048 blocks (8 a compute unit): gamma and beta are loaded once a block.
         int64_t b = (A.n + groups - 1) / groups;
-        if (b > 32768) b = 32768;
-        hipLaunchKernelGGL((k_norm_fwd<T, V, L, R>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
+        if (b > 2048) b = 2048;
+        hipLaunchKernelGGL((k_norm_fwd<T, P, V, L, R>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
     }
     return hipGetLastError();
 }
 
-template <class T, int V>
+template <class T, class P, int V>
 hipError_t norm_vec(const NormArgs& A, bool bwd, hipStream_t s) {
     const Shape S = norm_shape(A.d / V);
-    if (S.L == 8) return norm_go<T, V, 8, 1>(A, bwd, s);
-    if (S.L == 32) return norm_go<T, V, 32, 1>(A, bwd, s);
-    if (S.L == 64 && S.R == 1) return norm_go<T, V, 64, 1>(A, bwd, s);
-    if (S.L == 64 && S.R == 2) return norm_go<T, V, 64, 2>(A, bwd, s);
-    if (S.L == 64 && S.R == 4) return norm_go<T, V, 64, 4>(A, bwd, s);
-    if (S.R == 2) return norm_go<T, V, 256, 2>(A, bwd, s);
-    if (S.R == 4) return norm_go<T, V, 256, 4>(A, bwd, s);
+    if (S.L == 8) return norm_go<T, P, V, 8, 1>(A, bwd, s);
+    if (S.L == 32) return norm_go<T, P, V, 32, 1>(A, bwd, s);
+    if (S.L == 64 && S.R == 1) return norm_go<T, P, V, 64, 1>(A, bwd, s);
+    if (S.L == 64 && S.R == 2) return norm_go<T, P, V, 64, 2>(A, bwd, s);
+    if (S.L == 64 && S.R == 4) return norm_go<T, P, V, 64, 4>(A, bwd, s);
+    if (S.R == 2) return norm_go<T, P, V, 256, 2>(A, bwd, s);
+    if (S.R == 4) return norm_go<T, P, V, 256, 4>(A, bwd, s);
     if (bwd) {
-        hipLaunchKernelGGL((k_norm_bwd_wide<T, V>), dim3((unsigned)A.blocks), dim3(kNormThreads), 0, s, A);
+        hipLaunchKernelGGL((k_norm_bwd_wide<T, P, V>), dim3((unsigned)A.blocks), dim3(kNormThreads), 0, s, A);
     } else {
         const int64_t b = A.n < 32768 ? A.n : 32768;
-        hipLaunchKernelGGL((k_norm_fwd_wide<T, V>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
+        hipLaunchKernelGGL((k_norm_fwd_wide<T, P, V>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
     }
     return hipGetLastError();
 }
 
-template <class T>
+// 16 bytes a lane where the rows allow it, else two elements, else one.
+template <class T, class P>
 hipError_t norm_type(NormArgs& A, bool bwd, hipStream_t s) {
-    bool vec = rows_vec16(A.X, A.ldx, A.d, sizeof(T));
-    if (bwd)
-        vec = vec && rows_vec16(A.dY, A.lddy, A.d, sizeof(T)) && rows_vec16(A.dX, A.d, A.d, sizeof(T));
-    else
-        vec = vec && rows_vec16(A.Y, A.d, A.d, sizeof(T));
-    constexpr int V = 16 / (int)sizeof(T);
-    A.blocks = bwd_blocks(A.n, vec ? A.d / V : A.d);
-    return vec ? norm_vec<T, V>(A, bwd, s) : norm_vec<T, 1>(A, bwd, s);
+    constexpr int E = (int)sizeof(T), V = 16 / E;
+    auto fits = [&](int bytes) {
+        bool ok = rows_vec(A.X, A.ldx, A.d, E, bytes);
+        if (bwd)
+            ok = ok && rows_vec(A.dY, A.lddy, A.d, E, bytes) && rows_vec(A.dX, A.d, A.d, E, bytes);
+        else
+            ok = ok && rows_vec(A.Y, A.d, A.d, E, bytes);
+        const int pb = bytes / E * (int)sizeof(P) < 16 ? bytes / E * (int)sizeof(P) : 16;   // one parameter load
+        return ok && ((uintptr_t)A.gamma | (uintptr_t)A.beta) % pb == 0;
+    };
+    const int v = fits(16) ? V : fits(2 * E) ? 2 : 1;
+    A.blocks = bwd_blocks(A.n, A.d / v);
+    if (v == V) return norm_vec<T, P, V>(A, bwd, s);
+    return v == 2 ? norm_vec<T, P, 2>(A, bwd, s) : norm_vec<T, P, 1>(A, bwd, s);
 }
 
 hipError_t norm_any(NormArgs& A, bool bwd, int type, hipStream_t s) {
-    if (type == kF32) return norm_type<float>(A, bwd, s);
-    if (type == kBF16) return norm_type<__bf16>(A, bwd, s);
-    return norm_type<_Float16>(A, bwd, s);
+    if (type == kF32) return norm_type<float, float>(A, bwd, s);
+    if (type == kBF16) return A.param_f32 ? norm_type<__bf16, float>(A, bwd, s) : norm_type<__bf16, __bf16>(A, bwd, s);
+    return A.param_f32 ? norm_type<_Float16, float>(A, bwd, s) : norm_type<_Float16, _Float16>(A, bwd, s);
 }
 
 }  // namespace
 
-// Blocks of the backward pass: at least 8 rows a group of lanes where there
-// are that many, and at most 512.
-int norm_bwd_max_blocks(int64_t n, int32_t d, int type) {
-    const int a = bwd_blocks(n, d), b = bwd_blocks(n, (int)(d * row_type_bytes(type) / 16));
-    return a > b ? a : b;
-}
+int norm_bwd_max_blocks(int64_t n, int32_t d) { return bwd_blocks(n, d); }
 
 hipError_t launch_norm_fwd(NormArgs A, int type, hipStream_t s) {
     return A.n == 0 ? hipSuccess : norm_any(A, false, type, s);
@@ -408,7 +445,7 @@ hipError_t launch_norm_bwd(NormArgs A, int type, hipStream_t s) {
     }
     if (!A.dgamma && !A.dbeta) return hipSuccess;
     // No rows: blocks is 0 and the sums are zeros.
-    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((A.d + 63) / 64)), dim3(256), 0, s, A);
+    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((A.d + 63) / 64), 2), dim3(1024), 0, s, A);
     return hipGetLastError();
 }
 

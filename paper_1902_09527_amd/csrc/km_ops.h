@@ -30,19 +30,39 @@ __device__ __forceinline__ T from_f32(float v) {
 }
 
 // Sum over groups of W consecutive lanes (W a power of two up to 64), the
-// same value in every lane of a group.
+// same value in every lane of a group.  Cross-lane moves within the vector
+// unit, no LDS: quads by permutation, 8 and 16 lanes by mirroring (the parts
+// are uniform by then), 32 and 64 by swapping rows.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    const int i = __builtin_bit_cast(int, v);
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false));
+}
 template <int W>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if constexpr (W >= 2) v = add_dpp<0xb1>(v);    // quad_perm 1,0,3,2
+    if constexpr (W >= 4) v = add_dpp<0x4e>(v);    // quad_perm 2,3,0,1
+    if constexpr (W >= 8) v = add_dpp<0x141>(v);   // row_half_mirror
+    if constexpr (W >= 16) v = add_dpp<0x140>(v);  // row_mirror
+    if constexpr (W >= 32) {
+        const uint32_t i = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+        v = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
+    if constexpr (W >= 64) {
+        const uint32_t i = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+        v = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
     return v;
 }
 
 // Whether rows at p with row stride ld (elements of es bytes) and width d can
-// be moved 16 bytes at a time.
-inline bool rows_vec16(const void* p, int64_t ld, int64_t d, size_t es) {
-    return ((uintptr_t)p & 15) == 0 && (ld * (int64_t)es) % 16 == 0 && (d * (int64_t)es) % 16 == 0;
+// be moved `bytes` at a time.
+inline bool rows_vec(const void* p, int64_t ld, int64_t d, size_t es, int bytes) {
+    return (uintptr_t)p % bytes == 0 && (ld * (int64_t)es) % bytes == 0 && (d * (int64_t)es) % bytes == 0;
 }
+inline bool rows_vec16(const void* p, int64_t ld, int64_t d, size_t es) { return rows_vec(p, ld, d, es, 16); }
 
 // Error text and device checks of km_capi.hip, for the entry points elsewhere.
 int ops_hip_error(hipError_t e, const char* what);
@@ -104,7 +124,7 @@ struct NormArgs {
     float* part;                // backward: blocks x 2 x d partial sums
     int32_t blocks;             // backward: rows of part (set by the launch)
 };
-int norm_bwd_max_blocks(int64_t n, int32_t d, int type);   // most rows of part that the backward pass writes
+int norm_bwd_max_blocks(int64_t n, int32_t d);   // most rows of part that the backward pass writes
 hipError_t launch_norm_fwd(NormArgs A, int type, hipStream_t s);
 hipError_t launch_norm_bwd(NormArgs A, int type, hipStream_t s);
 

@@ -199,7 +199,7 @@ int kmeans_norm_forward(const void* X, int64_t ldx, int64_t n, int32_t d, int32_
 
 size_t kmeans_norm_workspace_bytes(int64_t n, int32_t d, int32_t type) {
     if (!type_ok(type) || !rows_ok(n, d, d)) return 0;
-    const size_t b = (size_t)km::norm_bwd_max_blocks(n, d, type) * 2 * d * 4;
+    const size_t b = (size_t)km::norm_bwd_max_blocks(n, d) * 2 * d * 4;
     return (b + 255) / 256 * 256;
 }
 
