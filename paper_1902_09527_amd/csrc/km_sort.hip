@@ -11,11 +11,15 @@
 // read once and written to the places of its slots (gather, gradient of
 // combine), or its slots' rows are read and their weighted sum is written
 // (combine, gradient of gather).  They are bound by the memory's rate.
+#include <type_traits>
+
 #include "km_ops.h"
 
 namespace km {
 
 namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int key_of(int id, int k) { return (unsigned)id < (unsigned)k ? id : k; }
 
@@ -58,57 +62,69 @@ __global__ __launch_bounds__(kSortRankMax) void k_sort_rank(SortArgs A) {
 
 // One counting pass: the digit of an item is (key >> shift) & (2^bits - 1);
 // with a single pass the key itself.  idx: the items' order so far (null: the
-// slots' own).
+// slots' own).  A tile is kSortThreads RO items, a wave's items consecutive
+// (64 RO of them), RO a lane; all of a lane's keys are loaded at once.
 struct Pass {
     const int32_t* idx;
     int32_t* out;          // order after this pass
     uint32_t* hist;        // tiles x bins: counts, then their prefix over the tiles
     uint32_t* tot;         // bins: totals
-    int32_t bins, shift, mask, rounds, bits, last, single;
+    int32_t bins, shift, mask, bits, last, single;
     int64_t tiles;
 };
 
-__device__ __forceinline__ int digit_of(const SortArgs& A, const Pass& P, int item) {
-    return (key_of(A.ids[item], A.k) >> P.shift) & P.mask;
+// The items of a lane and their keys (item -1: past the end).
+template <int RO>
+__device__ __forceinline__ void load_items(const SortArgs& A, const Pass& P, int64_t tile, int32_t* item,
+                                           int32_t* key) {
+    const int64_t w0 = (tile * kSortWaves + (threadIdx.x >> 6)) * 64 * RO + (threadIdx.x & 63);
+#pragma unroll
+    for (int r = 0; r < RO; ++r) {
+        const int64_t i = w0 + r * 64;
+        item[r] = i < A.N ? (P.idx ? P.idx[i] : (int32_t)i) : -1;
+    }
+#pragma unroll
+    for (int r = 0; r < RO; ++r) key[r] = item[r] >= 0 ? key_of(A.ids[item[r]], A.k) : 0;
 }
 
+template <int RO>
 __global__ __launch_bounds__(kSortThreads) void k_sort_hist(SortArgs A, Pass P) {
     __shared__ uint32_t s_hist[kSortBins];
+    int32_t item[RO], key[RO];
+    load_items<RO>(A, P, blockIdx.x, item, key);
     for (int b = threadIdx.x; b < P.bins; b += kSortThreads) s_hist[b] = 0;
     __syncthreads();
-    const int64_t t0 = (int64_t)blockIdx.x * kSortThreads * P.rounds;
-    for (int r = 0; r < P.rounds; ++r) {
-        const int64_t i = t0 + (int64_t)r * kSortThreads + threadIdx.x;
-        if (i < A.N) atomicAdd(&s_hist[digit_of(A, P, P.idx ? P.idx[i] : (int)i)], 1u);   // counts: order is no matter
-    }
+#pragma unroll
+    for (int r = 0; r < RO; ++r)
+        if (item[r] >= 0) atomicAdd(&s_hist[(key[r] >> P.shift) & P.mask], 1u);   // counts: order is no matter
     __syncthreads();
     uint32_t* h = P.hist + (int64_t)blockIdx.x * P.bins;
     for (int b = threadIdx.x; b < P.bins; b += kSortThreads) h[b] = s_hist[b];
 }
 
-// Prefix sums over the tiles, 64 digit values a block: 16 waves take a run of
-// tiles each, lanes the digit values.
+// Prefix sums over the tiles, 16 digit values a block: its 64 groups of 16
+// lanes take a run of tiles each.
 __global__ __launch_bounds__(1024) void k_sort_scan(Pass P) {
-    __shared__ uint32_t s_sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int b = blockIdx.x * 64 + lane;
-    const int64_t per = (P.tiles + 15) / 16, t0 = wave * per, t1 = t0 + per < P.tiles ? t0 + per : P.tiles;
+    __shared__ uint32_t s_sum[64][16];
+    const int lane = threadIdx.x & 15, seg = threadIdx.x >> 4;
+    const int b = blockIdx.x * 16 + lane;
+    const int64_t per = (P.tiles + 63) / 64, t0 = seg * per, t1 = t0 + per < P.tiles ? t0 + per : P.tiles;
     uint32_t sum = 0;
     if (b < P.bins) {
 #pragma unroll 8
         for (int64_t t = t0; t < t1; ++t) sum += P.hist[t * P.bins + b];
     }
-    s_sum[wave][lane] = sum;
+    s_sum[seg][lane] = sum;
     __syncthreads();
+    if (b >= P.bins) return;
     uint32_t run = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        if (w == wave) run = all;
+#pragma unroll 16
+    for (int w = 0; w < 64; ++w) {
+        if (w == seg) run = all;
         all += s_sum[w][lane];
     }
-    if (b >= P.bins) return;
-    if (wave == 0) P.tot[b] = all;
-#pragma unroll 4
+    if (seg == 0) P.tot[b] = all;
+#pragma unroll 8
     for (int64_t t = t0; t < t1; ++t) {
         const uint32_t v = P.hist[t * P.bins + b];
         P.hist[t * P.bins + b] = run;
@@ -116,29 +132,37 @@ __global__ __launch_bounds__(1024) void k_sort_scan(Pass P) {
     }
 }
 
+// A tile writes a few places of every cluster, next to those of the tiles
+// beside it.  Blocks are dealt over 8 XCDs with an L2 each, so an XCD takes
+// consecutive tiles: their pieces of a line meet in one L2 instead of going to
+// memory one by one (2M slots, 1000 clusters: 50 us without, the pieces of 16
+// bytes written as whole lines).
+template <int RO>
 __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass P) {
     extern __shared__ uint32_t s_place[];   // waves x bins: next place of each digit value, per wave
     __shared__ uint32_t s_wave[kSortWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = P.bins;
-    for (int b = tid; b < kSortWaves * bins; b += kSortThreads) s_place[b] = 0;
-    __syncthreads();
-    // A wave's items are consecutive, 64 a round.
-    const int64_t w0 = ((int64_t)blockIdx.x * kSortWaves + wave) * 64 * P.rounds;
-    uint32_t* mine = s_place + wave * bins;
-    for (int r = 0; r < P.rounds; ++r) {
-        const int64_t i = w0 + r * 64 + lane;
-        if (i < A.N) atomicAdd(&mine[digit_of(A, P, P.idx ? P.idx[i] : (int)i)], 1u);
-    }
-    __syncthreads();
-    // Exclusive sums of the totals over the digit values, 4 values a thread.
+    const int64_t share = (P.tiles + 7) / 8, tile = blockIdx.x % 8 * share + blockIdx.x / 8;
+    if (tile >= P.tiles) return;   // the grid is 8 share blocks
+    // The tile's prefixes and the totals, 2 values a thread.
     constexpr int kPer = kSortBins / kSortThreads;
-    uint32_t v[kPer], own = 0;
+    uint32_t v[kPer], before[kPer], own = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const int b = tid * kPer + j;
         v[j] = b < bins ? P.tot[b] : 0;
+        before[j] = b < bins ? P.hist[tile * bins + b] : 0;
         own += v[j];
     }
+    int32_t item[RO], key[RO];
+    load_items<RO>(A, P, tile, item, key);
+    for (int b = tid; b < kSortWaves * bins; b += kSortThreads) s_place[b] = 0;
+    __syncthreads();
+    uint32_t* mine = s_place + wave * bins;
+#pragma unroll
+    for (int r = 0; r < RO; ++r)
+        if (item[r] >= 0) atomicAdd(&mine[(key[r] >> P.shift) & P.mask], 1u);
+    // Exclusive sums of the totals over the digit values.
     uint32_t inc = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -153,8 +177,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass 
     for (int j = 0; j < kPer; ++j) {
         const int b = tid * kPer + j;
         if (b < bins) {
-            if (P.single && blockIdx.x == 0) A.offsets[b] = (int32_t)base;   // bins = k + 1: one pass only
-            uint32_t at = base + P.hist[(int64_t)blockIdx.x * bins + b];
+            if (P.single && tile == 0) A.offsets[b] = (int32_t)base;   // bins = k + 1: one pass only
+            uint32_t at = base + before[j];
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
                 const uint32_t c = s_place[w * bins + b];
@@ -167,12 +191,10 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass 
     __syncthreads();
     // Places: lanes of a round with the same digit value take consecutive
     // ones in lane order; the lowest of them moves the counter.
-    for (int r = 0; r < P.rounds; ++r) {
-        const int64_t i = w0 + r * 64 + lane;
-        const bool in = i < A.N;
-        const int item = in ? (P.idx ? P.idx[i] : (int)i) : 0;
-        const int key = in ? key_of(A.ids[item], A.k) : 0;
-        const int dg = in ? (key >> P.shift) & P.mask : 0;
+#pragma unroll
+    for (int r = 0; r < RO; ++r) {
+        const bool in = item[r] >= 0;
+        const int dg = (key[r] >> P.shift) & P.mask;
         uint64_t same = __ballot(in);
         for (int b = 0; b < P.bits; ++b) {
             const bool bit = (dg >> b) & 1;
@@ -185,10 +207,10 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass 
         at = __shfl(at, in ? lead : 0);
         if (in) {
             at += (uint32_t)__popcll(same & ((1ull << lane) - 1));
-            P.out[at] = item;
+            P.out[at] = item[r];
             if (P.last) {
-                A.pos[item] = (int32_t)at;
-                A.sorted_ids[at] = key < A.k ? key : -1;
+                A.pos[item[r]] = (int32_t)at;
+                A.sorted_ids[at] = key[r] < A.k ? key[r] : -1;
             }
         }
     }
@@ -218,10 +240,9 @@ SortShape sort_shape(int64_t N, int32_t k) {
     while ((1 << (most + 1)) <= kSortBins) ++most;
     S.passes = k < kSortBins ? 1 : (kbits + most - 1) / most;
     S.bits = (kbits + S.passes - 1) / S.passes;
-    // Tiles of 2048 slots while they are few (more blocks), then longer ones
-    // (the histograms stay small beside the slots).
-    int64_t rounds = N / ((int64_t)kSortThreads * 512);
-    S.rounds = (int)(rounds < 4 ? 4 : rounds > 64 ? 64 : rounds);
+    // Short tiles while they are few (more blocks), then longer ones (the
+    // histograms stay small beside the slots).
+    S.rounds = N <= (1 << 18) ? 2 : N <= (1 << 20) ? 4 : N <= (1 << 22) ? 8 : 16;
     const int64_t tile = (int64_t)kSortThreads * S.rounds;
     S.tiles = (N + tile - 1) / tile;
     const int64_t bins = S.passes == 1 ? (int64_t)k + 1 : (int64_t)1 << S.bits;
@@ -253,13 +274,21 @@ hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hip
         P.shift = q * S.bits;
         P.mask = (1 << S.bits) - 1;
         P.bits = S.bits;
-        P.rounds = S.rounds;
         P.tiles = S.tiles;
         P.last = q == S.passes - 1;
-        hipLaunchKernelGGL(k_sort_hist, dim3((unsigned)S.tiles), dim3(kSortThreads), 0, s, A, P);
-        hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)((P.bins + 63) / 64)), dim3(1024), 0, s, P);
-        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)S.tiles), dim3(kSortThreads),
-                           (size_t)kSortWaves * P.bins * 4, s, A, P);
+        const dim3 g((unsigned)S.tiles), g8((unsigned)((S.tiles + 7) / 8 * 8)), t(kSortThreads);
+        const size_t lds = (size_t)kSortWaves * P.bins * 4;
+#define KM_SORT(K, G, LDS)                                                                 \
+    do {                                                                                 \
+        if (S.rounds == 2) hipLaunchKernelGGL((K<2>), G, t, LDS, s, A, P);               \
+        else if (S.rounds == 4) hipLaunchKernelGGL((K<4>), G, t, LDS, s, A, P);          \
+        else if (S.rounds == 8) hipLaunchKernelGGL((K<8>), G, t, LDS, s, A, P);          \
+        else hipLaunchKernelGGL((K<16>), G, t, LDS, s, A, P);                            \
+    } while (0)
+        KM_SORT(k_sort_hist, g, 0);
+        hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)((P.bins + 15) / 16)), dim3(1024), 0, s, P);
+        KM_SORT(k_sort_scatter, g8, lds);
+#undef KM_SORT
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         in = P.out;
@@ -279,162 +308,226 @@ namespace {
 
 constexpr int kMoveThreads = 256;
 
-template <class T, int V, int L>
-__global__ __launch_bounds__(kMoveThreads) void k_gather(MoveArgs A) {
-    using W = Vec<T, V>;
-    const int l = threadIdx.x % L, nv = A.d / V;
+// Rows of up to L vectors (CU = 1) go four at a time, wider ones in four
+// vectors a lane (CU = 4), so that four loads of a lane are in flight.
+template <class R, int L, int CU>
+__global__ __launch_bounds__(kMoveThreads) void k_gather(MoveArgs A, int nv, int64_t ld) {
+    constexpr int RU = 4 / CU;
+    const int l = threadIdx.x % L;
     const int32_t used = *A.used;
-    const int64_t step = (int64_t)gridDim.x * (kMoveThreads / L);
-    for (int64_t i = (int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L; i < A.n; i += step) {
-        const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.src) + i * A.ld);
-        const int32_t* __restrict__ pos = A.pos + i * A.m;
-        for (int c = l; c < nv; c += 4 * L) {
-            W v[4];
+    const R* __restrict__ src = static_cast<const R*>(A.src);
+    R* dst = static_cast<R*>(A.dst);
+    const int64_t step = (int64_t)gridDim.x * (kMoveThreads / L) * RU;
+    for (int64_t i0 = ((int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L) * RU; i0 < A.n; i0 += step) {
+        for (int c = l; c < nv; c += CU * L) {
+            R v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (c + u * L < nv) v[u] = x[c + u * L];
+            for (int u = 0; u < 4; ++u) {
+                const int64_t i = i0 + u / CU;
+                const int cc = c + u % CU * L;
+                if (i < A.n && cc < nv) v[u] = src[i * ld + cc];
+            }
             for (int j = 0; j < A.m; ++j) {
-                const int32_t p = pos[j];
-                W* y = reinterpret_cast<W*>(static_cast<T*>(A.dst) + (int64_t)p * A.d);
+                int32_t p[RU];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (c + u * L < nv) y[c + u * L] = p < used ? v[u] : W{};
+                for (int r = 0; r < RU; ++r) p[r] = i0 + r < A.n ? A.pos[(i0 + r) * A.m + j] : 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int cc = c + u % CU * L;
+                    if (i0 + u / CU < A.n && cc < nv)
+                        dst[(int64_t)p[u / CU] * nv + cc] = p[u / CU] < used ? v[u] : R{};
+                }
             }
         }
     }
 }
 
 // Y[i] = sum_j w[i,j] Z[pos[i,j]] over the slots in use, in float32, j ascending.
-template <class T, int V, int L>
+template <class T, int V, int L, int CU>
 __global__ __launch_bounds__(kMoveThreads) void k_combine(MoveArgs A) {
     using W = Vec<T, V>;
+    constexpr int RU = 4 / CU;
     const int l = threadIdx.x % L, nv = A.d / V;
     const int32_t used = *A.used;
-    const int64_t step = (int64_t)gridDim.x * (kMoveThreads / L);
-    for (int64_t i = (int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L; i < A.n; i += step) {
-        const int32_t* __restrict__ pos = A.pos + i * A.m;
-        W* y = reinterpret_cast<W*>(static_cast<T*>(A.dst) + i * A.d);
-        for (int c = l; c < nv; c += 4 * L) {
+    const int64_t step = (int64_t)gridDim.x * (kMoveThreads / L) * RU;
+    for (int64_t i0 = ((int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L) * RU; i0 < A.n; i0 += step) {
+        for (int c = l; c < nv; c += CU * L) {
             float acc[4][V] = {};
             for (int j = 0; j < A.m; ++j) {
-                const int32_t p = pos[j];
-                if (p >= used) continue;
-                const W* __restrict__ z = reinterpret_cast<const W*>(static_cast<const T*>(A.src) + (int64_t)p * A.ld);
-                const float w = A.w ? A.w[i * A.m + j] : 1.0f;
+                int32_t p[RU];
+                float w[RU];
+#pragma unroll
+                for (int r = 0; r < RU; ++r) {
+                    const bool in = i0 + r < A.n;
+                    p[r] = in ? A.pos[(i0 + r) * A.m + j] : used;
+                    w[r] = in && A.w ? A.w[(i0 + r) * A.m + j] : 1.0f;
+                }
                 W v[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (c + u * L < nv) v[u] = z[c + u * L];
+                for (int u = 0; u < 4; ++u) {
+                    const int cc = c + u % CU * L;
+                    if (p[u / CU] < used && cc < nv)
+                        v[u] = reinterpret_cast<const W*>(static_cast<const T*>(A.src) + (int64_t)p[u / CU] * A.ld)[cc];
+                }
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                    if (c + u * L < nv)
+                    if (p[u / CU] < used && c + u % CU * L < nv)
 #pragma unroll
-                        for (int e = 0; e < V; ++e) acc[u][e] = fmaf(w, to_f32(v[u].e[e]), acc[u][e]);
+                        for (int e = 0; e < V; ++e) acc[u][e] = fmaf(w[u / CU], to_f32(v[u].e[e]), acc[u][e]);
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (c + u * L < nv) {
+            for (int u = 0; u < 4; ++u) {
+                const int cc = c + u % CU * L;
+                if (i0 + u / CU < A.n && cc < nv) {
                     W o;
 #pragma unroll
                     for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(acc[u][e]);
-                    y[c + u * L] = o;
+                    reinterpret_cast<W*>(static_cast<T*>(A.dst) + (i0 + u / CU) * A.d)[cc] = o;
                 }
+            }
         }
     }
 }
 
 // dZ[pos] = w dY[i] (zero rows for empty slots), dw[i,j] = <dY[i], Z[pos]>.
-template <class T, int V, int L>
+// A group of lanes takes one slot's row at a time, RU slots with CU = 1.
+template <class T, int V, int L, int CU>
 __global__ __launch_bounds__(kMoveThreads) void k_combine_bwd(MoveArgs A) {
     using W = Vec<T, V>;
+    constexpr int RU = 4 / CU;
     const int l = threadIdx.x % L, nv = A.d / V;
     const int32_t used = *A.used;
-    const int64_t step = (int64_t)gridDim.x * (kMoveThreads / L);
-    for (int64_t i = (int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L; i < A.n; i += step) {
-        const W* __restrict__ g = reinterpret_cast<const W*>(static_cast<const T*>(A.src) + i * A.ld);
-        for (int j = 0; j < A.m; ++j) {   // dY[i] comes from cache after the first slot
-            const int64_t q = i * A.m + j;
-            const int32_t p = A.pos[q];
-            const bool in = p < used;
-            const float w = A.w ? A.w[q] : 1.0f;
-            const W* __restrict__ z = reinterpret_cast<const W*>(static_cast<const T*>(A.src2) + (int64_t)p * A.ld2);
-            W* dz = reinterpret_cast<W*>(static_cast<T*>(A.dst) + (int64_t)p * A.d);
-            float dot = 0.0f;
-            for (int c = l; c < nv; c += 4 * L) {
-                W a[4], b[4];
+    const int64_t slots = A.n * A.m, step = (int64_t)gridDim.x * (kMoveThreads / L) * RU;
+    for (int64_t q0 = ((int64_t)blockIdx.x * (kMoveThreads / L) + threadIdx.x / L) * RU; q0 < slots; q0 += step) {
+        int32_t p[RU];
+        int64_t i[RU];
+        float w[RU], dot[RU];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (c + u * L < nv && in) {
-                        a[u] = g[c + u * L];
-                        if (A.dw) b[u] = z[c + u * L];
-                    }
+        for (int r = 0; r < RU; ++r) {
+            const bool in = q0 + r < slots;
+            p[r] = in ? A.pos[q0 + r] : 0;
+            w[r] = in && A.w ? A.w[q0 + r] : 1.0f;
+            i[r] = A.m == 1 ? q0 + r : (q0 + r) / A.m;
+            dot[r] = 0.0f;
+        }
+        for (int c = l; c < nv; c += CU * L) {
+            W a[4], b[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (c + u * L < nv) {
-                        W o{};
-                        if (in)
-#pragma unroll
-                            for (int e = 0; e < V; ++e) {
-                                const float x = to_f32(a[u].e[e]);
-                                o.e[e] = from_f32<T>(w * x);
-                                if (A.dw) dot = fmaf(x, to_f32(b[u].e[e]), dot);
-                            }
-                        dz[c + u * L] = o;
-                    }
+            for (int u = 0; u < 4; ++u) {
+                const int r = u / CU, cc = c + u % CU * L;
+                if (q0 + r < slots && cc < nv && p[r] < used) {
+                    a[u] = reinterpret_cast<const W*>(static_cast<const T*>(A.src) + i[r] * A.ld)[cc];
+                    if (A.dw)
+                        b[u] = reinterpret_cast<const W*>(static_cast<const T*>(A.src2) + (int64_t)p[r] * A.ld2)[cc];
+                }
             }
-            if (A.dw) {
-                dot = group_sum<L>(dot);
-                if (l == 0) A.dw[q] = dot;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = u / CU, cc = c + u % CU * L;
+                if (q0 + r < slots && cc < nv) {
+                    W* dz = reinterpret_cast<W*>(static_cast<T*>(A.dst) + (int64_t)p[r] * A.d) + cc;
+                    if (p[r] < used) {
+                        W o;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const float x = to_f32(a[u].e[e]);
+                            o.e[e] = from_f32<T>(w[r] * x);
+                            if (A.dw) dot[r] = fmaf(x, to_f32(b[u].e[e]), dot[r]);
+                        }
+                        *dz = o;
+                    } else {
+                        *dz = W{};
+                    }
+                }
+            }
+        }
+        if (A.dw) {
+#pragma unroll
+            for (int r = 0; r < RU; ++r) {
+                const float sum = group_sum<L>(dot[r]);
+                if (l == 0 && q0 + r < slots) A.dw[q0 + r] = sum;
             }
         }
     }
 }
 
-enum Mover { kGather, kCombine, kCombineBwd };
+dim3 move_grid(int64_t rows, int per) {
+    const int64_t blocks = (rows + per - 1) / per;
+    return dim3((unsigned)(blocks > 65536 ? 65536 : blocks));
+}
 
-template <class T, int V, int L>
-hipError_t move_go(const MoveArgs& A, Mover mv, hipStream_t s) {
-    const int64_t per = kMoveThreads / L;
-    int64_t blocks = (A.n + per - 1) / per;
-    if (blocks > 65536) blocks = 65536;
-    const dim3 g((unsigned)blocks), b(kMoveThreads);
-    switch (mv) {
-        case kGather: hipLaunchKernelGGL((k_gather<T, V, L>), g, b, 0, s, A); break;
-        case kCombine: hipLaunchKernelGGL((k_combine<T, V, L>), g, b, 0, s, A); break;
-        default: hipLaunchKernelGGL((k_combine_bwd<T, V, L>), g, b, 0, s, A); break;
-    }
+// Lanes a row: the fewest that take it in one vector each, 64 for wider rows.
+template <class F>
+hipError_t by_lanes(int nv, F&& go) {
+    using std::integral_constant;
+    if (nv <= 4) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    else if (nv <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (nv <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (nv <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (nv <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     return hipGetLastError();
 }
 
-template <class T, int V>
-hipError_t move_lanes(const MoveArgs& A, Mover mv, hipStream_t s) {
-    const int nv = A.d / V;
-    if (nv <= 4) return move_go<T, V, 4>(A, mv, s);
-    if (nv <= 16) return move_go<T, V, 16>(A, mv, s);
-    return move_go<T, V, 64>(A, mv, s);
+// gather moves words of 16, 4 or 2 bytes, whatever they hold.
+template <class R>
+hipError_t gather_words(const MoveArgs& A, size_t es, hipStream_t s) {
+    const int nv = (int)(A.d * es / sizeof(R));
+    const int64_t ld = A.ld * (int64_t)es / (int64_t)sizeof(R);
+    return by_lanes(nv, [&](auto l, auto cu) {
+        constexpr int L = decltype(l)::value, CU = decltype(cu)::value;
+        hipLaunchKernelGGL((k_gather<R, L, CU>), move_grid(A.n, kMoveThreads / L * (4 / CU)), dim3(kMoveThreads), 0, s,
+                           A, nv, ld);
+    });
 }
 
-template <class T>
-hipError_t move_type(const MoveArgs& A, Mover mv, hipStream_t s) {
-    bool vec = rows_vec16(A.src, A.ld, A.d, sizeof(T)) && rows_vec16(A.dst, A.d, A.d, sizeof(T));
-    if (A.src2) vec = vec && rows_vec16(A.src2, A.ld2, A.d, sizeof(T));
-    if (vec) return move_lanes<T, 16 / (int)sizeof(T)>(A, mv, s);
-    return move_lanes<T, 1>(A, mv, s);
+template <class T, int V, bool BWD>
+hipError_t combine_lanes(const MoveArgs& A, hipStream_t s) {
+    return by_lanes(A.d / V, [&](auto l, auto cu) {
+        constexpr int L = decltype(l)::value, CU = decltype(cu)::value, per = kMoveThreads / L * (4 / CU);
+        if constexpr (BWD)
+            hipLaunchKernelGGL((k_combine_bwd<T, V, L, CU>), move_grid(A.n * A.m, per), dim3(kMoveThreads), 0, s, A);
+        else
+            hipLaunchKernelGGL((k_combine<T, V, L, CU>), move_grid(A.n, per), dim3(kMoveThreads), 0, s, A);
+    });
 }
 
-hipError_t move_any(const MoveArgs& A, Mover mv, int type, hipStream_t s) {
+// 16 bytes a lane where the rows allow it, else two elements, else one.
+template <class T, bool BWD>
+hipError_t combine_type(const MoveArgs& A, hipStream_t s) {
+    constexpr int E = (int)sizeof(T);
+    auto fits = [&](int bytes) {
+        return rows_vec(A.src, A.ld, A.d, E, bytes) && rows_vec(A.dst, A.d, A.d, E, bytes) &&
+               (!A.src2 || rows_vec(A.src2, A.ld2, A.d, E, bytes));
+    };
+    if (fits(16)) return combine_lanes<T, 16 / E, BWD>(A, s);
+    if (fits(2 * E)) return combine_lanes<T, 2, BWD>(A, s);
+    return combine_lanes<T, 1, BWD>(A, s);
+}
+
+template <bool BWD>
+hipError_t combine_any(const MoveArgs& A, int type, hipStream_t s) {
     if (A.n == 0) return hipSuccess;
-    if (type == kF32) return move_type<float>(A, mv, s);
-    if (type == kBF16) return move_type<__bf16>(A, mv, s);
-    return move_type<_Float16>(A, mv, s);
+    if (type == kF32) return combine_type<float, BWD>(A, s);
+    if (type == kBF16) return combine_type<__bf16, BWD>(A, s);
+    return combine_type<_Float16, BWD>(A, s);
 }
 
 }  // namespace
 
-hipError_t launch_sort_gather(const MoveArgs& A, int type, hipStream_t s) { return move_any(A, kGather, type, s); }
-hipError_t launch_sort_combine(const MoveArgs& A, int type, hipStream_t s) { return move_any(A, kCombine, type, s); }
+hipError_t launch_sort_gather(const MoveArgs& A, int type, hipStream_t s) {
+    if (A.n == 0) return hipSuccess;
+    const size_t es = row_type_bytes(type);
+    auto fits = [&](int bytes) {
+        return rows_vec(A.src, A.ld, A.d, es, bytes) && rows_vec(A.dst, A.d, A.d, es, bytes);
+    };
+    if (fits(16)) return gather_words<u32x4>(A, es, s);
+    if (fits(4)) return gather_words<uint32_t>(A, es, s);
+    return gather_words<uint16_t>(A, es, s);
+}
+hipError_t launch_sort_combine(const MoveArgs& A, int type, hipStream_t s) { return combine_any<false>(A, type, s); }
 hipError_t launch_sort_combine_bwd(const MoveArgs& A, int type, hipStream_t s) {
-    return move_any(A, kCombineBwd, type, s);
+    return combine_any<true>(A, type, s);
 }
 
 }  // namespace km
