@@ -212,25 +212,33 @@ __device__ __forceinline__ int swz_tr(int k, int c) {
 }
 
 // Operand of 16 columns c0 .. along rows k0 + 0 .. KS of a tile whose rows
-// are the contraction (CPR chunks a row).
+// are the contraction (CPR chunks a row).  k0 and, for 16 bits, c0 move the
+// address by whole rows and chunk pairs only, so `at` (tr_lane) is a lane's
+// place for k0 = 0 and this c0.
 template <class T, int CPR>
-__device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int c0, int lane) {
+__device__ __forceinline__ int tr_lane(int c0, int lane) {
+    const int li = lane & 15, g = lane >> 4;
     if constexpr (sizeof(T) == 2) {
-        const int li = lane & 15, k = k0 + (lane >> 4) * 8 + (li >> 2), ch = c0 / 8 + ((li & 3) >> 1);
+        const int k = g * 8 + (li >> 2), ch = c0 / 8 + ((li & 3) >> 1);
+        return (k * CPR + swz_tr<T, CPR>(k, ch)) * 16 + (li & 1) * 8;
+    } else {
+        const int k = g * 4, c = c0 + li;
+        return (k * CPR + swz_tr<T, CPR>(k, c / 4)) * 16 + (c & 3) * 4;
+    }
+}
+template <class T, int CPR>
+__device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int at) {
+    if constexpr (sizeof(T) == 2) {
         s16x4 v[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (KM_LDS s16x4*)(tile + ((k + 4 * t) * CPR + swz_tr<T, CPR>(k + 4 * t, ch)) * 16 + (li & 1) * 8));
+            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KM_LDS s16x4*)(tile + at + (k0 + 4 * t) * CPR * 16));
         struct Two { s16x4 a, b; } w{v[0], v[1]};
         return __builtin_bit_cast(u32x4, w);
     } else {
-        const int c = c0 + (lane & 15), k = k0 + (lane >> 4) * 4;
         u32x4 v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = *reinterpret_cast<const uint32_t*>(tile + ((k + j) * CPR + swz_tr<T, CPR>(k + j, c / 4)) * 16 +
-                                                      (c & 3) * 4);
+        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(tile + at + (k0 + j) * CPR * 16);
         return v;
     }
 }
@@ -242,8 +250,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
     constexpr int kStage = (TM + TN) * 128;
     extern __shared__ __align__(16) char s_tiles[];   // two stages: TM rows of U, then TN rows (TR: BK rows) of W
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, li = lane & 15;
-    const int wr = wave / WC, wc = wave % WC;
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
 
     // Consecutive tiles go to one XCD (blocks are dealt over 8), down 4 tiles
     // of places before the next columns.
@@ -255,52 +263,75 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     const int64_t in_grp = t - grp * 4 * A.tn;
     const int64_t bm = (m0 + in_grp % gm) * TM, bn = in_grp / gm * TN;
 
+    // Where a thread's chunks of a stage come from: pointers that move on with
+    // the stages (AL), the place in the stage being fixed.
     const T* up[NU];
+    const T* wp[NW];
+    const int uc = swz(tid / 8, tid % 8) * E;   // NT / 8 rows further on the swizzle is the same
+    static_assert(NT % 128 == 0, "");
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         int64_t place = bm + (i * NT + tid) / 8;
         if (place >= A.n) place = A.n - 1;   // not stored
-        up[i] = static_cast<const T*>(A.U) + row_of(A.order, place) * A.ldu;
+        up[i] = static_cast<const T*>(A.U) + row_of(A.order, place) * A.ldu + uc;
+    }
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        const int q = i * NT + tid;
+        if constexpr (TR) {
+            const int kk = q / CPR;
+            wp[i] = static_cast<const T*>(A.W) + (int64_t)kk * A.P + bn + swz_tr<T, CPR>(kk, q % CPR) * E;
+        } else {
+            int64_t col = bn + q / 8;
+            if (col >= A.P) col = A.P - 1;   // not stored
+            wp[i] = static_cast<const T*>(A.W) + col * A.K + uc;
+        }
     }
     const int nk = (A.K + BK - 1) / BK;
+    // Stages without a chunk past the contraction's end or the last column.
+    const int whole = !TR || bn + TN <= A.P ? A.K / BK : 0;
 
-    auto load = [&](int kt, char* buf) {
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int q = i * NT + tid, row = q / 8;
-            const int64_t k0 = (int64_t)kt * BK + swz(row, q % 8) * E;
-            if constexpr (AL)
-                load_lds16(k0 < A.K ? (const void*)(up[i] + k0) : (const void*)ad_zero, buf + (i * NT + wave * 64) * 16);
-            else
-                *reinterpret_cast<u32x4*>(buf + q * 16) = chunk_guarded(up[i], k0, A.K);
-        }
-        char* wb = buf + TM * 128;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            const int q = i * NT + tid;
-            if constexpr (TR) {
-                const int kk = q / CPR;
-                const int64_t k = (int64_t)kt * BK + kk, col = bn + swz_tr<T, CPR>(kk, q % CPR) * E;
-                const T* src = static_cast<const T*>(A.W) + k * A.P;
-                if constexpr (AL)
-                    load_lds16(k < A.K && col < A.P ? (const void*)(src + col) : (const void*)ad_zero,
-                               wb + (i * NT + wave * 64) * 16);
-                else
-                    *reinterpret_cast<u32x4*>(wb + q * 16) =
-                        k < A.K ? chunk_guarded(src, col, A.P) : zero_chunk<T>();
+    // Chunk i of stage kt (of NU + NW a thread) to LDS; guard: it may lie past an end.
+    auto load = [&](int i, int kt, char* buf, bool guard) {
+        if (i < NU) {
+            if constexpr (AL) {
+                const void* src = !guard || kt * BK + uc < A.K ? (const void*)up[i] : (const void*)ad_zero;
+                load_lds16(src, buf + (i * NT + wave * 64) * 16);
+                up[i] += BK;
             } else {
-                const int row = q / 8;
-                int64_t col = bn + row;
-                if (col >= A.P) col = A.P - 1;   // not stored
-                const int64_t k0 = (int64_t)kt * BK + swz(row, q % 8) * E;
-                const T* src = static_cast<const T*>(A.W) + col * A.K;
-                if constexpr (AL)
-                    load_lds16(k0 < A.K ? (const void*)(src + k0) : (const void*)ad_zero,
-                               wb + (i * NT + wave * 64) * 16);
-                else
-                    *reinterpret_cast<u32x4*>(wb + q * 16) = chunk_guarded(src, k0, A.K);
+                *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) =
+                    chunk_guarded(up[i] - uc, (int64_t)kt * BK + uc, A.K);
+            }
+            return;
+        }
+        i -= NU;
+        const int q = i * NT + tid;
+        char* wb = buf + TM * 128;
+        if constexpr (TR) {
+            const int kk = q / CPR;
+            const int64_t col = bn + swz_tr<T, CPR>(kk, q % CPR) * E;
+            if constexpr (AL) {
+                const bool in = !guard || (kt * BK + kk < A.K && col < A.P);
+                load_lds16(in ? (const void*)wp[i] : (const void*)ad_zero, wb + (i * NT + wave * 64) * 16);
+                wp[i] += (int64_t)BK * A.P;
+            } else {
+                const int64_t k = (int64_t)kt * BK + kk;
+                *reinterpret_cast<u32x4*>(wb + q * 16) =
+                    k < A.K ? chunk_guarded(static_cast<const T*>(A.W) + k * A.P, col, A.P) : zero_chunk<T>();
+            }
+        } else {
+            if constexpr (AL) {
+                const void* src = !guard || kt * BK + uc < A.K ? (const void*)wp[i] : (const void*)ad_zero;
+                load_lds16(src, wb + (i * NT + wave * 64) * 16);
+                wp[i] += BK;
+            } else {
+                *reinterpret_cast<u32x4*>(wb + q * 16) = chunk_guarded(wp[i] - uc, (int64_t)kt * BK + uc, A.K);
             }
         }
+    };
+    auto load_all = [&](int kt, char* buf) {
+#pragma unroll
+        for (int i = 0; i < NU + NW; ++i) load(i, kt, buf, kt >= whole);
     };
 
     f32x4 acc[FR][FC];
@@ -309,36 +340,84 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
 #pragma unroll
         for (int h = 0; h < FC; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
 
-    load(0, s_tiles);
-    for (int kt = 0; kt < nk; ++kt) {
-        // The stage's loads have landed, and every wave is done with the other buffer.
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        const char* ub = s_tiles + (kt & 1) * kStage;
-        const char* wb = ub + TM * 128;
-        if (kt + 1 < nk) load(kt + 1, s_tiles + ((kt + 1) & 1) * kStage);
+    // A lane's places in a stage; the second half of a row is 64 bytes off
+    // (one bit of the swizzled chunk), 16 rows are 2048 bytes.
+    const int ua = (wr * (TM / WR) + li) * 128 + swz(li, g) * 16;
+    int wa[TR ? FC : 1];
+    if constexpr (TR) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            u32x4 b[FR], a[FC];
-#pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                const int row = wr * (TM / WR) + f * 16 + li;
-                b[f] = *reinterpret_cast<const u32x4*>(ub + row * 128 + swz(row, s * 4 + g) * 16);
-            }
-#pragma unroll
-            for (int h = 0; h < FC; ++h) {
-                const int c0 = wc * (TN / WC) + h * 16;
-                if constexpr (TR)
-                    a[h] = read_tr<T, CPR>(wb, s * KS, c0, lane);
-                else
-                    a[h] = *reinterpret_cast<const u32x4*>(wb + (c0 + li) * 128 + swz(c0 + li, s * 4 + g) * 16);
-            }
-#pragma unroll
-            for (int f = 0; f < FR; ++f)
-#pragma unroll
-                for (int h = 0; h < FC; ++h) acc[f][h] = Mma<T>::mma(a[h], b[f], acc[f][h]);
-        }
+        for (int h = 0; h < FC; ++h) wa[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
+    } else {
+        wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, g) * 16;
     }
+    struct Frags {
+        u32x4 b[FR], a[FC];
+    };
+    // Operand i of half s of a stage: first the columns', then the rows'.
+    auto read = [&](Frags& F, int i, const char* buf, int s) {
+        if (i < FC) {
+            if constexpr (TR)
+                F.a[i] = read_tr<T, CPR>(buf, s * KS, wa[i]);
+            else
+                F.a[i] = *reinterpret_cast<const u32x4*>(buf + (wa[0] ^ (s * 64)) + i * 2048);
+        } else {
+            F.b[i - FC] = *reinterpret_cast<const u32x4*>(buf + (ua ^ (s * 64)) + (i - FC) * 2048);
+        }
+    };
+
+    // Operands are read from LDS half a stage ahead of their products, and a
+    // stage is loaded while the one before it is multiplied.  The barrier of a
+    // stage stands between its two halves of products, when the second half's
+    // operands are in registers, and loads, reads and products are issued in
+    // turns (kParts of each), so that the matrix cores do not wait for either.
+    constexpr int kParts = FR < 4 ? FR : 4;
+    constexpr int kLoads = (NU + NW) / kParts, kReads = (FR + FC) / kParts;
+    static_assert((NU + NW) % kParts == 0 && (FR + FC) % kParts == 0 && FR % kParts == 0, "");
+    // The products of F; F2 read from buf2 (half s2); kl >= 0: stage kl loaded into bufl.
+    auto half = [&](const Frags& F, Frags& F2, const char* buf2, int s2, int kl, char* bufl, bool guard) {
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) {
+            if (kl >= 0) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) load(q * kLoads + i, kl, bufl, guard);
+            }
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) read(F2, q * kReads + i, buf2, s2);
+#pragma unroll
+            for (int f = q * (FR / kParts); f < (q + 1) * (FR / kParts); ++f)
+#pragma unroll
+                for (int h = 0; h < FC; ++h) acc[f][h] = Mma<T>::mma(F.a[h], F.b[f], acc[f][h]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // This wave's operands have arrived (F2 of the half before).
+    auto arrived = [&]() { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
+    // Every wave's reads of one stage and its loads of the next have ended.
+    auto turn = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+        __syncthreads();
+    };
+
+    Frags F0, F1;
+    load_all(0, s_tiles);
+    turn();
+    if (nk > 1) load_all(1, s_tiles + kStage);
+#pragma unroll
+    for (int i = 0; i < FR + FC; ++i) read(F0, i, s_tiles, 0);
+    auto stage = [&](int kt, bool last) {
+        char* cur = s_tiles + (kt & 1) * kStage;
+        const char* nxt = s_tiles + ((kt + 1) & 1) * kStage;
+        arrived();
+        __builtin_amdgcn_sched_barrier(0);
+        half(F0, F1, cur, 1, -1, cur, false);
+        turn();
+        __builtin_amdgcn_sched_barrier(0);
+        // After the last stage the reads are of what the buffer held before, and are not used.
+        half(F1, F0, nxt, 0, !last ? kt + 2 : kt + 2 < nk ? kt + 2 : -1, cur, last);
+    };
+    int kt = 0;
+    for (; kt + 2 < whole; ++kt) stage(kt, false);
+    for (; kt < nk; ++kt) stage(kt, true);
 
     // The adapters' term, cluster by cluster of the wave's places: a lane
     // keeps the sum only where its place is of the cluster, so that nothing of
@@ -615,9 +694,9 @@ __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
             for (int s = 0; s < 2; ++s) {
                 u32x4 a[2], b[RF];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) a[h] = read_tr<T, CPR>(s_u[buf], s * KS, wave * 32 + h * 16, lane);
+                for (int h = 0; h < 2; ++h) a[h] = read_tr<T, CPR>(s_u[buf], s * KS, tr_lane<T, CPR>(wave * 32 + h * 16, lane));
 #pragma unroll
-                for (int j = 0; j < RF; ++j) b[j] = read_tr<T, VPR>(s_v[buf], s * KS, j * 16, lane);
+                for (int j = 0; j < RF; ++j) b[j] = read_tr<T, VPR>(s_v[buf], s * KS, tr_lane<T, VPR>(j * 16, lane));
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
