@@ -15,6 +15,8 @@
 //
 // Sums are float32 (matrix-core accumulators); h and g are rounded to the
 // rows' type, once, as the matrix cores' operands.
+#include <type_traits>
+
 #include "km_ops.h"
 
 namespace km {
@@ -66,25 +68,33 @@ struct Mma<float> {
     }
 };
 
-template <class T>
-__device__ __forceinline__ u32x4 zero_chunk() {
-    return u32x4{0, 0, 0, 0};
-}
-
-// Elements p[0 .. E) at positions k0 .. of a row of K elements, zero past its end.
+// Elements at positions k0 .. k0 + E of a row of K >= 1 elements, `stride`
+// apart, zero past its end.  Without branches, so that a lane's loads are in
+// flight together: past the end the row's first elements are read.
 template <class T>
 __device__ __forceinline__ u32x4 chunk_guarded(const T* row, int64_t k0, int64_t K, int64_t stride = 1) {
     constexpr int E = Mma<T>::E;
-    Vec<T, E> v{};
+    Vec<T, E> v;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (k0 + e < K) v.e[e] = row[(k0 + e) * stride];
+    for (int e = 0; e < E; ++e) v.e[e] = row[(k0 + e < K ? k0 + e : 0) * stride];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v.e[e] = k0 + e < K ? v.e[e] : (T)0.0f;
     return __builtin_bit_cast(u32x4, v);
+}
+__device__ __forceinline__ u32x4 only_if(bool in, u32x4 v) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = in ? v[i] : 0u;
+    return o;
+}
+// The same for rows that can be read 16 bytes at a time (K a multiple of E).
+template <class T>
+__device__ __forceinline__ u32x4 chunk_aligned(const T* row, int64_t k0, int64_t K) {
+    return only_if(k0 < K, *reinterpret_cast<const u32x4*>(row + (k0 < K ? k0 : 0)));
 }
 template <class T>
 __device__ __forceinline__ u32x4 chunk(const T* row, int64_t k0, int64_t K, bool aligned) {
-    if (!aligned) return chunk_guarded(row, k0, K);
-    return k0 < K ? *reinterpret_cast<const u32x4*>(row + k0) : zero_chunk<T>();
+    return aligned ? chunk_aligned(row, k0, K) : chunk_guarded(row, k0, K);   // `aligned` is uniform
 }
 
 // Four consecutive results, col0 .. of a row of P.
@@ -109,6 +119,103 @@ __device__ __forceinline__ void load_lds16(const void* src, char* wave_base) {
 
 __device__ __forceinline__ int64_t row_of(const int32_t* order, int64_t place) { return order ? order[place] : place; }
 
+// Chunk position of a stage's rows in LDS: rows are 128 bytes, so 16 rows read
+// at one chunk index fall on all 64 banks once.
+__device__ __forceinline__ int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
+
+// The same for tiles that hold the contraction along their rows (TR): 16-bit
+// tiles are read 4 rows x 16 columns at a time, float32 by columns.
+template <class T, int CPR>
+__device__ __forceinline__ int swz_tr(int k, int c) {
+    const int m = sizeof(T) == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2;
+    return c ^ (m & (CPR - 1));
+}
+
+// Operand of 16 columns c0 .. along rows k0 + 0 .. KS of a tile whose rows
+// are the contraction (CPR chunks a row).  k0 and, for 16 bits, c0 move the
+// address by whole rows and chunk pairs only, so `at` (tr_lane) is a lane's
+// place for k0 = 0 and this c0.
+template <class T, int CPR>
+__device__ __forceinline__ int tr_lane(int c0, int lane) {
+    const int li = lane & 15, g = lane >> 4;
+    if constexpr (sizeof(T) == 2) {
+        const int k = g * 8 + (li >> 2), ch = c0 / 8 + ((li & 3) >> 1);
+        return (k * CPR + swz_tr<T, CPR>(k, ch)) * 16 + (li & 1) * 8;
+    } else {
+        const int k = g * 4, c = c0 + li;
+        return (k * CPR + swz_tr<T, CPR>(k, c / 4)) * 16 + (c & 3) * 4;
+    }
+}
+template <class T, int CPR>
+__device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int at) {
+    if constexpr (sizeof(T) == 2) {
+        s16x4 v[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KM_LDS s16x4*)(tile + at + (k0 + 4 * t) * CPR * 16));
+        struct Two { s16x4 a, b; } w{v[0], v[1]};
+        return __builtin_bit_cast(u32x4, w);
+    } else {
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(tile + at + (k0 + j) * CPR * 16);
+        return v;
+    }
+}
+
+// --------------------------------------------------------------------------
+// Chunks of clusters, for the adapters' gradients.
+
+struct Item {
+    int32_t c, p0, p1, slot;   // places p0 .. p1 of cluster c; slot: partial sum to write, -1: the result itself
+};
+
+// Chunks of every cluster, in order.
+struct ListArgs {
+    const int32_t* offsets;
+    int32_t k, chunk;
+    int32_t* count;      // items
+    Item* items;
+    int32_t *first, *num;   // per cluster: first partial slot, chunks (0: empty)
+};
+
+// By a block of 256 threads; s: 8 words of LDS.
+__device__ __forceinline__ void list_chunks(const ListArgs& A, int* s) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int items = 0, slots = 0;   // so far
+    for (int c0 = 0; c0 < A.k; c0 += 256) {
+        const int c = c0 + tid;
+        const int a = c < A.k ? A.offsets[c] : 0, b = c < A.k ? A.offsets[c + 1] : 0;
+        const int ni = (b - a + A.chunk - 1) / A.chunk, ns = ni > 1 ? ni : 0;
+        int xi = ni, xs = ns;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int ui = __shfl_up(xi, o), us = __shfl_up(xs, o);
+            if (lane >= o) xi += ui, xs += us;
+        }
+        if (lane == 63) s[wave] = xi, s[4 + wave] = xs;
+        __syncthreads();
+        int bi = items, bs = slots;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) bi += s[w], bs += s[4 + w];
+            items += s[w];
+            slots += s[4 + w];
+        }
+        bi += xi - ni;
+        bs += xs - ns;
+        if (c < A.k) {
+            A.first[c] = bs;
+            A.num[c] = ni;
+            for (int q = 0; q < ni; ++q) {
+                const int p = a + q * A.chunk;
+                A.items[bi + q] = Item{c, p, b - p < A.chunk ? b : p + A.chunk, ni > 1 ? bs + q : -1};
+            }
+        }
+        __syncthreads();
+    }
+    if (tid == 0) A.count[0] = items;
+}
+
 // --------------------------------------------------------------------------
 // Inner products: S[place] = s_c Q_c u (rounded to T, rp wide, zero past r)
 // and, if H is not null, H[row] = Q_c u.  16 places a block; its four waves
@@ -125,10 +232,17 @@ struct InnerArgs {
     int32_t K, r, rp, u16, q16, h4;   // u16 / q16: rows of U / Q can be read 16 bytes at a time; h4: H written by fours
 };
 
-template <class T, int RF, bool TR>
-__global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A) {
-    constexpr int E = Mma<T>::E, KS = 4 * E;
+template <class T, int RF, bool TR, bool AL>
+__global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, VPR = RF * 16 / E;
+    constexpr int UN = RF <= 2 ? 4 : RF == 4 ? 2 : 1;   // steps of a wave in flight
+    constexpr int NQ = (KS * VPR + 63) / 64;            // chunks a lane of one step's K x r operand
     __shared__ f32x4 s_red[4][RF][64];
+    __shared__ __align__(16) char s_q[TR ? 4 : 1][TR ? UN * KS * VPR * 16 : 16];
+    if (TR && blockIdx.x == gridDim.x - 1) {   // one more block: the chunks of the adapters' gradients
+        list_chunks(L, reinterpret_cast<int*>(s_q));
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
     const int64_t p0 = (int64_t)blockIdx.x * 16;
     const int64_t place = p0 + li;
@@ -143,16 +257,57 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A) {
 #pragma unroll
         for (int j = 0; j < RF; ++j) acc[j] = f32x4{0, 0, 0, 0};
         const T* q = static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.K;
-        for (int s = wave; s < steps; s += 4) {
-            const int64_t k0 = (int64_t)s * KS + g * E;
-            const u32x4 b = chunk(u, k0, A.K, A.u16);
+        for (int s = wave * UN; s < steps; s += 4 * UN) {   // steps past the last are of zeros
+            u32x4 b[UN];
 #pragma unroll
-            for (int j = 0; j < RF; ++j) {
-                const int rr = j * 16 + li;
-                u32x4 a = zero_chunk<T>();
-                if (rr < A.r)
-                    a = TR ? chunk_guarded(q + rr, k0, A.K, A.r) : chunk(q + (int64_t)rr * A.K, k0, A.K, A.q16);
-                acc[j] = Mma<T>::mma(a, b, acc[j]);
+            for (int x = 0; x < UN; ++x) {
+                const int64_t k0 = (int64_t)(s + x) * KS + g * E;
+                b[x] = AL ? chunk_aligned(u, k0, A.K) : chunk_guarded(u, k0, A.K);
+            }
+            if constexpr (TR) {
+                u32x4 v[UN][NQ];
+#pragma unroll
+                for (int x = 0; x < UN; ++x)
+#pragma unroll
+                    for (int y = 0; y < NQ; ++y) {
+                        const int z = y * 64 + lane, kk = z / VPR;
+                        const int64_t k = (int64_t)(s + x) * KS + kk;
+                        const T* src = q + (k < A.K ? k : 0) * A.r;
+                        v[x][y] = only_if(k < A.K, AL && A.q16 ? chunk_aligned(src, z % VPR * E, A.r)
+                                                               : chunk_guarded(src, z % VPR * E, A.r));
+                    }
+#pragma unroll
+                for (int x = 0; x < UN; ++x)
+#pragma unroll
+                    for (int y = 0; y < NQ; ++y) {
+                        const int z = y * 64 + lane, kk = z / VPR;
+                        if (kk < KS)
+                            *reinterpret_cast<u32x4*>(s_q[wave] + ((x * KS + kk) * VPR + swz_tr<T, VPR>(kk, z % VPR)) * 16) =
+                                v[x][y];
+                    }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the wave's own part of LDS
+#pragma unroll
+                for (int x = 0; x < UN; ++x)
+#pragma unroll
+                    for (int j = 0; j < RF; ++j)
+                        acc[j] = Mma<T>::mma(read_tr<T, VPR>(s_q[wave], x * KS, tr_lane<T, VPR>(j * 16, lane)), b[x],
+                                             acc[j]);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            } else {
+                u32x4 a[UN][RF];
+#pragma unroll
+                for (int x = 0; x < UN; ++x)
+#pragma unroll
+                    for (int j = 0; j < RF; ++j) {
+                        const int rr = j * 16 + li;   // rows past r give results that are not kept
+                        const T* src = q + (int64_t)(rr < A.r ? rr : 0) * A.K;
+                        const int64_t k0 = (int64_t)(s + x) * KS + g * E;
+                        a[x][j] = AL ? chunk_aligned(src, k0, A.K) : chunk_guarded(src, k0, A.K);
+                    }
+#pragma unroll
+                for (int x = 0; x < UN; ++x)
+#pragma unroll
+                    for (int j = 0; j < RF; ++j) acc[j] = Mma<T>::mma(a[x][j], b[x], acc[j]);
             }
         }
 #pragma unroll
@@ -198,50 +353,6 @@ struct MainArgs {
     int32_t K, P, r, rp, q16, y4;
     int32_t tm, tn;   // tiles
 };
-
-// Chunk position of a stage's rows in LDS: rows are 128 bytes, so 16 rows read
-// at one chunk index fall on all 64 banks once.
-__device__ __forceinline__ int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
-
-// The same for tiles that hold the contraction along their rows (TR): 16-bit
-// tiles are read 4 rows x 16 columns at a time, float32 by columns.
-template <class T, int CPR>
-__device__ __forceinline__ int swz_tr(int k, int c) {
-    const int m = sizeof(T) == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2;
-    return c ^ (m & (CPR - 1));
-}
-
-// Operand of 16 columns c0 .. along rows k0 + 0 .. KS of a tile whose rows
-// are the contraction (CPR chunks a row).  k0 and, for 16 bits, c0 move the
-// address by whole rows and chunk pairs only, so `at` (tr_lane) is a lane's
-// place for k0 = 0 and this c0.
-template <class T, int CPR>
-__device__ __forceinline__ int tr_lane(int c0, int lane) {
-    const int li = lane & 15, g = lane >> 4;
-    if constexpr (sizeof(T) == 2) {
-        const int k = g * 8 + (li >> 2), ch = c0 / 8 + ((li & 3) >> 1);
-        return (k * CPR + swz_tr<T, CPR>(k, ch)) * 16 + (li & 1) * 8;
-    } else {
-        const int k = g * 4, c = c0 + li;
-        return (k * CPR + swz_tr<T, CPR>(k, c / 4)) * 16 + (c & 3) * 4;
-    }
-}
-template <class T, int CPR>
-__device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int at) {
-    if constexpr (sizeof(T) == 2) {
-        s16x4 v[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KM_LDS s16x4*)(tile + at + (k0 + 4 * t) * CPR * 16));
-        struct Two { s16x4 a, b; } w{v[0], v[1]};
-        return __builtin_bit_cast(u32x4, w);
-    } else {
-        u32x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(tile + at + (k0 + j) * CPR * 16);
-        return v;
-    }
-}
 
 template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
 __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
@@ -316,8 +427,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
                 wp[i] += (int64_t)BK * A.P;
             } else {
                 const int64_t k = (int64_t)kt * BK + kk;
-                *reinterpret_cast<u32x4*>(wb + q * 16) =
-                    k < A.K ? chunk_guarded(static_cast<const T*>(A.W) + k * A.P, col, A.P) : zero_chunk<T>();
+                *reinterpret_cast<u32x4*>(wb + q * 16) = only_if(
+                    k < A.K, chunk_guarded(static_cast<const T*>(A.W) + (k < A.K ? k : 0) * A.P, col, A.P));
             }
         } else {
             if constexpr (AL) {
@@ -419,45 +530,68 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     for (; kt + 2 < whole; ++kt) stage(kt, false);
     for (; kt < nk; ++kt) stage(kt, true);
 
-    // The adapters' term, cluster by cluster of the wave's places: a lane
-    // keeps the sum only where its place is of the cluster, so that nothing of
-    // one cluster's adapter reaches another's rows.
-    const int64_t w0 = bm + wr * (TM / WR), w1 = w0 + TM / WR < A.n ? w0 + TM / WR : A.n;
-    const int64_t cb = bn + wc * (TN / WC);
-    int c = w0 < w1 ? __builtin_amdgcn_readfirstlane(A.sids[w0]) : -1;
-    while (c >= 0) {
-        const int64_t c0 = A.offsets[c], c1 = A.offsets[c + 1];
-        for (int k0 = 0; k0 < A.rp; k0 += KS) {
-            u32x4 a[FC];
+    // The adapters' term, cluster by cluster of the wave's places (they are in
+    // cluster order): a lane keeps the sum only where its place is of the
+    // cluster, so that nothing of one cluster's adapter reaches another's rows.
+    // The next cluster's operand is loaded during the products of one.
+    const int64_t w0 = bm + wr * (TM / WR), cb = bn + wc * (TN / WC);
+    int mine[FR];
 #pragma unroll
-            for (int h = 0; h < FC; ++h) {
-                const int64_t col = cb + h * 16 + li;
-                const int rr = k0 + g * E;
-                a[h] = zero_chunk<T>();
-                if (col < A.P) {
-                    if constexpr (TR)
-                        a[h] = chunk_guarded(static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.P + col, rr, A.r, A.P);
-                    else
-                        a[h] = chunk(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r, rr, A.r, A.q16);
-                }
-            }
+    for (int f = 0; f < FR; ++f) {
+        const int64_t place = w0 + f * 16 + li;
+        const int id = A.sids[place < A.n ? place : A.n - 1];
+        mine[f] = place < A.n ? id : -1;
+    }
+    auto after = [&](int c) {   // the lowest cluster above c of the wave's places, -1: none
+        int next = -1;
+#pragma unroll
+        for (int f = FR - 1; f >= 0; --f) {
+            const uint64_t m = __ballot(mine[f] > c);
+            if (m) next = __builtin_amdgcn_readlane(mine[f], __builtin_ctzll(m));
+        }
+        return next;
+    };
+    auto adapter = [&](u32x4* a, int c, int k0) {
+#pragma unroll
+        for (int h = 0; h < FC; ++h) {
+            const int64_t col = cb + h * 16 + li, cc = col < A.P ? col : 0;   // columns past P are not stored
+            if constexpr (TR)
+                a[h] = chunk_guarded(static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.P + cc, k0 + g * E, A.r, A.P);
+            else
+                a[h] = chunk(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + cc) * A.r, k0 + g * E, A.r, A.q16);
+        }
+    };
+    const int c_first = after(-1);
+    if (c_first >= 0) {
+        for (int k0 = 0; k0 < A.rp; k0 += KS) {
+            u32x4 b[FR], a[FC];
+            adapter(a, c_first, k0);
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
-                const int64_t f0 = w0 + f * 16, place = f0 + li;
-                if (f0 >= c1 || f0 + 16 <= c0) continue;
-                const bool is = place >= c0 && place < c1;
-                const u32x4 b = is ? *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) + place * A.rp + k0 +
-                                                                     g * E)
-                                   : zero_chunk<T>();
+                const int64_t place = w0 + f * 16 + li;
+                b[f] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) +
+                                                       (place < A.n ? place : A.n - 1) * A.rp + k0 + g * E);
+            }
+            for (int c = c_first; c >= 0;) {
+                const int next = after(c);
+                u32x4 an[FC];
+                adapter(an, next < 0 ? c : next, k0);
 #pragma unroll
-                for (int h = 0; h < FC; ++h) {
-                    const f32x4 d = Mma<T>::mma(a[h], b, acc[f][h]);
+                for (int f = 0; f < FR; ++f) {
+                    const bool is = mine[f] == c;
+                    if (!__ballot(is)) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
+                    for (int h = 0; h < FC; ++h) {
+                        const f32x4 d = Mma<T>::mma(a[h], b[f], acc[f][h]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
+                    }
                 }
+#pragma unroll
+                for (int h = 0; h < FC; ++h) a[h] = an[h];
+                c = next;
             }
         }
-        c = c1 < w1 ? __builtin_amdgcn_readfirstlane(A.sids[c1]) : -1;
     }
 
 #pragma unroll
@@ -520,9 +654,9 @@ __global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
 }
 
 // y: 16 columns a block, its 8 waves share the contraction; RF x 16 places.
-template <class T, int RF>
+template <class T, int RF, bool AL>
 __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
-    constexpr int E = Mma<T>::E, KS = 4 * E;
+    constexpr int E = Mma<T>::E, KS = 4 * E, UN = 4;
     __shared__ f32x4 s_red[8][RF][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
     const int64_t col0 = (int64_t)blockIdx.x * 16;
@@ -538,11 +672,19 @@ __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
 #pragma unroll
     for (int f = 0; f < RF; ++f) acc[f] = f32x4{0, 0, 0, 0};
     const int steps = (A.K + KS - 1) / KS;
-    for (int s = wave; s < steps; s += 8) {
-        const int64_t k0 = (int64_t)s * KS + g * E;
-        const u32x4 a = chunk(w, k0, A.K, A.x16);
+    for (int s = wave * UN; s < steps; s += 8 * UN) {   // steps past the last are of zeros
+        u32x4 a[UN], b[UN][RF];
 #pragma unroll
-        for (int f = 0; f < RF; ++f) acc[f] = Mma<T>::mma(a, chunk(x[f], k0, A.K, A.x16), acc[f]);
+        for (int y = 0; y < UN; ++y) {
+            const int64_t k0 = (int64_t)(s + y) * KS + g * E;
+            a[y] = AL ? chunk_aligned(w, k0, A.K) : chunk_guarded(w, k0, A.K);
+#pragma unroll
+            for (int f = 0; f < RF; ++f) b[y][f] = AL ? chunk_aligned(x[f], k0, A.K) : chunk_guarded(x[f], k0, A.K);
+        }
+#pragma unroll
+        for (int y = 0; y < UN; ++y)
+#pragma unroll
+            for (int f = 0; f < RF; ++f) acc[f] = Mma<T>::mma(a[y], b[y][f], acc[f]);
     }
 #pragma unroll
     for (int f = 0; f < RF; ++f) s_red[wave][f][lane] = acc[f];
@@ -574,56 +716,6 @@ __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
 // Gradients of the adapters: out_c = sum over the cluster's places of
 // U[row] V[place or row]^T, U wide (P), V r wide.
 
-struct Item {
-    int32_t c, p0, p1, slot;   // places p0 .. p1 of cluster c; slot: partial sum to write, -1: the result itself
-};
-
-// Chunks of every cluster, in order.  One block; lists[0] = number of items.
-struct ListArgs {
-    const int32_t* offsets;
-    int32_t k, chunk;
-    int32_t* count;      // items
-    Item* items;
-    int32_t *first, *num;   // per cluster: first partial slot, chunks (0: empty)
-};
-
-__global__ __launch_bounds__(1024) void k_ad_list(ListArgs A) {
-    __shared__ int s_i[16], s_s[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int items = 0, slots = 0;   // so far
-    for (int c0 = 0; c0 < A.k; c0 += 1024) {
-        const int c = c0 + tid;
-        const int a = c < A.k ? A.offsets[c] : 0, b = c < A.k ? A.offsets[c + 1] : 0;
-        const int ni = (b - a + A.chunk - 1) / A.chunk, ns = ni > 1 ? ni : 0;
-        int xi = ni, xs = ns;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int ui = __shfl_up(xi, o), us = __shfl_up(xs, o);
-            if (lane >= o) xi += ui, xs += us;
-        }
-        if (lane == 63) s_i[wave] = xi, s_s[wave] = xs;
-        __syncthreads();
-        int bi = items, bs = slots;
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) bi += s_i[w], bs += s_s[w];
-            items += s_i[w];
-            slots += s_s[w];
-        }
-        bi += xi - ni;
-        bs += xs - ns;
-        if (c < A.k) {
-            A.first[c] = bs;
-            A.num[c] = ni;
-            for (int q = 0; q < ni; ++q) {
-                const int p = a + q * A.chunk;
-                A.items[bi + q] = Item{c, p, b - p < A.chunk ? b : p + A.chunk, ni > 1 ? bs + q : -1};
-            }
-        }
-        __syncthreads();
-    }
-    if (tid == 0) A.count[0] = items;
-}
-
 struct GradArgs {
     const void* U;
     int64_t ldu;
@@ -640,43 +732,60 @@ struct GradArgs {
     int32_t k, P, r, v16, o4, tiles;   // o4: out written by fours
 };
 
-// 128 columns a block, 32 a wave; stages of 2 KS places.  WF: the wide operand
-// comes first (lanes hold four consecutive columns: dA), else second (four
-// consecutive indexes of r: dB).
+// 128 columns a block, 32 a wave; stages of 2 KS places, loaded while the one
+// before is multiplied (the skinny operand through registers).  WF: the wide
+// operand comes first (lanes hold four consecutive columns: dA), else second
+// (four consecutive indexes of r: dB).
 template <class T, int RF, bool WF, bool AL>
-__global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
+__device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 512], char (*s_v)[RF * 2048]) {
     constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, TC = 128, CPR = TC / E, VPR = RF * 16 / E;
-    constexpr int NU = BK * CPR / 256;
-    __shared__ __align__(16) char s_u[2][BK * TC * sizeof(T)];
-    __shared__ __align__(16) char s_v[2][BK * RF * 16 * sizeof(T)];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, li = lane & 15;
+    constexpr int NU = BK * CPR / 256, NV = (BK * VPR + 255) / 256;
+    static_assert(BK * CPR * 16 == 32 * 512 && BK * VPR * 16 == RF * 2048, "");
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t total = (int64_t)A.count[0] * A.tiles;
     for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
         const Item it = A.items[w / A.tiles];
         const int64_t bc = (w % A.tiles) * TC;
+        int64_t ur[NU], vr[NV];   // rows of the next stage to load
+        u32x4 v[NV];
+        auto rows = [&](int64_t p0) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int64_t p = p0 + (i * 256 + tid) / CPR;
+                ur[i] = row_of(A.order, p < it.p1 ? p : it.p0);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int64_t p = p0 + (i * 256 + tid) / VPR, q = p < it.p1 ? p : it.p0;
+                vr[i] = A.v_by_row ? row_of(A.order, q) : q;
+            }
+        };
         auto load = [&](int64_t p0, int buf) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int q = i * 256 + tid;
+                const bool in = p0 + q / VPR < it.p1;
+                v[i] = only_if(in, chunk(static_cast<const T*>(A.V) + vr[i] * A.ldv, q % VPR * E, A.r, A.v16));
+            }
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
                 const int q = i * 256 + tid, kk = q / CPR;
-                const int64_t p = p0 + kk, col = bc + swz_tr<T, CPR>(kk, q % CPR) * E;
-                const bool in = p < it.p1;
-                const T* src = static_cast<const T*>(A.U) + (in ? row_of(A.order, p) : 0) * A.ldu;
+                const int64_t col = bc + swz_tr<T, CPR>(kk, q % CPR) * E;
+                const bool in = p0 + kk < it.p1;
+                const T* src = static_cast<const T*>(A.U) + ur[i] * A.ldu;
                 if constexpr (AL)
                     load_lds16(in && col < A.P ? (const void*)(src + col) : (const void*)ad_zero,
                                s_u[buf] + (i * 256 + wave * 64) * 16);
                 else
-                    *reinterpret_cast<u32x4*>(s_u[buf] + q * 16) =
-                        in ? chunk_guarded(src, col, A.P) : zero_chunk<T>();
+                    *reinterpret_cast<u32x4*>(s_u[buf] + q * 16) = only_if(in, chunk_guarded(src, col, A.P));
             }
-            for (int q = tid; q < BK * VPR; q += 256) {
-                const int kk = q / VPR;
-                const int64_t p = p0 + kk;
-                u32x4 v = zero_chunk<T>();
-                if (p < it.p1) {
-                    const T* src = static_cast<const T*>(A.V) + (A.v_by_row ? row_of(A.order, p) : p) * A.ldv;
-                    v = chunk(src, (q % VPR) * E, A.r, A.v16);
-                }
-                *reinterpret_cast<u32x4*>(s_v[buf] + (kk * VPR + swz_tr<T, VPR>(kk, q % VPR)) * 16) = v;
+        };
+        auto put = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int q = i * 256 + tid, kk = q / VPR;
+                if (kk < BK) *reinterpret_cast<u32x4*>(s_v[buf] + (kk * VPR + swz_tr<T, VPR>(kk, q % VPR)) * 16) = v[i];
             }
         };
         f32x4 acc[2][RF];
@@ -685,16 +794,24 @@ __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
 #pragma unroll
             for (int j = 0; j < RF; ++j) acc[h][j] = f32x4{0, 0, 0, 0};
         int buf = 0;
+        rows(it.p0);
         load(it.p0, 0);
+        rows(it.p0 + BK);
+        put(0);
         for (int64_t p = it.p0; p < it.p1; p += BK, buf ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // The stage has landed, and every wave is done with the other buffer.
+            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
             __syncthreads();
-            if (p + BK < it.p1) load(p + BK, buf ^ 1);
+            if (p + BK < it.p1) {
+                load(p + BK, buf ^ 1);
+                rows(p + 2 * BK);
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 u32x4 a[2], b[RF];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) a[h] = read_tr<T, CPR>(s_u[buf], s * KS, tr_lane<T, CPR>(wave * 32 + h * 16, lane));
+                for (int h = 0; h < 2; ++h)
+                    a[h] = read_tr<T, CPR>(s_u[buf], s * KS, tr_lane<T, CPR>(wave * 32 + h * 16, lane));
 #pragma unroll
                 for (int j = 0; j < RF; ++j) b[j] = read_tr<T, VPR>(s_v[buf], s * KS, tr_lane<T, VPR>(j * 16, lane));
 #pragma unroll
@@ -703,6 +820,7 @@ __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
                     for (int j = 0; j < RF; ++j)
                         acc[h][j] = WF ? Mma<T>::mma(a[h], b[j], acc[h][j]) : Mma<T>::mma(b[j], a[h], acc[h][j]);
             }
+            if (p + BK < it.p1) put(buf ^ 1);
         }
         __syncthreads();   // both buffers are free for the next item
         const float sc = A.scale ? A.scale[it.c] : 1.0f;
@@ -714,9 +832,9 @@ __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
                 const int64_t slot = it.slot < 0 ? it.c : it.slot;
                 // WF: row rr of r, columns 4 g ..;  else row = column li, indexes 4 g ..
                 const int64_t rr = WF ? j * 16 + li : cw + li, x0 = WF ? cw + g * 4 : j * 16 + g * 4;
-                const int64_t rows = WF ? A.r : A.P, width = WF ? A.P : A.r;
-                if (rr >= rows) continue;
-                const int64_t at = (slot * rows + rr) * width;
+                const int64_t rows_ = WF ? A.r : A.P, width = WF ? A.P : A.r;
+                if (rr >= rows_) continue;
+                const int64_t at = (slot * rows_ + rr) * width;
                 if (it.slot < 0)
                     store4(static_cast<T*>(A.out) + at, x0, width, acc[h][j] * sc, A.o4);
                 else
@@ -725,17 +843,31 @@ __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A) {
     }
 }
 
+// dA (blockIdx.y = 0) and dB.
+template <class T, int RF, bool AL>
+__global__ __launch_bounds__(256) void k_ad_grad(GradArgs A, GradArgs B) {
+    __shared__ __align__(16) char s_u[2][32 * 512];
+    __shared__ __align__(16) char s_v[2][RF * 2048];
+    if (blockIdx.y == 0)
+        grad_block<T, RF, true, AL>(A, s_u, s_v);
+    else
+        grad_block<T, RF, false, AL>(B, s_u, s_v);
+}
+
 // Clusters of no chunk: zeros; of several: the sum of their parts in order.
+// dA: blockIdx.z = 0, dB: 1.
 template <class T>
-__global__ __launch_bounds__(256) void k_ad_join(GradArgs A) {
-    const int64_t size = (int64_t)A.r * A.P;
-    for (int c = blockIdx.y; c < A.k; c += gridDim.y) {
-        const int num = A.num[c];
+__global__ __launch_bounds__(256) void k_ad_join(GradArgs A, GradArgs B) {
+    const GradArgs& G = blockIdx.z ? B : A;
+    const int64_t size = (int64_t)G.r * G.P;
+    for (int c = blockIdx.y; c < G.k; c += gridDim.y) {
+        const int num = G.num[c];
         if (num == 1) continue;
-        const float* part = A.part + A.first[c] * size;
-        T* out = static_cast<T*>(A.out) + c * size;
+        const float* part = G.part + G.first[c] * size;
+        T* out = static_cast<T*>(G.out) + c * size;
         for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
             float sum = 0.0f;
+#pragma unroll 4
             for (int q = 0; q < num; ++q) sum += part[q * size + i];
             out[i] = from_f32<T>(sum);
         }
@@ -745,14 +877,26 @@ __global__ __launch_bounds__(256) void k_ad_join(GradArgs A) {
 // --------------------------------------------------------------------------
 // Launches
 
+// The operands' 16 x rf indexes of r: 1, 2, 4 or 8.
+template <class F>
+void by_rank(int rf, F&& go) {
+    using std::integral_constant;
+    if (rf == 1) go(integral_constant<int, 1>{});
+    else if (rf == 2) go(integral_constant<int, 2>{});
+    else if (rf <= 4) go(integral_constant<int, 4>{});
+    else go(integral_constant<int, 8>{});
+}
+
 template <class T, bool TR>
-hipError_t inner_go(const InnerArgs& A, hipStream_t s) {
-    const dim3 g((unsigned)((A.n + 15) / 16)), b(256);
+hipError_t inner_go(const InnerArgs& A, const ListArgs& L, hipStream_t s) {
+    const dim3 g((unsigned)((A.n + 15) / 16) + (TR ? 1 : 0)), b(256);
     const int rf = (A.r + 15) / 16;
-    if (rf == 1) hipLaunchKernelGGL((k_ad_inner<T, 1, TR>), g, b, 0, s, A);
-    else if (rf == 2) hipLaunchKernelGGL((k_ad_inner<T, 2, TR>), g, b, 0, s, A);
-    else if (rf <= 4) hipLaunchKernelGGL((k_ad_inner<T, 4, TR>), g, b, 0, s, A);
-    else hipLaunchKernelGGL((k_ad_inner<T, 8, TR>), g, b, 0, s, A);
+    auto go = [&](auto j) {
+        constexpr int RF = decltype(j)::value;
+        if (A.u16) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true>), g, b, 0, s, A, L);
+        else hipLaunchKernelGGL((k_ad_inner<T, RF, TR, false>), g, b, 0, s, A, L);
+    };
+    by_rank(rf, go);
     return hipGetLastError();
 }
 
@@ -785,28 +929,22 @@ hipError_t main_go(const MainArgs& A, bool al, hipStream_t s) {
     return main_tile<T, 64, 64, 2, 2, TR, true>(A, s);
 }
 
-template <class T, bool WF>
-hipError_t grad_go(const GradArgs& A, bool al, int64_t max_items, hipStream_t s) {
-    int64_t blocks = max_items * A.tiles;
+template <class T>
+hipError_t grad_go(const GradArgs& A, const GradArgs& B, bool al, int64_t max_items, hipStream_t s) {
+    int64_t blocks = max_items * (A.tiles > B.tiles ? A.tiles : B.tiles);
     if (blocks > 65536) blocks = 65536;
     if (blocks < 1) blocks = 1;
-    const dim3 g((unsigned)blocks), b(256);
-    const int rf = (A.r + 15) / 16;
-#define KM_GRAD(RF)                                                                 \
-    do {                                                                            \
-        if (al) hipLaunchKernelGGL((k_ad_grad<T, RF, WF, true>), g, b, 0, s, A);    \
-        else hipLaunchKernelGGL((k_ad_grad<T, RF, WF, false>), g, b, 0, s, A);      \
-    } while (0)
-    if (rf == 1) KM_GRAD(1);
-    else if (rf == 2) KM_GRAD(2);
-    else if (rf <= 4) KM_GRAD(4);
-    else KM_GRAD(8);
-#undef KM_GRAD
+    by_rank((A.r + 15) / 16, [&](auto j) {
+        constexpr int RF = decltype(j)::value;
+        const dim3 g((unsigned)blocks, 2), b(256);
+        if (al) hipLaunchKernelGGL((k_ad_grad<T, RF, true>), g, b, 0, s, A, B);
+        else hipLaunchKernelGGL((k_ad_grad<T, RF, false>), g, b, 0, s, A, B);
+    });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t size = (int64_t)A.r * A.P, gx = (size + 1023) / 1024;
-    hipLaunchKernelGGL((k_ad_join<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(A.k < 128 ? A.k : 128)),
-                       dim3(256), 0, s, A);
+    const int64_t size = (int64_t)A.r * (A.P > B.P ? A.P : B.P), gx = (size + 1023) / 1024;
+    hipLaunchKernelGGL((k_ad_join<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(A.k < 128 ? A.k : 128), 2),
+                       dim3(256), 0, s, A, B);
     return hipGetLastError();
 }
 
@@ -841,9 +979,15 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         hipLaunchKernelGGL((k_ad_few_inner<T>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         const dim3 g((unsigned)((D.dout + 15) / 16)), b(512);
-        if (D.n <= 16) hipLaunchKernelGGL((k_ad_few_main<T, 1>), g, b, 0, s, F);
-        else if (D.n <= 32) hipLaunchKernelGGL((k_ad_few_main<T, 2>), g, b, 0, s, F);
-        else hipLaunchKernelGGL((k_ad_few_main<T, 4>), g, b, 0, s, F);
+        auto go = [&](auto f) {
+            constexpr int RF = decltype(f)::value;
+            if (x16) hipLaunchKernelGGL((k_ad_few_main<T, RF, true>), g, b, 0, s, F);
+            else hipLaunchKernelGGL((k_ad_few_main<T, RF, false>), g, b, 0, s, F);
+        };
+        if (D.n <= 16) go(std::integral_constant<int, 1>{});
+        else if (D.n <= 32) go(std::integral_constant<int, 2>{});
+        else if (D.n <= 48) go(std::integral_constant<int, 3>{});
+        else go(std::integral_constant<int, 4>{});
         return hipGetLastError();
     }
     InnerArgs I{};
@@ -860,9 +1004,9 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     I.K = D.di;
     I.r = D.r;
     I.rp = L.rp;
-    I.u16 = I.q16 = x16;
+    I.u16 = x16;
     I.h4 = D.r % 4 == 0 && a16(D.H);
-    if ((e = inner_go<T, false>(I, s)) != hipSuccess) return e;
+    if ((e = inner_go<T, false>(I, ListArgs{}, s)) != hipSuccess) return e;
     MainArgs M{};
     M.U = D.X;
     M.ldu = D.ldx;
@@ -889,22 +1033,31 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     const bool dy16 = rows_vec16(D.dY, D.lddy, D.dout, sizeof(T)), x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T));
     hipError_t e;
     char* S = ws + L.off_s;
+    ListArgs Q{};
+    Q.offsets = D.offsets;
+    Q.k = D.k;
+    Q.chunk = L.chunk;
+    Q.count = reinterpret_cast<int32_t*>(ws + L.off_count);
+    Q.items = reinterpret_cast<Item*>(ws + L.off_items);
+    Q.first = reinterpret_cast<int32_t*>(ws + L.off_first);
+    Q.num = Q.first + D.k;
+    InnerArgs I{};
+    I.U = D.dY;
+    I.ldu = D.lddy;
+    I.Q = D.B;
+    I.order = D.order;
+    I.sids = D.sids;
+    I.offsets = D.offsets;
+    I.scale = D.scale;
+    I.S = S;
+    I.n = D.n;
+    I.K = D.dout;
+    I.r = D.r;
+    I.rp = L.rp;
+    I.u16 = dy16;
+    I.q16 = D.r % E == 0 && a16(D.B);
+    if ((e = inner_go<T, true>(I, Q, s)) != hipSuccess) return e;
     if (D.n > 0) {
-        InnerArgs I{};
-        I.U = D.dY;
-        I.ldu = D.lddy;
-        I.Q = D.B;
-        I.order = D.order;
-        I.sids = D.sids;
-        I.offsets = D.offsets;
-        I.scale = D.scale;
-        I.S = S;
-        I.n = D.n;
-        I.K = D.dout;
-        I.r = D.r;
-        I.rp = L.rp;
-        I.u16 = dy16;
-        if ((e = inner_go<T, true>(I, s)) != hipSuccess) return e;
         MainArgs M{};
         M.U = D.dY;
         M.ldu = D.lddy;
@@ -923,16 +1076,6 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.y4 = D.di % 4 == 0 && a16(D.dX);
         if ((e = main_go<T, true>(M, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
     }
-    ListArgs Q{};
-    Q.offsets = D.offsets;
-    Q.k = D.k;
-    Q.chunk = L.chunk;
-    Q.count = reinterpret_cast<int32_t*>(ws + L.off_count);
-    Q.items = reinterpret_cast<Item*>(ws + L.off_items);
-    Q.first = reinterpret_cast<int32_t*>(ws + L.off_first);
-    Q.num = Q.first + D.k;
-    hipLaunchKernelGGL(k_ad_list, dim3(1), dim3(1024), 0, s, Q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     GradArgs G{};
     G.order = D.order;
     G.count = Q.count;
@@ -963,8 +1106,9 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     B.P = D.dout;
     B.tiles = (D.dout + 127) / 128;
     B.o4 = D.r % 4 == 0 && a16(D.dB);
-    if ((e = grad_go<T, true>(G, x16, L.max_items, s)) != hipSuccess) return e;
-    return grad_go<T, false>(B, dy16, L.max_items, s);
+    // Two halves of the partial sums' segment.
+    B.part = G.part + L.part_a;
+    return grad_go<T>(G, B, x16 && dy16, L.max_items, s);
 }
 
 }  // namespace
@@ -995,7 +1139,8 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
         L.off_count = take(4);
         L.off_items = take((size_t)L.max_items * sizeof(Item));
         L.off_first = take((size_t)k * 8);
-        L.off_part = take((size_t)slots * r * (di > dout ? di : dout) * 4);
+        L.part_a = slots * r * di;
+        L.off_part = take((size_t)(L.part_a + slots * r * dout) * 4);
     }
     L.bytes = o > 0 ? o : 256;
     return L;
