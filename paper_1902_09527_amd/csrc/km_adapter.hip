@@ -123,6 +123,8 @@ __device__ __forceinline__ int64_t row_of(const int32_t* order, int64_t place) {
 // at one chunk index fall on all 64 banks once.
 __device__ __forceinline__ int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
 
+__device__ __forceinline__ int swz4(int row, int c) { return c ^ ((row >> 2) & 3); }   // rows of 64 bytes
+
 // The same for tiles that hold the contraction along their rows (TR): 16-bit
 // tiles are read 4 rows x 16 columns at a time, float32 by columns.
 template <class T, int CPR>
@@ -360,7 +362,12 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
     constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
     constexpr int kStage = (TM + TN) * 128;
-    extern __shared__ __align__(16) char s_tiles[];   // two stages: TM rows of U, then TN rows (TR: BK rows) of W
+    // Two stages: TM rows of U, then TN rows (TR: BK rows) of W; then the first
+    // matrix step of the places' inner products, their rows and clusters.
+    extern __shared__ __align__(16) char s_tiles[];
+    char* s_inner = s_tiles + 2 * kStage;
+    int32_t* s_rows = reinterpret_cast<int32_t*>(s_inner + TM * 64);
+    int32_t* s_ids = s_rows + TM;
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
 
@@ -373,6 +380,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     const int gm = A.tm - m0 < 4 ? (int)(A.tm - m0) : 4;
     const int64_t in_grp = t - grp * 4 * A.tn;
     const int64_t bm = (m0 + in_grp % gm) * TM, bn = in_grp / gm * TN;
+    const int64_t w0 = bm + wr * (TM / WR), cb = bn + wc * (TN / WC);
 
     // Where a thread's chunks of a stage come from: pointers that move on with
     // the stages (AL), the place in the stage being fixed.
@@ -384,7 +392,12 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     for (int i = 0; i < NU; ++i) {
         int64_t place = bm + (i * NT + tid) / 8;
         if (place >= A.n) place = A.n - 1;   // not stored
-        up[i] = static_cast<const T*>(A.U) + row_of(A.order, place) * A.ldu + uc;
+        const int64_t row = row_of(A.order, place);
+        up[i] = static_cast<const T*>(A.U) + row * A.ldu + uc;
+        if (tid % 8 == 0) {
+            s_rows[(i * NT + tid) / 8] = (int32_t)row;
+            s_ids[(i * NT + tid) / 8] = A.sids[place];
+        }
     }
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
@@ -444,6 +457,15 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
 #pragma unroll
         for (int i = 0; i < NU + NW; ++i) load(i, kt, buf, kt >= whole);
     };
+
+    load_all(0, s_tiles);
+    if (nk > 1) load_all(1, s_tiles + kStage);
+#pragma unroll
+    for (int i = 0; i < TM * 4 / NT; ++i) {
+        const int q = i * NT + tid;
+        const int64_t place = bm + q / 4 < A.n ? bm + q / 4 : A.n - 1;
+        load_lds16(static_cast<const T*>(A.S) + place * A.rp + q % 4 * E, s_inner + (i * NT + wave * 64) * 16);
+    }
 
     f32x4 acc[FR][FC];
 #pragma unroll
@@ -510,9 +532,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     };
 
     Frags F0, F1;
-    load_all(0, s_tiles);
     turn();
-    if (nk > 1) load_all(1, s_tiles + kStage);
 #pragma unroll
     for (int i = 0; i < FR + FC; ++i) read(F0, i, s_tiles, 0);
     auto stage = [&](int kt, bool last) {
@@ -528,20 +548,64 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     };
     int kt = 0;
     for (; kt + 2 < whole; ++kt) stage(kt, false);
-    for (; kt < nk; ++kt) stage(kt, true);
+    for (; kt + 1 < nk; ++kt) stage(kt, true);
+
+    // The adapters' operand of one cluster and matrix step, the wave's CN
+    // columns, to its part of the buffer that the last stage leaves free (two
+    // places in turn).  The first is loaded beside the last stage.
+    constexpr int CN = TN / WC;
+    char* s_q = s_tiles + (nk & 1) * kStage + wave * (2 * CN * 64);
+    static_assert(WR * WC * 2 * CN * 64 <= kStage, "");
+    auto fetch = [&](int c, int k0, int buf) {
+        char* to = s_q + buf * CN * 64;
+        if (A.q16) {
+#pragma unroll
+            for (int i = 0; i < CN * 4 / 64; ++i) {
+                const int q = i * 64 + lane;
+                const T* src;
+                bool in;
+                if constexpr (TR) {
+                    const int kk = q / (CN / E);
+                    const int64_t col = cb + swz_tr<T, CN / E>(kk, q % (CN / E)) * E;
+                    in = k0 + kk < A.r && col < A.P;
+                    src = static_cast<const T*>(A.Q) + ((int64_t)c * A.r + k0 + kk) * A.P + col;
+                } else {
+                    const int64_t col = cb + q / 4;
+                    const int rr = k0 + swz4(q / 4, q % 4) * E;
+                    in = col < A.P && rr < A.r;
+                    src = static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r + rr;
+                }
+                load_lds16(in ? (const void*)src : (const void*)ad_zero, to + i * 1024);
+            }
+        } else {
+#pragma unroll 1
+            for (int q = lane; q < CN * 4; q += 64) {
+                u32x4 v;
+                if constexpr (TR) {
+                    const int kk = q / (CN / E), rr = k0 + kk < A.r ? k0 + kk : 0;
+                    v = only_if(k0 + kk < A.r,
+                                chunk_guarded(static_cast<const T*>(A.Q) + ((int64_t)c * A.r + rr) * A.P,
+                                              cb + swz_tr<T, CN / E>(kk, q % (CN / E)) * E, A.P));
+                } else {
+                    const int64_t col = cb + q / 4 < A.P ? cb + q / 4 : 0;   // columns past P are not stored
+                    v = chunk_guarded(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r,
+                                      k0 + swz4(q / 4, q % 4) * E, A.r);
+                }
+                *reinterpret_cast<u32x4*>(to + q * 16) = v;
+            }
+        }
+    };
+    const int c_first = w0 < A.n ? __builtin_amdgcn_readfirstlane(s_ids[w0 - bm]) : -1;
+    if (c_first >= 0) fetch(c_first, 0, 0);
+    stage(kt, true);
 
     // The adapters' term, cluster by cluster of the wave's places (they are in
     // cluster order): a lane keeps the sum only where its place is of the
     // cluster, so that nothing of one cluster's adapter reaches another's rows.
     // The next cluster's operand is loaded during the products of one.
-    const int64_t w0 = bm + wr * (TM / WR), cb = bn + wc * (TN / WC);
     int mine[FR];
 #pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int64_t place = w0 + f * 16 + li;
-        const int id = A.sids[place < A.n ? place : A.n - 1];
-        mine[f] = place < A.n ? id : -1;
-    }
+    for (int f = 0; f < FR; ++f) mine[f] = w0 + f * 16 + li < A.n ? s_ids[w0 - bm + f * 16 + li] : -1;
     auto after = [&](int c) {   // the lowest cluster above c of the wave's places, -1: none
         int next = -1;
 #pragma unroll
@@ -551,46 +615,38 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         }
         return next;
     };
-    auto adapter = [&](u32x4* a, int c, int k0) {
+    for (int k0 = 0; c_first >= 0 && k0 < A.rp; k0 += KS) {
+        int buf = 0;
+        if (k0 > 0) fetch(c_first, k0, 0);
+        for (int c = c_first; c >= 0; buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the wave's own part of LDS
+            u32x4 a[FC];
 #pragma unroll
-        for (int h = 0; h < FC; ++h) {
-            const int64_t col = cb + h * 16 + li, cc = col < A.P ? col : 0;   // columns past P are not stored
-            if constexpr (TR)
-                a[h] = chunk_guarded(static_cast<const T*>(A.Q) + (int64_t)c * A.r * A.P + cc, k0 + g * E, A.r, A.P);
-            else
-                a[h] = chunk(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + cc) * A.r, k0 + g * E, A.r, A.q16);
-        }
-    };
-    const int c_first = after(-1);
-    if (c_first >= 0) {
-        for (int k0 = 0; k0 < A.rp; k0 += KS) {
-            u32x4 b[FR], a[FC];
-            adapter(a, c_first, k0);
+            for (int h = 0; h < FC; ++h) {
+                const char* q = s_q + buf * CN * 64;
+                if constexpr (TR)
+                    a[h] = read_tr<T, CN / E>(q, 0, tr_lane<T, CN / E>(h * 16, lane));
+                else
+                    a[h] = *reinterpret_cast<const u32x4*>(q + ((h * 16 + li) * 4 + swz4(li, g)) * 16);
+            }
+            const int next = after(c);
+            if (next >= 0) fetch(next, k0, buf ^ 1);
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
-                const int64_t place = w0 + f * 16 + li;
-                b[f] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) +
-                                                       (place < A.n ? place : A.n - 1) * A.rp + k0 + g * E);
-            }
-            for (int c = c_first; c >= 0;) {
-                const int next = after(c);
-                u32x4 an[FC];
-                adapter(an, next < 0 ? c : next, k0);
+                const bool is = mine[f] == c;
+                if (!__ballot(is)) continue;
+                const int64_t place = w0 + f * 16 + li < A.n ? w0 + f * 16 + li : A.n - 1;
+                const u32x4 b = k0 == 0
+                                    ? *reinterpret_cast<const u32x4*>(s_inner + (place - bm) * 64 + g * 16)
+                                    : *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) + place * A.rp + k0 + g * E);
 #pragma unroll
-                for (int f = 0; f < FR; ++f) {
-                    const bool is = mine[f] == c;
-                    if (!__ballot(is)) continue;
+                for (int h = 0; h < FC; ++h) {
+                    const f32x4 d = Mma<T>::mma(a[h], b, acc[f][h]);
 #pragma unroll
-                    for (int h = 0; h < FC; ++h) {
-                        const f32x4 d = Mma<T>::mma(a[h], b[f], acc[f][h]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
-                    }
+                    for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
                 }
-#pragma unroll
-                for (int h = 0; h < FC; ++h) a[h] = an[h];
-                c = next;
             }
+            c = next;
         }
     }
 
@@ -598,7 +654,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     for (int f = 0; f < FR; ++f) {
         const int64_t place = w0 + f * 16 + li;
         if (place >= A.n) continue;
-        T* y = static_cast<T*>(A.Y) + row_of(A.order, place) * A.P;
+        T* y = static_cast<T*>(A.Y) + (int64_t)s_rows[place - bm] * A.P;
 #pragma unroll
         for (int h = 0; h < FC; ++h) store4(y, cb + h * 16 + g * 4, A.P, acc[f][h], A.y4);
     }
@@ -909,7 +965,7 @@ template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
 hipError_t main_tile(MainArgs A, hipStream_t s) {
     A.tm = (int)((A.n + TM - 1) / TM);
     A.tn = (A.P + TN - 1) / TN;
-    constexpr int lds = 2 * (TM + TN) * 128;
+    constexpr int lds = 2 * (TM + TN) * 128 + TM * 72;
     if (lds > 65536) {
         const hipError_t e = raise_lds(k_ad_main<T, TM, TN, WR, WC, TR, AL>, lds);
         if (e != hipSuccess) return e;
@@ -1074,6 +1130,7 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.r = D.r;
         M.rp = L.rp;
         M.y4 = D.di % 4 == 0 && a16(D.dX);
+    M.q16 = D.di % E == 0 && a16(D.A);
         if ((e = main_go<T, true>(M, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
     }
     GradArgs G{};
