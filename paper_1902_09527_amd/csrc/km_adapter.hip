@@ -15,6 +15,8 @@
 //
 // Sums are float32 (matrix-core accumulators); h and g are rounded to the
 // rows' type, once, as the matrix cores' operands.
+#include <math.h>
+
 #include <type_traits>
 
 #include "km_ops.h"
@@ -354,18 +356,20 @@ struct MainArgs {
     int64_t n;
     int32_t K, P, r, rp, q16, y4;
     int32_t tm, tn;   // tiles
+    int32_t splits;   // parts of the contraction, a block each; more than one: sums to part
+    float* part;      // splits x n x P, by place
 };
 
-template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
+template <class T, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
 __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
     constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
     constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
     constexpr int kStage = (TM + TN) * 128;
-    // Two stages: TM rows of U, then TN rows (TR: BK rows) of W; then the first
-    // matrix step of the places' inner products, their rows and clusters.
+    // A ring of NS stages: TM rows of U, then TN rows (TR: BK rows) of W; then the
+    // first matrix step of the places' inner products, their rows and clusters.
     extern __shared__ __align__(16) char s_tiles[];
-    char* s_inner = s_tiles + 2 * kStage;
+    char* s_inner = s_tiles + NS * kStage;
     int32_t* s_rows = reinterpret_cast<int32_t*>(s_inner + TM * 64);
     int32_t* s_ids = s_rows + TM;
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
@@ -373,9 +377,13 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
 
     // Consecutive tiles go to one XCD (blocks are dealt over 8), down 4 tiles
     // of places before the next columns.
-    const int64_t tiles = (int64_t)A.tm * A.tn, per = (tiles + 7) / 8;
-    const int64_t t = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    const int64_t tiles = (int64_t)A.tm * A.tn * A.splits, per = (tiles + 7) / 8;
+    int64_t t = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per || t >= tiles) return;
+    // This block's stages k_first .. of the contraction.
+    const int all = (A.K + BK - 1) / BK, share = (all + A.splits - 1) / A.splits, split = (int)(t % A.splits);
+    t /= A.splits;
+    const int k_first = split * share, nk = all - k_first < share ? all - k_first : share;   // >= 1, as the host sees to
     const int64_t grp = t / (4 * (int64_t)A.tn), m0 = grp * 4;
     const int gm = A.tm - m0 < 4 ? (int)(A.tm - m0) : 4;
     const int64_t in_grp = t - grp * 4 * A.tn;
@@ -393,7 +401,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         int64_t place = bm + (i * NT + tid) / 8;
         if (place >= A.n) place = A.n - 1;   // not stored
         const int64_t row = row_of(A.order, place);
-        up[i] = static_cast<const T*>(A.U) + row * A.ldu + uc;
+        up[i] = static_cast<const T*>(A.U) + row * A.ldu + uc + (int64_t)k_first * BK;
         if (tid % 8 == 0) {
             s_rows[(i * NT + tid) / 8] = (int32_t)row;
             s_ids[(i * NT + tid) / 8] = A.sids[place];
@@ -404,27 +412,26 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         const int q = i * NT + tid;
         if constexpr (TR) {
             const int kk = q / CPR;
-            wp[i] = static_cast<const T*>(A.W) + (int64_t)kk * A.P + bn + swz_tr<T, CPR>(kk, q % CPR) * E;
+            wp[i] = static_cast<const T*>(A.W) + ((int64_t)k_first * BK + kk) * A.P + bn + swz_tr<T, CPR>(kk, q % CPR) * E;
         } else {
             int64_t col = bn + q / 8;
             if (col >= A.P) col = A.P - 1;   // not stored
-            wp[i] = static_cast<const T*>(A.W) + col * A.K + uc;
+            wp[i] = static_cast<const T*>(A.W) + col * A.K + uc + (int64_t)k_first * BK;
         }
     }
-    const int nk = (A.K + BK - 1) / BK;
-    // Stages without a chunk past the contraction's end or the last column.
-    const int whole = !TR || bn + TN <= A.P ? A.K / BK : 0;
+    // Stages (of this block) without a chunk past the contraction's end or the last column.
+    const int k_left = A.K - k_first * BK, whole = !TR || bn + TN <= A.P ? k_left / BK : 0;
 
     // Chunk i of stage kt (of NU + NW a thread) to LDS; guard: it may lie past an end.
     auto load = [&](int i, int kt, char* buf, bool guard) {
         if (i < NU) {
             if constexpr (AL) {
-                const void* src = !guard || kt * BK + uc < A.K ? (const void*)up[i] : (const void*)ad_zero;
+                const void* src = !guard || kt * BK + uc < k_left ? (const void*)up[i] : (const void*)ad_zero;
                 load_lds16(src, buf + (i * NT + wave * 64) * 16);
                 up[i] += BK;
             } else {
                 *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) =
-                    chunk_guarded(up[i] - uc, (int64_t)kt * BK + uc, A.K);
+                    chunk_guarded(up[i] - uc, (int64_t)kt * BK + uc, k_left);
             }
             return;
         }
@@ -435,21 +442,21 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             const int kk = q / CPR;
             const int64_t col = bn + swz_tr<T, CPR>(kk, q % CPR) * E;
             if constexpr (AL) {
-                const bool in = !guard || (kt * BK + kk < A.K && col < A.P);
+                const bool in = !guard || (kt * BK + kk < k_left && col < A.P);
                 load_lds16(in ? (const void*)wp[i] : (const void*)ad_zero, wb + (i * NT + wave * 64) * 16);
                 wp[i] += (int64_t)BK * A.P;
             } else {
-                const int64_t k = (int64_t)kt * BK + kk;
+                const int64_t k = (int64_t)(k_first + kt) * BK + kk;
                 *reinterpret_cast<u32x4*>(wb + q * 16) = only_if(
                     k < A.K, chunk_guarded(static_cast<const T*>(A.W) + (k < A.K ? k : 0) * A.P, col, A.P));
             }
         } else {
             if constexpr (AL) {
-                const void* src = !guard || kt * BK + uc < A.K ? (const void*)wp[i] : (const void*)ad_zero;
+                const void* src = !guard || kt * BK + uc < k_left ? (const void*)wp[i] : (const void*)ad_zero;
                 load_lds16(src, wb + (i * NT + wave * 64) * 16);
                 wp[i] += BK;
             } else {
-                *reinterpret_cast<u32x4*>(wb + q * 16) = chunk_guarded(wp[i] - uc, (int64_t)kt * BK + uc, A.K);
+                *reinterpret_cast<u32x4*>(wb + q * 16) = chunk_guarded(wp[i] - uc, (int64_t)kt * BK + uc, k_left);
             }
         }
     };
@@ -458,8 +465,9 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         for (int i = 0; i < NU + NW; ++i) load(i, kt, buf, kt >= whole);
     };
 
-    load_all(0, s_tiles);
-    if (nk > 1) load_all(1, s_tiles + kStage);
+#pragma unroll
+    for (int kt = 0; kt < NS; ++kt)
+        if (kt < nk) load_all(kt, s_tiles + kt * kStage);
 #pragma unroll
     for (int i = 0; i < TM * 4 / NT; ++i) {
         const int q = i * NT + tid;
@@ -503,7 +511,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     // stage stands between its two halves of products, when the second half's
     // operands are in registers, and loads, reads and products are issued in
     // turns (kParts of each), so that the matrix cores do not wait for either.
-    constexpr int kParts = FR < 4 ? FR : 4;
+    constexpr int kParts = FR % 4 == 0 && (FR + FC) % 4 == 0 ? 4 : 2;
     constexpr int kLoads = (NU + NW) / kParts, kReads = (FR + FC) / kParts;
     static_assert((NU + NW) % kParts == 0 && (FR + FC) % kParts == 0 && FR % kParts == 0, "");
     // The products of F; F2 read from buf2 (half s2); kl >= 0: stage kl loaded into bufl.
@@ -525,36 +533,44 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     };
     // This wave's operands have arrived (F2 of the half before).
     auto arrived = [&]() { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
-    // Every wave's reads of one stage and its loads of the next have ended.
-    auto turn = [&]() {
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
-        __syncthreads();
+    // Every wave's reads of one stage and its loads of the next have ended; the
+    // loads of the stages behind that one (kBehind) may be on their way.
+    constexpr int kBehind = (NS - 2) * (NU + NW);
+    static_assert(kBehind < 64, "");
+    auto turn = [&](bool all) {
+        if (all) __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+        else __builtin_amdgcn_s_waitcnt(0x0070 | (kBehind & 15) | (kBehind >> 4) << 14);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
 
     Frags F0, F1;
-    turn();
+    turn(true);
 #pragma unroll
     for (int i = 0; i < FR + FC; ++i) read(F0, i, s_tiles, 0);
+    int at = 0;   // the stage's place in the ring
     auto stage = [&](int kt, bool last) {
-        char* cur = s_tiles + (kt & 1) * kStage;
-        const char* nxt = s_tiles + ((kt + 1) & 1) * kStage;
+        char* cur = s_tiles + at * kStage;
+        at = at + 1 == NS ? 0 : at + 1;
+        const char* nxt = s_tiles + at * kStage;
         arrived();
         __builtin_amdgcn_sched_barrier(0);
         half(F0, F1, cur, 1, -1, cur, false);
-        turn();
+        turn(last);
         __builtin_amdgcn_sched_barrier(0);
         // After the last stage the reads are of what the buffer held before, and are not used.
-        half(F1, F0, nxt, 0, !last ? kt + 2 : kt + 2 < nk ? kt + 2 : -1, cur, last);
+        half(F1, F0, nxt, 0, !last ? kt + NS : kt + NS < nk ? kt + NS : -1, cur, last);
     };
     int kt = 0;
-    for (; kt + 2 < whole; ++kt) stage(kt, false);
+    for (; kt + NS < whole && kt + NS < nk; ++kt) stage(kt, false);
     for (; kt + 1 < nk; ++kt) stage(kt, true);
 
     // The adapters' operand of one cluster and matrix step, the wave's CN
-    // columns, to its part of the buffer that the last stage leaves free (two
+    // columns, to its part of the buffer of the stage before the last (two
     // places in turn).  The first is loaded beside the last stage.
     constexpr int CN = TN / WC;
-    char* s_q = s_tiles + (nk & 1) * kStage + wave * (2 * CN * 64);
+    char* s_q = s_tiles + (at == 0 ? NS - 1 : at - 1) * kStage + wave * (2 * CN * 64);
     static_assert(WR * WC * 2 * CN * 64 <= kStage, "");
     auto fetch = [&](int c, int k0, int buf) {
         char* to = s_q + buf * CN * 64;
@@ -595,7 +611,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             }
         }
     };
-    const int c_first = w0 < A.n ? __builtin_amdgcn_readfirstlane(s_ids[w0 - bm]) : -1;
+    // The adapters' term belongs to the first part of the contraction.
+    const int c_first = w0 < A.n && split == 0 ? __builtin_amdgcn_readfirstlane(s_ids[w0 - bm]) : -1;
     if (c_first >= 0) fetch(c_first, 0, 0);
     stage(kt, true);
 
@@ -654,38 +671,64 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     for (int f = 0; f < FR; ++f) {
         const int64_t place = w0 + f * 16 + li;
         if (place >= A.n) continue;
+        if (A.splits > 1) {
+            float* y = A.part + ((int64_t)split * A.n + place) * A.P;
+#pragma unroll
+            for (int h = 0; h < FC; ++h) store4(y, cb + h * 16 + g * 4, A.P, acc[f][h], A.P % 4 == 0);
+            continue;
+        }
         T* y = static_cast<T*>(A.Y) + (int64_t)s_rows[place - bm] * A.P;
 #pragma unroll
         for (int h = 0; h < FC; ++h) store4(y, cb + h * 16 + g * 4, A.P, acc[f][h], A.y4);
     }
 }
 
+// The parts of the contraction, added in order: a block a place and 1024 columns.
+template <class T>
+__global__ __launch_bounds__(256) void k_ad_sum(MainArgs A) {
+    const int64_t place = blockIdx.x, col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
+    if (col >= A.P) return;
+    T* y = static_cast<T*>(A.Y) + row_of(A.order, place) * A.P;
+    const float* p = A.part + place * A.P + col;
+    const int64_t step = A.n * A.P;
+    f32x4 v{0, 0, 0, 0};
+    if (A.P % 4 == 0) {
+#pragma unroll 4
+        for (int q = 0; q < A.splits; ++q) v += *reinterpret_cast<const f32x4*>(p + q * step);
+    } else {
+        for (int q = 0; q < A.splits; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < A.P) v[i] += p[q * step + i];
+    }
+    store4(y, col, A.P, v, A.y4);
+}
+
 // --------------------------------------------------------------------------
 // Few rows, forward: the time is that of reading W (and the adapters) once.
 
-// h: a wave a (place, index), its lanes along the row.  S is float32 here.
 struct FewArgs {
     const void* X;
     int64_t ldx;
     const void *W, *A, *B;
     const int32_t *order, *cl;   // cl: the cluster of every place (a plan's), or of every row (order null)
     const float* scale;
-    float* S;
-    void *H, *Y;
-    int32_t n, K, P, r, k, x16, y4;
+    void *S, *H, *Y;             // S: float32, n x r; PAD: of the rows' type, n x rp, zero past r
+    int32_t n, K, P, r, rp, k, x16, q16, y4;
 };
 
-template <class T>
+// h: a wave a (place, index), its lanes along the row.
+template <class T, bool PAD>
 __global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
     constexpr int E = Mma<T>::E;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wide = PAD ? A.rp : A.r;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= (int64_t)A.n * A.r) return;
-    const int p = (int)(w / A.r), j = (int)(w % A.r);
+    if (w >= (int64_t)A.n * wide) return;
+    const int p = (int)(w / wide), j = (int)(w % wide);
     const int c = A.cl[p];
     const int64_t row = row_of(A.order, p);
     float sum = 0.0f;
-    const bool in = (unsigned)c < (unsigned)A.k;
+    const bool in = (unsigned)c < (unsigned)A.k && j < A.r;
     if (in) {
         const T* x = static_cast<const T*>(A.X) + row * A.ldx;
         const T* a = static_cast<const T*>(A.A) + ((int64_t)c * A.r + j) * A.K;
@@ -704,8 +747,55 @@ __global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
     }
     sum = group_sum<64>(sum);
     if (lane == 0) {
-        static_cast<T*>(A.H)[row * A.r + j] = from_f32<T>(sum);
-        A.S[(int64_t)p * A.r + j] = in ? sum * (A.scale ? A.scale[c] : 1.0f) : 0.0f;
+        if (j < A.r) static_cast<T*>(A.H)[row * A.r + j] = from_f32<T>(sum);
+        const float s = in ? sum * (A.scale ? A.scale[c] : 1.0f) : 0.0f;
+        if constexpr (PAD) static_cast<T*>(A.S)[(int64_t)p * A.rp + j] = from_f32<T>(s);
+        else static_cast<float*>(A.S)[(int64_t)p * A.r + j] = s;
+    }
+}
+
+// g: a block a (place, 16 indexes), its threads along the contraction, a row
+// of B_c each.  One more block lists the chunks.
+template <class T>
+__global__ __launch_bounds__(256) void k_ad_few_inner_t(FewArgs A, ListArgs L) {
+    constexpr int E = Mma<T>::E;
+    __shared__ float s_sum[4][16];
+    if (blockIdx.x == gridDim.x - 1) {
+        list_chunks(L, reinterpret_cast<int*>(s_sum));
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, jc = A.rp / 16;
+    const int p = (int)(blockIdx.x / jc), j0 = (int)(blockIdx.x % jc) * 16;
+    const int c = A.cl[p];
+    float acc[16] = {};
+    if (c >= 0 && j0 < A.r) {
+        const T* x = static_cast<const T*>(A.X) + row_of(A.order, p) * A.ldx;
+        const T* b = static_cast<const T*>(A.B) + (int64_t)c * A.K * A.r;
+#pragma unroll 2
+        for (int k = threadIdx.x; k < A.K; k += 256) {
+            const float u = to_f32(x[k]);
+#pragma unroll
+            for (int q = 0; q < 16 / E; ++q) {
+                const Vec<T, E> v = __builtin_bit_cast(
+                    Vec<T, E>, A.q16 ? chunk_aligned(b + (int64_t)k * A.r, j0 + q * E, A.r)
+                                     : chunk_guarded(b + (int64_t)k * A.r, j0 + q * E, A.r));
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[q * E + e] = fmaf(u, to_f32(v.e[e]), acc[q * E + e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        acc[i] = group_sum<64>(acc[i]);
+        if (lane == 0) s_sum[wave][i] = acc[i];
+    }
+    __syncthreads();
+    const int i = threadIdx.x;
+    if (i < 16) {
+        const bool in = c >= 0 && j0 + i < A.r;
+        const float s = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
+        static_cast<T*>(A.S)[(int64_t)p * A.rp + j0 + i] =
+            from_f32<T>(in ? s * (A.scale ? A.scale[c] : 1.0f) : 0.0f);
     }
 }
 
@@ -754,7 +844,7 @@ __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
         const int c = A.cl[p];
         const int64_t o0 = col0 + g * 4;
         if ((unsigned)c < (unsigned)A.k) {
-            const float* s = A.S + (int64_t)p * A.r;
+            const float* s = static_cast<const float*>(A.S) + (int64_t)p * A.r;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (o0 + i >= A.P) continue;
@@ -961,28 +1051,32 @@ hipError_t raise_lds(K* kernel, int bytes) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <class T, int TM, int TN, int WR, int WC, bool TR, bool AL>
+template <class T, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
 hipError_t main_tile(MainArgs A, hipStream_t s) {
     A.tm = (int)((A.n + TM - 1) / TM);
     A.tn = (A.P + TN - 1) / TN;
-    constexpr int lds = 2 * (TM + TN) * 128 + TM * 72;
+    constexpr int BK = 8 * Mma<T>::E;
+    const int all = (A.K + BK - 1) / BK, share = (all + A.splits - 1) / A.splits;
+    A.splits = (all + share - 1) / share;   // no part without a stage
+    constexpr int lds = NS * (TM + TN) * 128 + TM * 72;
     if (lds > 65536) {
-        const hipError_t e = raise_lds(k_ad_main<T, TM, TN, WR, WC, TR, AL>, lds);
+        const hipError_t e = raise_lds(k_ad_main<T, TM, TN, WR, WC, NS, TR, AL>, lds);
         if (e != hipSuccess) return e;
     }
-    const int64_t tiles = (int64_t)A.tm * A.tn;
-    hipLaunchKernelGGL((k_ad_main<T, TM, TN, WR, WC, TR, AL>), dim3((unsigned)((tiles + 7) / 8 * 8)),
+    const int64_t tiles = (int64_t)A.tm * A.tn * A.splits;
+    hipLaunchKernelGGL((k_ad_main<T, TM, TN, WR, WC, NS, TR, AL>), dim3((unsigned)((tiles + 7) / 8 * 8)),
                        dim3(64 * WR * WC), lds, s, A);
+    if (A.splits > 1)
+        hipLaunchKernelGGL((k_ad_sum<T>), dim3((unsigned)A.n, (unsigned)((A.P + 1023) / 1024)), dim3(256), 0, s, A);
     return hipGetLastError();
 }
 
 template <class T, bool TR>
-hipError_t main_go(const MainArgs& A, bool al, hipStream_t s) {
-    if (!al) return main_tile<T, 64, 64, 2, 2, TR, false>(A, s);
-    auto tiles = [&](int64_t m, int64_t n) { return (A.n + m - 1) / m * ((A.P + n - 1) / n); };
-    if (tiles(256, 256) >= 256) return main_tile<T, 256, 256, 2, 4, TR, true>(A, s);
-    if (tiles(128, 128) >= 256) return main_tile<T, 128, 128, 2, 2, TR, true>(A, s);
-    return main_tile<T, 64, 64, 2, 2, TR, true>(A, s);
+hipError_t main_go(const MainArgs& A, const MainShape& M, bool al, hipStream_t s) {
+    if (!al) return main_tile<T, 64, 64, 2, 2, 2, TR, false>(A, s);
+    if (M.tile == 256) return main_tile<T, 256, 256, 2, 4, 2, TR, true>(A, s);
+    if (M.tile == 128) return main_tile<T, 128, 128, 2, 4, 4, TR, true>(A, s);
+    return main_tile<T, 64, 64, 2, 2, 2, TR, true>(A, s);
 }
 
 template <class T>
@@ -1004,6 +1098,11 @@ hipError_t grad_go(const GradArgs& A, const GradArgs& B, bool al, int64_t max_it
     return hipGetLastError();
 }
 
+// Rows up to which the inner products are formed a wave a row and index: the
+// 16-row blocks of k_ad_inner take a block's clusters one after the other, and
+// there are too few of them (128 rows of 4096, 32 clusters: 50 us).
+constexpr int kFewInner = 1024;
+
 bool a16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <class T>
@@ -1012,7 +1111,26 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     const bool x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T)) && a16(D.W) && a16(D.A);
     const bool y4 = D.dout % 4 == 0 && a16(D.Y);
     hipError_t e;
-    if (L.few) {
+    MainArgs M{};
+    M.U = D.X;
+    M.ldu = D.ldx;
+    M.W = D.W;
+    M.Q = D.B;
+    M.S = ws + L.off_s;
+    M.order = D.order;
+    M.sids = D.sids;
+    M.offsets = D.offsets;
+    M.Y = D.Y;
+    M.n = D.n;
+    M.K = D.di;
+    M.P = D.dout;
+    M.r = D.r;
+    M.rp = L.rp;
+    M.q16 = D.r % E == 0 && a16(D.B);
+    M.y4 = y4;
+    M.splits = L.main.splits;
+    M.part = reinterpret_cast<float*>(ws + L.off_split);
+    if (L.few || D.n <= kFewInner) {
         FewArgs F{};
         F.X = D.X;
         F.ldx = D.ldx;
@@ -1022,7 +1140,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         F.order = D.order;
         F.cl = D.sids ? D.sids : D.ids;
         F.scale = D.scale;
-        F.S = reinterpret_cast<float*>(ws + L.off_s);
+        F.S = ws + L.off_s;
         F.H = D.H;
         F.Y = D.Y;
         F.n = (int32_t)D.n;
@@ -1032,7 +1150,13 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         F.k = D.k;
         F.x16 = x16;
         F.y4 = y4;
-        hipLaunchKernelGGL((k_ad_few_inner<T>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
+        F.rp = L.rp;
+        if (!L.few) {
+            hipLaunchKernelGGL((k_ad_few_inner<T, true>), dim3((unsigned)((D.n * L.rp + 3) / 4)), dim3(256), 0, s, F);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            return main_go<T, false>(M, L.main, x16, s);
+        }
+        hipLaunchKernelGGL((k_ad_few_inner<T, false>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         const dim3 g((unsigned)((D.dout + 15) / 16)), b(512);
         auto go = [&](auto f) {
@@ -1063,24 +1187,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     I.u16 = x16;
     I.h4 = D.r % 4 == 0 && a16(D.H);
     if ((e = inner_go<T, false>(I, ListArgs{}, s)) != hipSuccess) return e;
-    MainArgs M{};
-    M.U = D.X;
-    M.ldu = D.ldx;
-    M.W = D.W;
-    M.Q = D.B;
-    M.S = I.S;
-    M.order = D.order;
-    M.sids = D.sids;
-    M.offsets = D.offsets;
-    M.Y = D.Y;
-    M.n = D.n;
-    M.K = D.di;
-    M.P = D.dout;
-    M.r = D.r;
-    M.rp = L.rp;
-    M.q16 = D.r % E == 0 && a16(D.B);
-    M.y4 = y4;
-    return main_go<T, false>(M, x16, s);
+    return main_go<T, false>(M, L.main, x16, s);
 }
 
 template <class T>
@@ -1112,7 +1219,26 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     I.rp = L.rp;
     I.u16 = dy16;
     I.q16 = D.r % E == 0 && a16(D.B);
-    if ((e = inner_go<T, true>(I, Q, s)) != hipSuccess) return e;
+    if (D.n <= kFewInner) {
+        FewArgs F{};
+        F.X = D.dY;
+        F.ldx = D.lddy;
+        F.B = D.B;
+        F.order = D.order;
+        F.cl = D.sids;
+        F.scale = D.scale;
+        F.S = S;
+        F.n = (int32_t)D.n;
+        F.K = D.dout;
+        F.r = D.r;
+        F.rp = L.rp;
+        F.k = D.k;
+        F.q16 = I.q16;
+        hipLaunchKernelGGL((k_ad_few_inner_t<T>), dim3((unsigned)(D.n * (L.rp / 16) + 1)), dim3(256), 0, s, F, Q);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else if ((e = inner_go<T, true>(I, Q, s)) != hipSuccess) {
+        return e;
+    }
     if (D.n > 0) {
         MainArgs M{};
         M.U = D.dY;
@@ -1131,7 +1257,9 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.rp = L.rp;
         M.y4 = D.di % 4 == 0 && a16(D.dX);
     M.q16 = D.di % E == 0 && a16(D.A);
-        if ((e = main_go<T, true>(M, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
+        M.splits = L.main.splits;
+        M.part = reinterpret_cast<float*>(ws + L.off_split);
+        if ((e = main_go<T, true>(M, L.main, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
     }
     GradArgs G{};
     G.order = D.order;
@@ -1170,6 +1298,45 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
 
 }  // namespace
 
+namespace {
+
+// The tile and the parts of the contraction of an n x P product over K, by an
+// estimate of its time.  Unit: a 64 x 64 tile's stage by itself on a compute
+// unit.  256 and 128 wide tiles take a compute unit each, four of 64 share one
+// and make up for each other's waits.  Measured at 4096^3, a flop of the three
+// costs 1 : 1.4 : 1.9 in 16 bits and 1 : 1.04 : 1.13 in float32; a tile's start
+// and end cost about `edge` of its stages.  Parts of the contraction keep the
+// chip busy where there are few tiles, and cost the float32 sums they write
+// and a launch.
+MainShape main_shape(int64_t n, int32_t K, int32_t P, int type) {
+    const bool f32 = type == kF32;
+    const int all = (K + (f32 ? 31 : 63)) / (f32 ? 32 : 64);
+    const double us = f32 ? 0.48 : 0.122;   // a unit
+    const struct {
+        int tile, slots;
+        double work, cost16, cost32, edge16, edge32;
+    } kinds[3] = {{256, 256, 16, 1.0, 1.0, 4, 1}, {128, 256, 4, 1.4, 1.04, 12, 3}, {64, 1024, 4, 1.9, 1.13, 4, 1}};
+    MainShape best{64, 1};
+    double least = 0;
+    for (const auto& k : kinds)
+        for (int splits = 1; splits <= 8 && splits <= all; splits *= 2) {
+            const double tiles = (double)((n + k.tile - 1) / k.tile) * ((P + k.tile - 1) / k.tile) * splits;
+            double rounds = tiles / k.slots;
+            if (k.tile == 64) rounds = rounds < 0.25 ? 0.75 : rounds + 0.5;
+            else rounds = ceil(rounds);
+            double t = rounds * k.work * (f32 ? k.cost32 : k.cost16) *
+                       ((all + splits - 1) / splits + (f32 ? k.edge32 : k.edge16));
+            if (splits > 1) t += (6 + (double)splits * n * P * 8 / 4e6) / us;
+            if (least == 0 || t < least) {
+                least = t;
+                best = MainShape{k.tile, splits};
+            }
+        }
+    return best;
+}
+
+}  // namespace
+
 AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward) {
     AdapterShape L{};
     const int ks = type == kF32 ? 16 : 32;
@@ -1182,6 +1349,8 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
         o += up(b);
         return at;
     };
+    L.main = main_shape(n, backward ? dout : di, backward ? di : dout, type);
+    L.off_split = take(!L.few && L.main.splits > 1 ? (size_t)L.main.splits * n * (backward ? di : dout) * 4 : 0);
     L.off_s = take(L.few ? (size_t)n * r * 4 : (size_t)n * L.rp * row_type_bytes(type));
     if (backward) {
         // Chunks long enough that their float32 sums are a small part of the
