@@ -89,10 +89,11 @@ __device__ __forceinline__ u32x4 only_if(bool in, u32x4 v) {
     for (int i = 0; i < 4; ++i) o[i] = in ? v[i] : 0u;
     return o;
 }
-// The same for rows that can be read 16 bytes at a time (K a multiple of E).
+// The same for rows that can be read 16 bytes at a time (K a multiple of E):
+// past the end the zero bytes are read, so that nothing waits for the load.
 template <class T>
-__device__ __forceinline__ u32x4 chunk_aligned(const T* row, int64_t k0, int64_t K) {
-    return only_if(k0 < K, *reinterpret_cast<const u32x4*>(row + (k0 < K ? k0 : 0)));
+__device__ __forceinline__ u32x4 chunk_aligned(const T* row, int64_t k0, int64_t K, bool in = true) {
+    return *(in && k0 < K ? reinterpret_cast<const u32x4*>(row + k0) : reinterpret_cast<const u32x4*>(ad_zero));
 }
 template <class T>
 __device__ __forceinline__ u32x4 chunk(const T* row, int64_t k0, int64_t K, bool aligned) {
@@ -236,7 +237,7 @@ struct InnerArgs {
     int32_t K, r, rp, u16, q16, h4;   // u16 / q16: rows of U / Q can be read 16 bytes at a time; h4: H written by fours
 };
 
-template <class T, int RF, bool TR, bool AL>
+template <class T, int RF, bool TR, bool AL, bool QAL>
 __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
     constexpr int E = Mma<T>::E, KS = 4 * E, VPR = RF * 16 / E;
     constexpr int UN = RF <= 2 ? 4 : RF == 4 ? 2 : 1;   // steps of a wave in flight
@@ -276,10 +277,12 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
                     for (int y = 0; y < NQ; ++y) {
                         const int z = y * 64 + lane, kk = z / VPR;
                         const int64_t k = (int64_t)(s + x) * KS + kk;
-                        const T* src = q + (k < A.K ? k : 0) * A.r;
-                        v[x][y] = only_if(k < A.K, AL && A.q16 ? chunk_aligned(src, z % VPR * E, A.r)
-                                                               : chunk_guarded(src, z % VPR * E, A.r));
+                        if constexpr (QAL)
+                            v[x][y] = chunk_aligned(q + k * A.r, z % VPR * E, A.r, k < A.K);
+                        else
+                            v[x][y] = only_if(k < A.K, chunk_guarded(q + (k < A.K ? k : 0) * A.r, z % VPR * E, A.r));
                     }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int x = 0; x < UN; ++x)
 #pragma unroll
@@ -306,8 +309,9 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
                         const int rr = j * 16 + li;   // rows past r give results that are not kept
                         const T* src = q + (int64_t)(rr < A.r ? rr : 0) * A.K;
                         const int64_t k0 = (int64_t)(s + x) * KS + g * E;
-                        a[x][j] = AL ? chunk_aligned(src, k0, A.K) : chunk_guarded(src, k0, A.K);
+                        a[x][j] = QAL ? chunk_aligned(src, k0, A.K) : chunk_guarded(src, k0, A.K);
                     }
+                __builtin_amdgcn_sched_barrier(0);   // all of them are issued before the first is waited for
 #pragma unroll
                 for (int x = 0; x < UN; ++x)
 #pragma unroll
@@ -799,15 +803,15 @@ __global__ __launch_bounds__(256) void k_ad_few_inner_t(FewArgs A, ListArgs L) {
     }
 }
 
-// y: 16 columns a block, its 8 waves share the contraction; RF x 16 places.
+// y: 16 columns a block, its 16 waves share the contraction; RF x 16 places.
 template <class T, int RF, bool AL>
-__global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
-    constexpr int E = Mma<T>::E, KS = 4 * E, UN = 4;
-    __shared__ f32x4 s_red[8][RF][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
+__global__ __launch_bounds__(1024) void k_ad_few_main(FewArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, UN = AL ? 4 : 1, NWAVE = 16;
+    __shared__ f32x4 s_red[NWAVE / 2][RF][64];
+    const int lane = threadIdx.x & 63, g = lane >> 4, li = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t col0 = (int64_t)blockIdx.x * 16;
-    const int64_t col = col0 + li < A.P ? col0 + li : A.P - 1;
-    const T* w = static_cast<const T*>(A.W) + col * A.K;
+    const T* w = static_cast<const T*>(A.W) + (col0 + li < A.P ? col0 + li : A.P - 1) * A.K;   // columns past P: not stored
     const T* x[RF];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
@@ -818,7 +822,7 @@ __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
 #pragma unroll
     for (int f = 0; f < RF; ++f) acc[f] = f32x4{0, 0, 0, 0};
     const int steps = (A.K + KS - 1) / KS;
-    for (int s = wave * UN; s < steps; s += 8 * UN) {   // steps past the last are of zeros
+    for (int s = wave * UN; s < steps; s += NWAVE * UN) {   // steps past the last are of zeros
         u32x4 a[UN], b[UN][RF];
 #pragma unroll
         for (int y = 0; y < UN; ++y) {
@@ -827,31 +831,50 @@ __global__ __launch_bounds__(512) void k_ad_few_main(FewArgs A) {
 #pragma unroll
             for (int f = 0; f < RF; ++f) b[y][f] = AL ? chunk_aligned(x[f], k0, A.K) : chunk_guarded(x[f], k0, A.K);
         }
+        __builtin_amdgcn_sched_barrier(0);   // all of them are issued before the first is waited for
 #pragma unroll
         for (int y = 0; y < UN; ++y)
 #pragma unroll
             for (int f = 0; f < RF; ++f) acc[f] = Mma<T>::mma(a[y], b[y][f], acc[f]);
     }
+    // The waves' sums: the upper half's to the lower half, then in order.
+    constexpr int H = NWAVE / 2;
+    if (wave >= H)
 #pragma unroll
-    for (int f = 0; f < RF; ++f) s_red[wave][f][lane] = acc[f];
+        for (int q = 0; q < RF; ++q) s_red[wave - H][q][lane] = acc[q];
     __syncthreads();
-    for (int f = wave; f < RF; f += 8) {
-        const int p = f * 16 + li;
+    if (wave < H)
+#pragma unroll
+        for (int q = 0; q < RF; ++q) s_red[wave][q][lane] += acc[q];
+    __syncthreads();
+    for (int q = wave; q < RF; q += NWAVE) {
+        const int p = q * 16 + li;
         if (p >= A.n) continue;
         f32x4 v{0, 0, 0, 0};
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v += s_red[q][f][lane];
+        for (int y = 0; y < H; ++y) v += s_red[y][q][lane];
         const int c = A.cl[p];
         const int64_t o0 = col0 + g * 4;
         if ((unsigned)c < (unsigned)A.k) {
             const float* s = static_cast<const float*>(A.S) + (int64_t)p * A.r;
+            const T* b[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (o0 + i >= A.P) continue;
-                const T* b = static_cast<const T*>(A.B) + ((int64_t)c * A.P + o0 + i) * A.r;
-                float d = 0.0f;
-                for (int j = 0; j < A.r; ++j) d = fmaf(s[j], to_f32(b[j]), d);
-                v[i] += d;
+            for (int i = 0; i < 4; ++i)
+                b[i] = static_cast<const T*>(A.B) + ((int64_t)c * A.P + (o0 + i < A.P ? o0 + i : 0)) * A.r;
+            if (A.q16) {
+                for (int j = 0; j < A.r; j += E) {
+                    Vec<T, E> t[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[i] = *reinterpret_cast<const Vec<T, E>*>(b[i] + j);
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = fmaf(s[j + e], to_f32(t[i].e[e]), v[i]);
+                }
+            } else {
+                for (int j = 0; j < A.r; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = fmaf(s[j], to_f32(b[i][j]), v[i]);
             }
         }
         store4(static_cast<T*>(A.Y) + row_of(A.order, p) * A.P, o0, A.P, v, A.y4);
@@ -1039,8 +1062,9 @@ hipError_t inner_go(const InnerArgs& A, const ListArgs& L, hipStream_t s) {
     const int rf = (A.r + 15) / 16;
     auto go = [&](auto j) {
         constexpr int RF = decltype(j)::value;
-        if (A.u16) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true>), g, b, 0, s, A, L);
-        else hipLaunchKernelGGL((k_ad_inner<T, RF, TR, false>), g, b, 0, s, A, L);
+        if (A.u16 && A.q16) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true, true>), g, b, 0, s, A, L);
+        else if (A.u16 && TR) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true, false>), g, b, 0, s, A, L);
+        else hipLaunchKernelGGL((k_ad_inner<T, RF, TR, false, false>), g, b, 0, s, A, L);
     };
     by_rank(rf, go);
     return hipGetLastError();
@@ -1151,6 +1175,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         F.x16 = x16;
         F.y4 = y4;
         F.rp = L.rp;
+        F.q16 = M.q16;
         if (!L.few) {
             hipLaunchKernelGGL((k_ad_few_inner<T, true>), dim3((unsigned)((D.n * L.rp + 3) / 4)), dim3(256), 0, s, F);
             if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -1158,9 +1183,9 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         }
         hipLaunchKernelGGL((k_ad_few_inner<T, false>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        const dim3 g((unsigned)((D.dout + 15) / 16)), b(512);
         auto go = [&](auto f) {
             constexpr int RF = decltype(f)::value;
+            const dim3 g((unsigned)((D.dout + 15) / 16)), b(1024);
             if (x16) hipLaunchKernelGGL((k_ad_few_main<T, RF, true>), g, b, 0, s, F);
             else hipLaunchKernelGGL((k_ad_few_main<T, RF, false>), g, b, 0, s, F);
         };
@@ -1184,7 +1209,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     I.K = D.di;
     I.r = D.r;
     I.rp = L.rp;
-    I.u16 = x16;
+    I.u16 = I.q16 = x16;
     I.h4 = D.r % 4 == 0 && a16(D.H);
     if ((e = inner_go<T, false>(I, ListArgs{}, s)) != hipSuccess) return e;
     return main_go<T, false>(M, L.main, x16, s);

@@ -55,22 +55,26 @@ def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None, n: Op
         raise ValueError("%s must have %d rows, got %d" % (name, n, rows))
     if d is not None and cols != d:
         raise ValueError("%s must have %d columns, got %d" % (name, d, cols))
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError("%s must have contiguous rows (last stride 1)" % name)
-    ld = t.stride(0) if rows > 1 else cols
+    if rows <= 1:
+        return cols
     if ld < cols:
         raise ValueError("%s must have rows that do not overlap" % name)
     return ld
 
 
 def _array(t: torch.Tensor, name: str, dtype: torch.dtype, shape: Tuple[int, ...], device: torch.device) -> None:
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device \
+            and t.is_contiguous():
+        return
     _gpu(t, name, device)
     if t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if tuple(t.shape) != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    raise ValueError("%s must be contiguous" % name)
 
 
 def _p(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -82,26 +86,27 @@ class _On:
     on that stream, and inputs made on another one are kept until it has
     used them."""
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], *inputs: Optional[torch.Tensor]):
-        self.device = device
-        self.inputs = inputs
-        self.stream = stream
-        if stream is not None and stream.device != device:
-            raise ValueError("stream is on %s, the tensors on %s" % (stream.device, device))
-        self.ctx = None
+    __slots__ = ("device", "stream", "inputs", "ctx")
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream],
+                 inputs: Tuple[Optional[torch.Tensor], ...]):
+        self.device, self.stream, self.inputs, self.ctx = device, stream, inputs, None
 
     def __enter__(self) -> int:
         if self.stream is not None:
+            if self.stream.device != self.device:
+                raise ValueError("stream is on %s, the tensors on %s" % (self.stream.device, self.device))
             self.ctx = torch.cuda.stream(self.stream)
             self.ctx.__enter__()
             for t in self.inputs:
                 if t is not None:
                     t.record_stream(self.stream)
             return self.stream.cuda_stream
-        if torch.cuda.current_device() != self.device.index:
-            self.ctx = torch.cuda.device(self.device)
+        index = self.device.index
+        if torch.cuda.current_device() != index:
+            self.ctx = torch.cuda.device(index)
             self.ctx.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return torch.cuda.current_stream(index).cuda_stream
 
     def __exit__(self, *exc) -> None:
         if self.ctx is not None:
@@ -156,11 +161,10 @@ def cluster_sort(ids: torch.Tensor, k: int, stream: Optional[torch.cuda.Stream] 
     lib = N.load()
     if not 1 <= k < 2 ** 31 - 1 or n * m >= 2 ** 31:
         raise N.KMError(N.KM_ERR_INVALID_ARG, "kmeans_sort_plan", "1 <= k < 2^31 - 1 and n m < 2^31 needed")
-    with _On(dev, stream, ids) as s:
-        order = torch.empty(n * m, dtype=torch.int32, device=dev)
-        pos = torch.empty_like(ids)
-        sorted_ids = torch.empty(n * m, dtype=torch.int32, device=dev)
-        offsets = torch.empty(k + 1, dtype=torch.int32, device=dev)
+    with _On(dev, stream, (ids,)) as s:
+        # The plan is one allocation: the workspace may be let go, the views share their memory.
+        order, pos, sorted_ids, offsets = ids.new_empty(3 * n * m + k + 1).split((n * m, n * m, n * m, k + 1))
+        pos = pos.view(ids.shape)
         ws = _workspace(lib.kmeans_sort_workspace_bytes(n, m, k), dev, "kmeans_sort_workspace_bytes")
         st = lib.kmeans_sort_plan(_p(ids), n, m, k, _p(order), _p(pos), _p(sorted_ids), _p(offsets), _p(ws),
                                   ws.numel(), s)
@@ -182,8 +186,8 @@ def cluster_gather(X: torch.Tensor, plan: ClusterPlan, stream: Optional[torch.cu
     ld = _rows(X, "X", n=plan.n if isinstance(plan, ClusterPlan) else None)
     _plan(plan, X.device)
     d = X.shape[1]
-    with _On(X.device, stream, X, plan.pos, plan.offsets) as s:
-        out = torch.empty(plan.n * plan.m, d, dtype=X.dtype, device=X.device)
+    with _On(X.device, stream, (X, plan.pos, plan.offsets)) as s:
+        out = X.new_empty((plan.n * plan.m, d))
         st = N.load().kmeans_sort_gather(_p(X), ld, plan.n, plan.m, plan.k, d, _TYPES[X.dtype], _p(plan.pos),
                                          _p(plan.offsets), _p(out), s)
     N.check(st, "kmeans_sort_gather")
@@ -200,8 +204,8 @@ def cluster_combine(Z: torch.Tensor, plan: ClusterPlan, weights: Optional[torch.
     if weights is not None:
         _array(weights, "weights", torch.float32, tuple(plan.pos.shape), Z.device)
     d = Z.shape[1]
-    with _On(Z.device, stream, Z, plan.pos, plan.offsets, weights) as s:
-        out = torch.empty(plan.n, d, dtype=Z.dtype, device=Z.device)
+    with _On(Z.device, stream, (Z, plan.pos, plan.offsets, weights)) as s:
+        out = Z.new_empty((plan.n, d))
         st = N.load().kmeans_sort_combine(_p(Z), ld, plan.n, plan.m, plan.k, d, _TYPES[Z.dtype], _p(plan.pos),
                                           _p(plan.offsets), _p(weights), _p(out), s)
     N.check(st, "kmeans_sort_combine")
@@ -218,8 +222,8 @@ def cluster_combine_backward(dY: torch.Tensor, Z: torch.Tensor, plan: ClusterPla
     d = dY.shape[1]
     ldz = _rows(Z, "Z", like=dY, n=plan.n * plan.m, d=d)
     _array(weights, "weights", torch.float32, tuple(plan.pos.shape), dY.device)
-    with _On(dY.device, stream, dY, Z, plan.pos, plan.offsets, weights) as s:
-        dz = torch.empty(plan.n * plan.m, d, dtype=dY.dtype, device=dY.device)
+    with _On(dY.device, stream, (dY, Z, plan.pos, plan.offsets, weights)) as s:
+        dz = dY.new_empty((plan.n * plan.m, d))
         dw = torch.empty_like(weights)
         st = N.load().kmeans_sort_combine_backward(_p(dY), ld, _p(Z), ldz, plan.n, plan.m, plan.k, d,
                                                    _TYPES[dY.dtype], _p(plan.pos), _p(plan.offsets), _p(weights),
@@ -248,10 +252,9 @@ def layernorm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opti
     ld = _rows(X, "X")
     f32 = _params(X, weight=weight, bias=bias)
     n, d = X.shape
-    with _On(X.device, stream, X, weight, bias) as s:
-        y = torch.empty(n, d, dtype=X.dtype, device=X.device)
-        mean = torch.empty(n, dtype=torch.float32, device=X.device)
-        rstd = torch.empty(n, dtype=torch.float32, device=X.device)
+    with _On(X.device, stream, (X, weight, bias)) as s:
+        y = X.new_empty((n, d))
+        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=X.device).unbind()
         st = N.load().kmeans_norm_forward(_p(X), ld, n, d, _TYPES[X.dtype], _p(weight), _p(bias), f32, float(eps),
                                           _p(y), _p(mean), _p(rstd), s)
     N.check(st, "kmeans_norm_forward")
@@ -270,10 +273,9 @@ def layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rs
     _array(mean, "mean", torch.float32, (n,), X.device)
     _array(rstd, "rstd", torch.float32, (n,), X.device)
     lib = N.load()
-    with _On(X.device, stream, dY, X, mean, rstd, weight) as s:
-        dx = torch.empty(n, d, dtype=X.dtype, device=X.device)
-        dg = torch.empty(d, dtype=torch.float32, device=X.device)
-        db = torch.empty(d, dtype=torch.float32, device=X.device)
+    with _On(X.device, stream, (dY, X, mean, rstd, weight)) as s:
+        dx = X.new_empty((n, d))
+        dg, db = torch.empty((2, d), dtype=torch.float32, device=X.device).unbind()
         ws = _workspace(lib.kmeans_norm_workspace_bytes(n, d, _TYPES[X.dtype]), X.device,
                         "kmeans_norm_workspace_bytes")
         st = lib.kmeans_norm_backward(_p(dY), ldy, _p(X), ld, n, d, _TYPES[X.dtype], _p(mean), _p(rstd),
@@ -286,10 +288,10 @@ def _adapters(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor
               scale: Optional[torch.Tensor]) -> Tuple[int, int, int, int]:
     """Check the weights of an adapter projection; (din, dout, k, r)."""
     for t, name, dims in ((W, "W", 2), (A, "A", 3), (B, "B", 3)):
-        _gpu(t, name, X.device)
-        if t.dim() != dims or 0 in t.shape:
+        if not isinstance(t, torch.Tensor) or t.dim() != dims or t.numel() == 0:
+            _gpu(t, name, X.device)
             raise ValueError("%s must be a non-empty %d-D tensor" % (name, dims))
-    (dout, din), (k, r) = W.shape, A.shape[:2]
+    (dout, din), (k, r, _) = W.shape, A.shape
     if X.shape[1] != din:
         raise ValueError("X must have %d columns" % din)
     _array(W, "W", X.dtype, (dout, din), X.device)
@@ -341,9 +343,8 @@ def adapter_linear(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
     need = lib.kmeans_adapter_workspace_bytes(n, din, dout, k, r, _TYPES[X.dtype], 0)
     if need == 0 and r > 128:
         raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_adapter_forward", "adapters have a rank of at most 128")
-    with _On(dev, stream, X, W, A, B, ids, order, sids, offsets, scale) as s:
-        y = torch.empty(n, dout, dtype=X.dtype, device=dev)
-        h = torch.empty(n, r, dtype=X.dtype, device=dev)
+    with _On(dev, stream, (X, W, A, B, ids, order, sids, offsets, scale)) as s:
+        y, h = X.new_empty((n, dout)), X.new_empty((n, r))
         ws = _workspace(need, dev, "kmeans_adapter_workspace_bytes")
         st = lib.kmeans_adapter_forward(_p(X), ld, n, din, dout, k, r, _TYPES[X.dtype], _p(W), _p(A), _p(B),
                                         _p(scale), _p(ids), _p(order), _p(sids), _p(offsets), _p(y), _p(h),
@@ -368,8 +369,8 @@ def adapter_linear_backward(dY: torch.Tensor, X: torch.Tensor, H: torch.Tensor, 
     need = lib.kmeans_adapter_workspace_bytes(n, din, dout, k, r, _TYPES[X.dtype], 1)
     if need == 0 and r > 128:
         raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_adapter_backward", "adapters have a rank of at most 128")
-    with _On(dev, stream, dY, X, H, W, A, B, order, plan.sorted_ids, plan.offsets, scale) as s:
-        dx = torch.empty(n, din, dtype=X.dtype, device=dev)
+    with _On(dev, stream, (dY, X, H, W, A, B, order, plan.sorted_ids, plan.offsets, scale)) as s:
+        dx = X.new_empty((n, din))
         da, db = torch.empty_like(A), torch.empty_like(B)
         ws = _workspace(need, dev, "kmeans_adapter_workspace_bytes")
         st = lib.kmeans_adapter_backward(_p(dY), ldy, _p(X), ld, _p(H), n, din, dout, k, r, _TYPES[X.dtype], _p(W),
