@@ -358,7 +358,7 @@ struct MainArgs {
     const int32_t *order, *sids, *offsets;
     void* Y;
     int64_t n;
-    int32_t K, P, r, rp, q16, y4;
+    int32_t K, P, r, rp, q16, y4, y16;   // y4 / y16: Y can be written 4 elements / 16 bytes at a time
     int32_t tm, tn;   // tiles
     int32_t splits;   // parts of the contraction, a block each; more than one: sums to part
     float* part;      // splits x n x P, by place
@@ -615,9 +615,22 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             }
         }
     };
-    // The adapters' term belongs to the first part of the contraction.
-    const int c_first = w0 < A.n && split == 0 ? __builtin_amdgcn_readfirstlane(s_ids[w0 - bm]) : -1;
+    // The adapters' term belongs to the first part of the contraction.  The
+    // wave's first two clusters (its places are in cluster order, -1 last):
+    constexpr int RM = TM / WR;
+    int c_first = -1, c_second = -1;
+    if (w0 < A.n && split == 0) {
+        const int* ids = s_ids + (w0 - bm);
+        c_first = __builtin_amdgcn_readfirstlane(ids[0]);
+#pragma unroll
+        for (int i = (RM + 63) / 64 - 1; i >= 0; --i) {
+            const int at = i * 64 + lane, id = at < RM && w0 + at < A.n ? ids[at] : -1;
+            const uint64_t m = __ballot(id > c_first);
+            if (m) c_second = __builtin_amdgcn_readlane(id, __builtin_ctzll(m));
+        }
+    }
     if (c_first >= 0) fetch(c_first, 0, 0);
+    if (c_second >= 0) fetch(c_second, 0, 1);
     stage(kt, true);
 
     // The adapters' term, cluster by cluster of the wave's places (they are in
@@ -636,11 +649,16 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         }
         return next;
     };
-    for (int k0 = 0; c_first >= 0 && k0 < A.rp; k0 += KS) {
-        int buf = 0;
-        if (k0 > 0) fetch(c_first, k0, 0);
-        for (int c = c_first; c >= 0; buf ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the wave's own part of LDS
+    for (int k0 = 0; c_first >= 0 && k0 < A.r; k0 += KS) {
+        if (k0 > 0) {
+            fetch(c_first, k0, 0);
+            if (c_second >= 0) fetch(c_second, k0, 1);
+        }
+        int buf = 0, c = c_first, next = c_second;
+        while (c >= 0) {
+            // This cluster's operand is in the wave's own part of LDS; the next one's may be on its way.
+            if (next >= 0 && A.q16) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(CN * 4 / 64) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             u32x4 a[FC];
 #pragma unroll
             for (int h = 0; h < FC; ++h) {
@@ -650,8 +668,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
                 else
                     a[h] = *reinterpret_cast<const u32x4*>(q + ((h * 16 + li) * 4 + swz4(li, g)) * 16);
             }
-            const int next = after(c);
-            if (next >= 0) fetch(next, k0, buf ^ 1);
+            const int after_next = next >= 0 ? after(next) : -1;
+            if (after_next >= 0) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is overwritten
+                fetch(after_next, k0, buf);
+            }
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
                 const bool is = mine[f] == c;
@@ -668,9 +689,40 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
                 }
             }
             c = next;
+            next = after_next;
+            buf ^= 1;
         }
     }
 
+    // 16-bit results go through LDS so that whole 128-byte lines are written
+    // (a lane holds 8 bytes of a row): 8 rows an instruction.
+    if constexpr (sizeof(T) == 2 && CN == 64) {
+        static_assert(RM * 128 * WR * WC <= NS * kStage, "");
+        if (A.splits == 1 && A.y16) {   // the same for the whole grid
+            __syncthreads();            // every wave is done with the stages and operands
+            char* own = s_tiles + wave * (RM * 128);
+#pragma unroll
+            for (int f = 0; f < FR; ++f)
+#pragma unroll
+                for (int h = 0; h < FC; ++h) {
+                    Vec<T, 4> o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o.e[i] = from_f32<T>(acc[f][h][i]);
+                    const int row = f * 16 + li, ch = h * 2 + (g >> 1);
+                    *reinterpret_cast<Vec<T, 4>*>(own + row * 128 + ((ch ^ (row & 7)) * 16) + (g & 1) * 8) = o;
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            const int64_t col = cb + lane % 8 * 8;
+#pragma unroll
+            for (int i = 0; i < RM / 8; ++i) {
+                const int row = i * 8 + lane / 8;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(own + row * 128 + ((lane % 8) ^ (row & 7)) * 16);
+                if (w0 + row < A.n && col < A.P)
+                    *reinterpret_cast<u32x4*>(static_cast<T*>(A.Y) + (int64_t)s_rows[w0 - bm + row] * A.P + col) = v;
+            }
+            return;
+        }
+    }
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
         const int64_t place = w0 + f * 16 + li;
@@ -1152,6 +1204,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     M.rp = L.rp;
     M.q16 = D.r % E == 0 && a16(D.B);
     M.y4 = y4;
+    M.y16 = D.dout % E == 0 && a16(D.Y);
     M.splits = L.main.splits;
     M.part = reinterpret_cast<float*>(ws + L.off_split);
     if (L.few || D.n <= kFewInner) {
@@ -1281,6 +1334,7 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.r = D.r;
         M.rp = L.rp;
         M.y4 = D.di % 4 == 0 && a16(D.dX);
+    M.y16 = D.di % E == 0 && a16(D.dX);
     M.q16 = D.di % E == 0 && a16(D.A);
         M.splits = L.main.splits;
         M.part = reinterpret_cast<float*>(ws + L.off_split);
