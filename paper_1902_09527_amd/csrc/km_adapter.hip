@@ -360,6 +360,7 @@ struct MainArgs {
     int64_t n;
     int32_t K, P, r, rp, q16, y4, y16;   // y4 / y16: Y can be written 4 elements / 16 bytes at a time
     int32_t tm, tn;   // tiles
+    int64_t ldw;      // row stride of W
     int32_t splits;   // parts of the contraction, a block each; more than one: sums to part
     float* part;      // splits x n x P, by place
 };
@@ -416,11 +417,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         const int q = i * NT + tid;
         if constexpr (TR) {
             const int kk = q / CPR;
-            wp[i] = static_cast<const T*>(A.W) + ((int64_t)k_first * BK + kk) * A.P + bn + swz_tr<T, CPR>(kk, q % CPR) * E;
+            wp[i] = static_cast<const T*>(A.W) + ((int64_t)k_first * BK + kk) * A.ldw + bn + swz_tr<T, CPR>(kk, q % CPR) * E;
         } else {
             int64_t col = bn + q / 8;
             if (col >= A.P) col = A.P - 1;   // not stored
-            wp[i] = static_cast<const T*>(A.W) + col * A.K + uc + (int64_t)k_first * BK;
+            wp[i] = static_cast<const T*>(A.W) + col * A.ldw + uc + (int64_t)k_first * BK;
         }
     }
     // Stages (of this block) without a chunk past the contraction's end or the last column.
@@ -448,11 +449,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             if constexpr (AL) {
                 const bool in = !guard || (kt * BK + kk < k_left && col < A.P);
                 load_lds16(in ? (const void*)wp[i] : (const void*)ad_zero, wb + (i * NT + wave * 64) * 16);
-                wp[i] += (int64_t)BK * A.P;
+                wp[i] += BK * A.ldw;
             } else {
                 const int64_t k = (int64_t)(k_first + kt) * BK + kk;
                 *reinterpret_cast<u32x4*>(wb + q * 16) = only_if(
-                    k < A.K, chunk_guarded(static_cast<const T*>(A.W) + (k < A.K ? k : 0) * A.P, col, A.P));
+                    k < A.K, chunk_guarded(static_cast<const T*>(A.W) + (k < A.K ? k : 0) * A.ldw, col, A.P));
             }
         } else {
             if constexpr (AL) {
@@ -694,12 +695,13 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         }
     }
 
-    // 16-bit results go through LDS so that whole 128-byte lines are written
-    // (a lane holds 8 bytes of a row): 8 rows an instruction.
+    // 16-bit results go through LDS so that 128 consecutive bytes of a row are
+    // written at once (a lane holds 8): 8 rows an instruction, or one where rows
+    // are not 16-byte aligned.
     if constexpr (sizeof(T) == 2 && CN == 64) {
         static_assert(RM * 128 * WR * WC <= NS * kStage, "");
-        if (A.splits == 1 && A.y16) {   // the same for the whole grid
-            __syncthreads();            // every wave is done with the stages and operands
+        if (A.splits == 1) {    // the same for the whole grid
+            __syncthreads();    // every wave is done with the stages and operands
             char* own = s_tiles + wave * (RM * 128);
 #pragma unroll
             for (int f = 0; f < FR; ++f)
@@ -712,6 +714,13 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
                     *reinterpret_cast<Vec<T, 4>*>(own + row * 128 + ((ch ^ (row & 7)) * 16) + (g & 1) * 8) = o;
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (!A.y16) {
+                for (int row = 0; row < RM && w0 + row < A.n; ++row)
+                    if (cb + lane < A.P)
+                        static_cast<T*>(A.Y)[(int64_t)s_rows[w0 - bm + row] * A.P + cb + lane] =
+                            *reinterpret_cast<const T*>(own + row * 128 + ((lane >> 3) ^ (row & 7)) * 16 + (lane & 7) * 2);
+                return;
+            }
             const int64_t col = cb + lane % 8 * 8;
 #pragma unroll
             for (int i = 0; i < RM / 8; ++i) {
@@ -1096,7 +1105,26 @@ __global__ __launch_bounds__(256) void k_ad_join(GradArgs A, GradArgs B) {
 }
 
 // --------------------------------------------------------------------------
+// Rows of a width that is no multiple of 16 bytes, copied with zeros up to one:
+// the tiles' loads then move 16 bytes.  A thread a chunk.
+template <class T>
+__global__ __launch_bounds__(256) void k_ad_pad(const T* src, int64_t ld, int64_t rows, int32_t d, T* dst, int32_t dp) {
+    constexpr int E = Mma<T>::E;
+    const int64_t per = dp / E, total = rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256)
+        *reinterpret_cast<u32x4*>(dst + i * E) = chunk_guarded(src + i / per * ld, i % per * E, d);
+}
+
+// --------------------------------------------------------------------------
 // Launches
+
+template <class T>
+hipError_t pad_rows(const void* src, int64_t ld, int64_t rows, int32_t d, char* dst, int32_t dp, hipStream_t s) {
+    const int64_t blocks = (rows * (dp / Mma<T>::E) + 255) / 256;
+    hipLaunchKernelGGL((k_ad_pad<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s,
+                       static_cast<const T*>(src), ld, rows, d, reinterpret_cast<T*>(dst), dp);
+    return hipGetLastError();
+}
 
 // The operands' 16 x rf indexes of r: 1, 2, 4 or 8.
 template <class F>
@@ -1115,7 +1143,7 @@ hipError_t inner_go(const InnerArgs& A, const ListArgs& L, hipStream_t s) {
     auto go = [&](auto j) {
         constexpr int RF = decltype(j)::value;
         if (A.u16 && A.q16) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true, true>), g, b, 0, s, A, L);
-        else if (A.u16 && TR) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true, false>), g, b, 0, s, A, L);
+        else if (A.u16) hipLaunchKernelGGL((k_ad_inner<T, RF, TR, true, false>), g, b, 0, s, A, L);
         else hipLaunchKernelGGL((k_ad_inner<T, RF, TR, false, false>), g, b, 0, s, A, L);
     };
     by_rank(rf, go);
@@ -1191,6 +1219,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     M.U = D.X;
     M.ldu = D.ldx;
     M.W = D.W;
+    M.ldw = D.di;
     M.Q = D.B;
     M.S = ws + L.off_s;
     M.order = D.order;
@@ -1207,6 +1236,15 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     M.y16 = D.dout % E == 0 && a16(D.Y);
     M.splits = L.main.splits;
     M.part = reinterpret_cast<float*>(ws + L.off_split);
+    bool u16 = x16;
+    if (!L.few && L.pad_i != D.di) {
+        if ((e = pad_rows<T>(D.X, D.ldx, D.n, D.di, ws + L.off_x, L.pad_i, s)) != hipSuccess) return e;
+        if ((e = pad_rows<T>(D.W, D.di, D.dout, D.di, ws + L.off_w, L.pad_i, s)) != hipSuccess) return e;
+        M.U = ws + L.off_x;
+        M.W = ws + L.off_w;
+        M.ldu = M.ldw = L.pad_i;
+        u16 = true;
+    }
     if (L.few || D.n <= kFewInner) {
         FewArgs F{};
         F.X = D.X;
@@ -1232,7 +1270,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         if (!L.few) {
             hipLaunchKernelGGL((k_ad_few_inner<T, true>), dim3((unsigned)((D.n * L.rp + 3) / 4)), dim3(256), 0, s, F);
             if ((e = hipGetLastError()) != hipSuccess) return e;
-            return main_go<T, false>(M, L.main, x16, s);
+            return main_go<T, false>(M, L.main, u16, s);
         }
         hipLaunchKernelGGL((k_ad_few_inner<T, false>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
         if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -1249,8 +1287,8 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         return hipGetLastError();
     }
     InnerArgs I{};
-    I.U = D.X;
-    I.ldu = D.ldx;
+    I.U = M.U;
+    I.ldu = M.ldu;
     I.Q = D.A;
     I.order = D.order;
     I.sids = D.sids;
@@ -1262,18 +1300,36 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     I.K = D.di;
     I.r = D.r;
     I.rp = L.rp;
-    I.u16 = I.q16 = x16;
+    I.u16 = u16;
+    I.q16 = x16;
     I.h4 = D.r % 4 == 0 && a16(D.H);
     if ((e = inner_go<T, false>(I, ListArgs{}, s)) != hipSuccess) return e;
-    return main_go<T, false>(M, L.main, x16, s);
+    return main_go<T, false>(M, L.main, u16, s);
 }
 
 template <class T>
 hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipStream_t s) {
     constexpr int E = Mma<T>::E;
-    const bool dy16 = rows_vec16(D.dY, D.lddy, D.dout, sizeof(T)), x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T));
+    bool dy16 = rows_vec16(D.dY, D.lddy, D.dout, sizeof(T)), x16 = rows_vec16(D.X, D.ldx, D.di, sizeof(T));
+    bool w16 = D.di % E == 0 && a16(D.W);
     hipError_t e;
     char* S = ws + L.off_s;
+    const void *dY = D.dY, *X = D.X, *W = D.W;
+    int64_t lddy = D.lddy, ldx = D.ldx, ldw = D.di;
+    if (D.n > 0 && L.pad_o != D.dout) {
+        if ((e = pad_rows<T>(dY, lddy, D.n, D.dout, ws + L.off_y, L.pad_o, s)) != hipSuccess) return e;
+        dY = ws + L.off_y;
+        lddy = L.pad_o;
+        dy16 = true;
+    }
+    if (D.n > 0 && L.pad_i != D.di) {
+        if ((e = pad_rows<T>(X, ldx, D.n, D.di, ws + L.off_x, L.pad_i, s)) != hipSuccess) return e;
+        if ((e = pad_rows<T>(W, ldw, D.dout, D.di, ws + L.off_w, L.pad_i, s)) != hipSuccess) return e;
+        X = ws + L.off_x;
+        W = ws + L.off_w;
+        ldx = ldw = L.pad_i;
+        x16 = w16 = true;
+    }
     ListArgs Q{};
     Q.offsets = D.offsets;
     Q.k = D.k;
@@ -1283,8 +1339,8 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     Q.first = reinterpret_cast<int32_t*>(ws + L.off_first);
     Q.num = Q.first + D.k;
     InnerArgs I{};
-    I.U = D.dY;
-    I.ldu = D.lddy;
+    I.U = dY;
+    I.ldu = lddy;
     I.Q = D.B;
     I.order = D.order;
     I.sids = D.sids;
@@ -1299,8 +1355,8 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     I.q16 = D.r % E == 0 && a16(D.B);
     if (D.n <= kFewInner) {
         FewArgs F{};
-        F.X = D.dY;
-        F.ldx = D.lddy;
+        F.X = dY;
+        F.ldx = lddy;
         F.B = D.B;
         F.order = D.order;
         F.cl = D.sids;
@@ -1319,9 +1375,10 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     }
     if (D.n > 0) {
         MainArgs M{};
-        M.U = D.dY;
-        M.ldu = D.lddy;
-        M.W = D.W;
+        M.U = dY;
+        M.ldu = lddy;
+        M.W = W;
+        M.ldw = ldw;
         M.Q = D.A;
         M.S = S;
         M.order = D.order;
@@ -1334,11 +1391,11 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.r = D.r;
         M.rp = L.rp;
         M.y4 = D.di % 4 == 0 && a16(D.dX);
-    M.y16 = D.di % E == 0 && a16(D.dX);
-    M.q16 = D.di % E == 0 && a16(D.A);
+        M.y16 = D.di % E == 0 && a16(D.dX);
+        M.q16 = D.di % E == 0 && a16(D.A);
         M.splits = L.main.splits;
         M.part = reinterpret_cast<float*>(ws + L.off_split);
-        if ((e = main_go<T, true>(M, L.main, dy16 && D.di % E == 0 && a16(D.W), s)) != hipSuccess) return e;
+        if ((e = main_go<T, true>(M, L.main, dy16 && w16, s)) != hipSuccess) return e;
     }
     GradArgs G{};
     G.order = D.order;
@@ -1349,8 +1406,8 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     G.k = D.k;
     G.r = D.r;
     G.part = reinterpret_cast<float*>(ws + L.off_part);
-    G.U = D.X;
-    G.ldu = D.ldx;
+    G.U = X;
+    G.ldu = ldx;
     G.V = S;
     G.ldv = L.rp;
     G.v16 = 1;
@@ -1359,8 +1416,8 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     G.tiles = (D.di + 127) / 128;
     G.o4 = D.di % 4 == 0 && a16(D.dA);
     GradArgs B = G;
-    B.U = D.dY;
-    B.ldu = D.lddy;
+    B.U = dY;
+    B.ldu = lddy;
     B.V = D.H;
     B.ldv = D.r;
     B.v_by_row = 1;
@@ -1430,6 +1487,15 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
     };
     L.main = main_shape(n, backward ? dout : di, backward ? di : dout, type);
     L.off_split = take(!L.few && L.main.splits > 1 ? (size_t)L.main.splits * n * (backward ? di : dout) * 4 : 0);
+    // Copies of rows whose width is no multiple of 16 bytes (few rows are read as they are).
+    const int e = ks / 4;
+    const size_t es = row_type_bytes(type);
+    L.pad_i = (di + e - 1) / e * e;
+    L.pad_o = (dout + e - 1) / e * e;
+    const bool ci = !L.few && L.pad_i != di, co = backward && L.pad_o != dout;
+    L.off_x = take(ci ? (size_t)n * L.pad_i * es : 0);
+    L.off_w = take(ci ? (size_t)dout * L.pad_i * es : 0);
+    L.off_y = take(co ? (size_t)n * L.pad_o * es : 0);
     L.off_s = take(L.few ? (size_t)n * r * 4 : (size_t)n * L.rp * row_type_bytes(type));
     if (backward) {
         // Chunks long enough that their float32 sums are a small part of the
