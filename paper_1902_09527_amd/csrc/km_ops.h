@@ -72,7 +72,7 @@ int ops_check_range(const void* p, size_t bytes, int device, const char* what);
 // ---- rows sorted by cluster and back (km_sort.hip)
 
 constexpr int64_t kSortRankMax = 1024;   // slots up to which one block ranks them by comparing
-constexpr int kSortBins = 1024;          // most digit values of a counting pass
+constexpr int kSortBins = 4096;          // most digit values of a counting pass
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
 

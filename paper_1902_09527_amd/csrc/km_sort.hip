@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = P.bins;
     const int64_t share = (P.tiles + 7) / 8, tile = blockIdx.x % 8 * share + blockIdx.x / 8;
     if (tile >= P.tiles) return;   // the grid is 8 share blocks
-    // The tile's prefixes and the totals, 2 values a thread.
+    // The tile's prefixes and the totals, kPer values a thread.
     constexpr int kPer = kSortBins / kSortThreads;
     uint32_t v[kPer], before[kPer], own = 0;
 #pragma unroll
@@ -278,6 +278,18 @@ hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hip
         P.last = q == S.passes - 1;
         const dim3 g((unsigned)S.tiles), g8((unsigned)((S.tiles + 7) / 8 * 8)), t(kSortThreads);
         const size_t lds = (size_t)kSortWaves * P.bins * 4;
+        if (lds > 60 * 1024) {   // beyond what a kernel has without asking
+            hipError_t e = hipSuccess;
+            auto raise = [&](auto* kernel) {
+                e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                        kSortWaves * kSortBins * 4);
+            };
+            if (S.rounds == 2) raise(k_sort_scatter<2>);
+            else if (S.rounds == 4) raise(k_sort_scatter<4>);
+            else if (S.rounds == 8) raise(k_sort_scatter<8>);
+            else raise(k_sort_scatter<16>);
+            if (e != hipSuccess) return e;
+        }
 #define KM_SORT(K, G, LDS)                                                                 \
     do {                                                                                 \
         if (S.rounds == 2) hipLaunchKernelGGL((K<2>), G, t, LDS, s, A, P);               \

@@ -53,6 +53,13 @@ def test_plan(n, m, k):
         _check_plan(_ids(rng, n, m, k, empty), k)
 
 
+@pytest.mark.parametrize("k", [2047, 4094, 4095, 4096, 4097])
+@pytest.mark.parametrize("n", [1025, 30_011, 300_007, 1_200_000])
+def test_plan_at_the_edge_of_one_pass(n, k):
+    rng = np.random.default_rng(n + k)
+    _check_plan(_ids(rng, n, 1, k, 0.05), k)
+
+
 @pytest.mark.parametrize("n", [1, 100, 5000])
 def test_plan_with_every_slot_empty_or_one_cluster(n):
     _check_plan(np.full((n, 2), -1, np.int32), 9)
