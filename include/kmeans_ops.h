@@ -17,7 +17,7 @@
  * DEVICE pointers on the current device; a pointer may be NULL where its
  * array is empty.  Rows are `d` contiguous elements, `ld` elements apart
  * (ld >= d) where an argument ld* is given, else d apart.  Outputs must not
- * overlap inputs.  Workspaces are the caller's: device memory of at least
+ * overlap inputs.  Rows have at most 2^28 elements.  Workspaces are the caller's: device memory of at least
  * the bytes that the *_workspace_bytes function gives, 256-byte aligned,
  * contents on entry of no matter, not to be used by another call until this
  * one's work completes.  Sums, statistics and gradients are formed in
@@ -118,8 +118,8 @@ int kmeans_norm_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
  *   or a plan of kmeans_sort_plan with n slots (ids is not read): sorted_ids,
  *          offsets and order (m = 1), or order = NULL for rows that are in
  *          the plan's order already (the output of kmeans_sort_gather).
- * Requires n >= 0, din, dout, k >= 1, 1 <= r <= 128 (else
- * KM_ERR_UNSUPPORTED), n < 2^31.  backward: the workspace of the backward
+ * Requires n >= 0, din, dout, k, r >= 1; KM_ERR_UNSUPPORTED beyond r = 128,
+ * n = 2^27 and din, dout = 2^24.  backward: the workspace of the backward
  * pass, else of the forward pass.
  */
 size_t kmeans_adapter_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type,

@@ -10,9 +10,11 @@ namespace {
 
 bool type_ok(int32_t t) { return t == KM_F32 || t == KM_BF16 || t == KM_F16; }
 
-// n rows of d elements, ld apart: sizes that stay within 63-bit byte offsets.
+// n rows of d elements, ld apart: sizes that stay within 63-bit byte offsets
+// (and widths within 32-bit column indexes).
+constexpr int64_t kMostColumns = (int64_t)1 << 28;
 bool rows_ok(int64_t n, int64_t d, int64_t ld) {
-    return n >= 0 && d >= 1 && ld >= d && (n == 0 || ld <= (INT64_MAX / 16) / n);
+    return n >= 0 && d >= 1 && d <= kMostColumns && ld >= d && (n == 0 || ld <= (INT64_MAX / 16) / n);
 }
 
 // Checks arrays against the current device; the first refusal is kept.
@@ -271,6 +273,8 @@ static AdapterPlan adapter_plan(int64_t n, int32_t k, size_t at) {
 static int adapter_sizes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type) {
     if (!slots_ok(n, 1, k) || din < 1 || dout < 1 || r < 1 || !type_ok(type))
         return bad("n, din, dout, k, r or type out of range");
+    if (n > (int64_t)1 << 27 || din > 1 << 24 || dout > 1 << 24)   // the kernels' grids and 32-bit stage counts
+        return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^27 rows or 2^24 columns");
     if (r > km::kAdapterMaxRank)
         return km::ops_error(KM_ERR_UNSUPPORTED, "adapters have a rank of at most %d", km::kAdapterMaxRank);
     if (!rows_ok(n, din, din) || !rows_ok(n, dout, dout) || !rows_ok(dout, din, din) ||

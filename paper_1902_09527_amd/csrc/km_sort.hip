@@ -21,6 +21,9 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Clusters up to which the one-block sort writes the offsets itself.
+constexpr int kSortRankOffsets = 1 << 16;
+
 __device__ __forceinline__ int key_of(int id, int k) { return (unsigned)id < (unsigned)k ? id : k; }
 
 // Up to kSortRankMax slots: the place of slot p is the number of slots with a
@@ -50,6 +53,7 @@ __global__ __launch_bounds__(kSortRankMax) void k_sort_rank(SortArgs A) {
         A.sorted_ids[place] = key < k ? key : -1;
     }
     __syncthreads();
+    if (k > kSortRankOffsets) return;   // k_sort_offsets, over the chip
     for (int64_t c = p; c <= k; c += blockDim.x) {   // offsets[c]: slots with a key below c
         int lo = 0, hi = N;
         while (lo < hi) {
@@ -216,7 +220,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(SortArgs A, Pass 
     }
 }
 
-// offsets after several passes: the first place whose key is not below c.
+// offsets after several passes, or of very many clusters: the first place
+// whose key is not below c.
 __global__ __launch_bounds__(256) void k_sort_offsets(SortArgs A) {
     for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c <= A.k; c += (int64_t)gridDim.x * 256) {
         int32_t lo = 0, hi = A.N;
@@ -226,6 +231,12 @@ __global__ __launch_bounds__(256) void k_sort_offsets(SortArgs A) {
         }
         A.offsets[c] = lo;
     }
+}
+
+hipError_t sort_offsets(const SortArgs& A, hipStream_t s) {
+    const int64_t b = ((int64_t)A.k + 256) / 256;
+    hipLaunchKernelGGL(k_sort_offsets, dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, A);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -258,7 +269,8 @@ hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hip
     if (S.passes == 0) {
         const int threads = A.N < 1 ? 64 : (A.N + 63) / 64 * 64;
         hipLaunchKernelGGL(k_sort_rank, dim3(1), dim3(threads), 0, s, A);
-        return hipGetLastError();
+        hipError_t e = hipGetLastError();
+        return e == hipSuccess && A.k > kSortRankOffsets ? sort_offsets(A, s) : e;
     }
     // Passes alternate between the workspace's order and A.order and end in A.order.
     int32_t* tmp = reinterpret_cast<int32_t*>(ws + S.off_idx);
@@ -305,11 +317,7 @@ hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hip
         if (e != hipSuccess) return e;
         in = P.out;
     }
-    if (S.passes > 1) {
-        const int64_t b = ((int64_t)A.k + 256) / 256;
-        hipLaunchKernelGGL(k_sort_offsets, dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, A);
-    }
-    return hipGetLastError();
+    return S.passes > 1 ? sort_offsets(A, s) : hipSuccess;
 }
 
 // --------------------------------------------------------------------------

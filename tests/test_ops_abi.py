@@ -70,6 +70,9 @@ def test_adapter_refusals():
     assert [fwd(X=None), fwd(ldx=63), fwd(n=-1), fwd(W=None), fwd(ids=None), fwd(ids=None, order=FAKE),
             fwd(ids=None, sids=FAKE), fwd(ws=None), fwd(wsb=size() - 1), fwd(ws=C.c_void_p(0x1010))] == [BAD] * 10
     assert fwd(r=129) == N.KM_ERR_UNSUPPORTED
+    assert fwd(n=2 ** 27 + 1) == N.KM_ERR_UNSUPPORTED
+    assert lib.kmeans_sort_workspace_bytes(1, 1, 1) > 0
+    assert lib.kmeans_norm_workspace_bytes(1, 2 ** 28 + 1, 0) == 0
 
     def bwd(dY=FAKE, H=FAKE, n=100, sids=FAKE, off=FAKE, dA=FAKE, wsb=size(b=1)):
         return lib.kmeans_adapter_backward(dY, 32, FAKE, 64, H, n, 64, 32, 4, 8, 1, FAKE, FAKE, FAKE, None, None, sids,
