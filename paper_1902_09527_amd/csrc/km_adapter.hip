@@ -168,6 +168,70 @@ __device__ __forceinline__ u32x4 read_tr(const char* tile, int k0, int at) {
     }
 }
 
+// The same for N operands (1, 2 or 4) at the places `at`, `k0` rows in, where
+// loads to LDS are on their way: the compiler would let the transposing read
+// wait for all of them (it cannot tell that they go elsewhere), so 16-bit
+// operands are read and waited for in one piece here.
+template <int OFF, int STEP>
+__device__ __forceinline__ void tr_wait(u32x4 (&v)[1], const uint32_t (&p)[1]) {
+    uint64_t x[2];
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\t"
+                 "ds_read_b64_tr_b16 %1, %2 offset:%4\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1])
+                 : "v"(p[0]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    struct Two { uint64_t a, b; };
+    v[0] = __builtin_bit_cast(u32x4, Two{x[0], x[1]});
+}
+template <int OFF, int STEP>
+__device__ __forceinline__ void tr_wait(u32x4 (&v)[2], const uint32_t (&p)[2]) {
+    uint64_t x[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                 "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+                 : "v"(p[0]), "v"(p[1]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    struct Two { uint64_t a, b; };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = __builtin_bit_cast(u32x4, Two{x[2 * i], x[2 * i + 1]});
+}
+template <int OFF, int STEP>
+__device__ __forceinline__ void tr_wait(u32x4 (&v)[4], const uint32_t (&p)[4]) {
+    uint64_t x[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+                   "=&v"(x[7])
+                 : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    struct Two { uint64_t a, b; };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(u32x4, Two{x[2 * i], x[2 * i + 1]});
+}
+template <class T, int CPR, int K0, int N>
+__device__ __forceinline__ void read_tr_wait(u32x4 (&v)[N], const char* tile, const int (&at)[N]) {
+    if constexpr (sizeof(T) == 2) {
+        uint32_t p[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = (uint32_t)(uintptr_t)(KM_LDS const char*)(tile + at[i]);
+        tr_wait<K0 * CPR * 16, 4 * CPR * 16>(v, p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = read_tr<T, CPR>(tile, K0, at[i]);
+    }
+}
+
 // --------------------------------------------------------------------------
 // Chunks of clusters, for the adapters' gradients.
 
@@ -499,15 +563,18 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     struct Frags {
         u32x4 b[FR], a[FC];
     };
-    // Operand i of half s of a stage: first the columns', then the rows'.
+    // Operand i of half s of a stage: first the columns' (TR: read_cols), then the rows'.
     auto read = [&](Frags& F, int i, const char* buf, int s) {
         if (i < FC) {
-            if constexpr (TR)
-                F.a[i] = read_tr<T, CPR>(buf, s * KS, wa[i]);
-            else
-                F.a[i] = *reinterpret_cast<const u32x4*>(buf + (wa[0] ^ (s * 64)) + i * 2048);
+            if constexpr (!TR) F.a[i] = *reinterpret_cast<const u32x4*>(buf + (wa[0] ^ (s * 64)) + i * 2048);
         } else {
             F.b[i - FC] = *reinterpret_cast<const u32x4*>(buf + (ua ^ (s * 64)) + (i - FC) * 2048);
+        }
+    };
+    auto read_cols = [&](Frags& F, const char* buf, int s) {
+        if constexpr (TR) {
+            if (s == 0) read_tr_wait<T, CPR, 0>(F.a, buf, wa);
+            else read_tr_wait<T, CPR, KS>(F.a, buf, wa);
         }
     };
 
@@ -534,6 +601,10 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
 #pragma unroll
                 for (int h = 0; h < FC; ++h) acc[f][h] = Mma<T>::mma(F.a[h], F.b[f], acc[f][h]);
             __builtin_amdgcn_sched_barrier(0);
+            if (TR && q == 0) {   // while the first products are at work
+                read_cols(F2, buf2, s2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     // This wave's operands have arrived (F2 of the half before).
@@ -554,6 +625,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     turn(true);
 #pragma unroll
     for (int i = 0; i < FR + FC; ++i) read(F0, i, s_tiles, 0);
+    read_cols(F0, s_tiles, 0);
     int at = 0;   // the stage's place in the ring
     auto stage = [&](int kt, bool last) {
         char* cur = s_tiles + at * kStage;
@@ -661,12 +733,15 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             if (next >= 0 && A.q16) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(CN * 4 / 64) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             u32x4 a[FC];
+            const char* q = s_q + buf * CN * 64;
+            if constexpr (TR) {
+                int qa[FC];
 #pragma unroll
-            for (int h = 0; h < FC; ++h) {
-                const char* q = s_q + buf * CN * 64;
-                if constexpr (TR)
-                    a[h] = read_tr<T, CN / E>(q, 0, tr_lane<T, CN / E>(h * 16, lane));
-                else
+                for (int h = 0; h < FC; ++h) qa[h] = tr_lane<T, CN / E>(h * 16, lane);
+                read_tr_wait<T, CN / E, 0>(a, q, qa);
+            } else {
+#pragma unroll
+                for (int h = 0; h < FC; ++h)
                     a[h] = *reinterpret_cast<const u32x4*>(q + ((h * 16 + li) * 4 + swz4(li, g)) * 16);
             }
             const int after_next = next >= 0 ? after(next) : -1;
@@ -1018,6 +1093,20 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
                 if (kk < BK) *reinterpret_cast<u32x4*>(s_v[buf] + (kk * VPR + swz_tr<T, VPR>(kk, q % VPR)) * 16) = v[i];
             }
         };
+        const int ua[2] = {tr_lane<T, CPR>(wave * 32, lane), tr_lane<T, CPR>(wave * 32 + 16, lane)};
+        auto read_skinny = [&](u32x4 (&b)[RF], const char* tile, auto k0) {   // four at a time
+            constexpr int N = RF < 4 ? RF : 4;
+#pragma unroll
+            for (int j = 0; j < RF; j += N) {
+                u32x4 v[N];
+                int at[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) at[i] = tr_lane<T, VPR>((j + i) * 16, lane);
+                read_tr_wait<T, VPR, decltype(k0)::value>(v, tile, at);
+#pragma unroll
+                for (int i = 0; i < N; ++i) b[j + i] = v[i];
+            }
+        };
         f32x4 acc[2][RF];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -1039,11 +1128,13 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 u32x4 a[2], b[RF];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    a[h] = read_tr<T, CPR>(s_u[buf], s * KS, tr_lane<T, CPR>(wave * 32 + h * 16, lane));
-#pragma unroll
-                for (int j = 0; j < RF; ++j) b[j] = read_tr<T, VPR>(s_v[buf], s * KS, tr_lane<T, VPR>(j * 16, lane));
+                if (s == 0) {
+                    read_tr_wait<T, CPR, 0>(a, s_u[buf], ua);
+                    read_skinny(b, s_v[buf], std::integral_constant<int, 0>{});
+                } else {
+                    read_tr_wait<T, CPR, KS>(a, s_u[buf], ua);
+                    read_skinny(b, s_v[buf], std::integral_constant<int, KS>{});
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
