@@ -854,6 +854,7 @@ struct FewArgs {
     const int32_t *order, *cl;   // cl: the cluster of every place (a plan's), or of every row (order null)
     const float* scale;
     void *S, *H, *Y;             // S: float32, n x r; PAD: of the rows' type, n x rp, zero past r
+    int64_t ldw;                 // row stride of W
     int32_t n, K, P, r, rp, k, x16, q16, y4;
 };
 
@@ -947,7 +948,7 @@ __global__ __launch_bounds__(1024) void k_ad_few_main(FewArgs A) {
     const int lane = threadIdx.x & 63, g = lane >> 4, li = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t col0 = (int64_t)blockIdx.x * 16;
-    const T* w = static_cast<const T*>(A.W) + (col0 + li < A.P ? col0 + li : A.P - 1) * A.K;   // columns past P: not stored
+    const T* w = static_cast<const T*>(A.W) + (col0 + li < A.P ? col0 + li : A.P - 1) * A.ldw;   // columns past P: not stored
     const T* x[RF];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
@@ -1328,7 +1329,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     M.splits = L.main.splits;
     M.part = reinterpret_cast<float*>(ws + L.off_split);
     bool u16 = x16;
-    if (!L.few && L.pad_i != D.di) {
+    if (L.pad_i != D.di) {
         if ((e = pad_rows<T>(D.X, D.ldx, D.n, D.di, ws + L.off_x, L.pad_i, s)) != hipSuccess) return e;
         if ((e = pad_rows<T>(D.W, D.di, D.dout, D.di, ws + L.off_w, L.pad_i, s)) != hipSuccess) return e;
         M.U = ws + L.off_x;
@@ -1365,10 +1366,14 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         }
         hipLaunchKernelGGL((k_ad_few_inner<T, false>), dim3((unsigned)((D.n * D.r + 3) / 4)), dim3(256), 0, s, F);
         if ((e = hipGetLastError()) != hipSuccess) return e;
+        F.X = M.U;
+        F.ldx = M.ldu;
+        F.W = M.W;
+        F.ldw = M.ldw;
         auto go = [&](auto f) {
             constexpr int RF = decltype(f)::value;
             const dim3 g((unsigned)((D.dout + 15) / 16)), b(1024);
-            if (x16) hipLaunchKernelGGL((k_ad_few_main<T, RF, true>), g, b, 0, s, F);
+            if (u16) hipLaunchKernelGGL((k_ad_few_main<T, RF, true>), g, b, 0, s, F);
             else hipLaunchKernelGGL((k_ad_few_main<T, RF, false>), g, b, 0, s, F);
         };
         if (D.n <= 16) go(std::integral_constant<int, 1>{});
@@ -1578,12 +1583,16 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
     };
     L.main = main_shape(n, backward ? dout : di, backward ? di : dout, type);
     L.off_split = take(!L.few && L.main.splits > 1 ? (size_t)L.main.splits * n * (backward ? di : dout) * 4 : 0);
-    // Copies of rows whose width is no multiple of 16 bytes (few rows are read as they are).
+    // Copies of rows whose width is no multiple of 16 bytes.
     const int e = ks / 4;
     const size_t es = row_type_bytes(type);
     L.pad_i = (di + e - 1) / e * e;
     L.pad_o = (dout + e - 1) / e * e;
-    const bool ci = !L.few && L.pad_i != di, co = backward && L.pad_o != dout;
+    // Few rows: element loads cost a wave about 3 ns an element of its rows and
+    // columns (48 rows of 4097: 147 us, 58 with the copies), the copies two
+    // launches and W's traffic at 3 TB/s (1 row of 4097: 36 us without, 41 with).
+    if (L.few && 0.003 * di * ((n + 15) / 16 + 1) < 7 + 2.0 * dout * di * es / 3e6) L.pad_i = di;
+    const bool ci = L.pad_i != di, co = backward && L.pad_o != dout;
     L.off_x = take(ci ? (size_t)n * L.pad_i * es : 0);
     L.off_w = take(ci ? (size_t)dout * L.pad_i * es : 0);
     L.off_y = take(co ? (size_t)n * L.pad_o * es : 0);
