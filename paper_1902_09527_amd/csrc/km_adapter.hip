@@ -136,10 +136,9 @@ __device__ __forceinline__ int swz_tr(int k, int c) {
     return c ^ (m & (CPR - 1));
 }
 
-// Operand of 16 columns c0 .. along rows k0 + 0 .. KS of a tile whose rows
-// are the contraction (CPR chunks a row).  k0 and, for 16 bits, c0 move the
-// address by whole rows and chunk pairs only, so `at` (tr_lane) is a lane's
-// place for k0 = 0 and this c0.
+// Operand of 16 columns c0 .. along rows k0 + 0 .. of a tile whose rows are the
+// contraction (CPR chunks a row).  The swizzle is the same k0 rows further (a
+// multiple of a matrix step), so `at` (tr_lane) is a lane's place for k0 = 0.
 template <class T, int CPR>
 __device__ __forceinline__ int tr_lane(int c0, int lane) {
     const int li = lane & 15, g = lane >> 4;
@@ -289,7 +288,11 @@ __device__ __forceinline__ void list_chunks(const ListArgs& A, int* s) {
 // Inner products: S[place] = s_c Q_c u (rounded to T, rp wide, zero past r)
 // and, if H is not null, H[row] = Q_c u.  16 places a block; its four waves
 // share the contraction, their sums are added in wave order through LDS.
-// TR = false: Q_c is r x K (rows along the contraction); true: K x r.
+// TR = false: Q_c is r x K (rows along the contraction); true: K x r, brought
+// through LDS, a wave's own part, and read transposed.  The clusters of a block
+// follow one another.  Bound by the latency of its few rounds of loads: 8192 x
+// 2048 bf16, 64 clusters, r = 16: 18 to 21 us forward, 16 backward (the rows are
+// 7 us of memory time); 16384 x 4096 float16, r = 32: 78 us.
 struct InnerArgs {
     const void* U;
     int64_t ldu;
@@ -414,7 +417,18 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
 // The shared product over places with the adapters' term:
 //   Y[row] = V u + Q_c S[place],  V = W (P x K) forward, W^T (W is K x P) with TR.
 // A tile is TM places x TN columns, WR x WC waves; the contraction goes in
-// stages of 128 bytes a row, loaded to LDS while the stage before is used.
+// stages of 128 bytes a row, loaded to LDS (NS stages) while the one before is
+// used.
+//
+// 256 x 256 with 8 waves: the most products a byte loaded that registers and
+// LDS hold (128 accumulators a lane, 128 KB of stages).  16384 x 4096 x 8192
+// float16: 880 to 1040 us by the clock the card keeps (1.06 to 1.25 PFLOP/s; the
+// library's product alone 813 us); 8192 x 2048 x 2048 bf16: 67 to 73 us forward,
+// 69 to 75 backward (0.92 to 1.03 PFLOP/s; library 54), of which some 20 us are a
+// tile's start and end.  The matrix cores are busy 64 % of a clock that falls to
+// 1.6 GHz under this load: half of the stage loads taken out saves 8 %, L2 hits
+// for all of them 6 %, so it is the card's power that is left to save.
+// float32, 100,003 x 256 x 256: 148 us (89 TFLOP/s; 8 stages a tile).
 struct MainArgs {
     const void* U;
     int64_t ldu;
@@ -941,6 +955,9 @@ __global__ __launch_bounds__(256) void k_ad_few_inner_t(FewArgs A, ListArgs L) {
 }
 
 // y: 16 columns a block, its 16 waves share the contraction; RF x 16 places.
+// 48 rows of 4096 x 4096 bf16: 20 us (W once at the memory's rate: 7; every
+// block reads all rows of X, 100 MB from L2), 1 row of 1024 x 1024: 4.7 us.  32
+// columns a block halve that traffic but fill half of the chip: 26 us.
 template <class T, int RF, bool AL>
 __global__ __launch_bounds__(1024) void k_ad_few_main(FewArgs A) {
     constexpr int E = Mma<T>::E, KS = 4 * E, UN = AL ? 4 : 1, NWAVE = 16;
@@ -1038,6 +1055,10 @@ struct GradArgs {
     int32_t k, P, r, v16, o4, tiles;   // o4: out written by fours
 };
 
+// Bound by the latency of a chunk's stages: 8192 x 2048 bf16, 64 clusters, r =
+// 16: 26 us for both gradients (rows: 14 us of memory time); 100,003 x 256
+// float32: 57 us (43).
+//
 // 128 columns a block, 32 a wave; stages of 2 KS places, loaded while the one
 // before is multiplied (the skinny operand through registers).  WF: the wide
 // operand comes first (lanes hold four consecutive columns: dA), else second

@@ -7,10 +7,17 @@
 // slots of a tile wave by wave in their order.  No result depends on the
 // order in which blocks or lanes run.
 //
+// Measured: 32 slots 2.6 us; 1M slots of 100 clusters 26 us (histogram 4,
+// prefixes 6.6, scatter 15), 2M of 1000 56 us (8, 8.5, 39); bound by launches
+// and latency, and by the scatter's pieces of lines.
+//
 // The row movers are one pass over the rows each, in slot order: a row is
 // read once and written to the places of its slots (gather, gradient of
 // combine), or its slots' rows are read and their weighted sum is written
-// (combine, gradient of gather).  They are bound by the memory's rate.
+// (combine, gradient of gather).  They are bound by the memory's rate: 2M x
+// 256 float32 rows 773 us out and 778 us back (5.3 TB/s of rows read and
+// written; a large copy reaches 4.8), 16,382 x 2048 bf16 rows 31 us for the
+// gradients of combine (5.4 TB/s).
 #include <type_traits>
 
 #include "km_ops.h"
@@ -28,7 +35,7 @@ __device__ __forceinline__ int key_of(int id, int k) { return (unsigned)id < (un
 
 // Up to kSortRankMax slots: the place of slot p is the number of slots with a
 // smaller (key, p), counted against keys in LDS.  (N / 64) N comparisons of a
-// wave: 4 us at 1024 slots, one launch instead of three.
+// wave, one launch instead of three: 2.6 us at 32 slots.
 __global__ __launch_bounds__(kSortRankMax) void k_sort_rank(SortArgs A) {
     __shared__ __align__(16) int s_key[kSortRankMax];
     __shared__ int s_sorted[kSortRankMax];
