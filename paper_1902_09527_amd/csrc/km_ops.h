@@ -71,13 +71,13 @@ int ops_check_range(const void* p, size_t bytes, int device, const char* what);
 
 // ---- rows sorted by cluster and back (km_sort.hip)
 
-constexpr int64_t kSortRankMax = 1024;   // slots up to which one block ranks them by comparing
+constexpr int64_t kSortRankMax = 6144;   // slots up to which they are ranked by comparing
 constexpr int kSortBins = 4096;          // most digit values of a counting pass
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
 
 // How N slots with keys 0..k are sorted: passes over digits of `bits` bits,
-// tiles of kSortThreads * rounds slots.  passes = 0: ranked in one block.
+// tiles of kSortThreads * rounds slots.  passes = 0: ranked by comparing.
 struct SortShape {
     int passes, bits, rounds;
     int64_t tiles;

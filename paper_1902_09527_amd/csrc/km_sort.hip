@@ -1,13 +1,13 @@
 // Rows sorted by cluster and back.
 //
 // The plan is a stable counting sort of the n m slots by cluster (empty slots
-// last): up to kSortRankMax slots in one block, more in passes over digits of
+// last): up to kSortRankMax slots by comparing, more in passes over digits of
 // the cluster index (one pass for up to kSortBins - 1 clusters): a histogram
 // per tile, its prefix sums over the tiles, and the scatter, which ranks the
 // slots of a tile wave by wave in their order.  No result depends on the
 // order in which blocks or lanes run.
 //
-// Measured: 32 slots 2.6 us; 1M slots of 100 clusters 26 us (histogram 4,
+// Measured: 32 slots 4.0 us; 1M slots of 100 clusters 26 us (histogram 4,
 // prefixes 6.6, scatter 15), 2M of 1000 56 us (8, 8.5, 39); bound by launches
 // and latency, and by the scatter's pieces of lines.
 //
@@ -28,46 +28,74 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Clusters up to which the one-block sort writes the offsets itself.
-constexpr int kSortRankOffsets = 1 << 16;
+// Clusters up to which the ranking counts the offsets too.
+constexpr int kSortRankOffsets = 1 << 13;
 
 __device__ __forceinline__ int key_of(int id, int k) { return (unsigned)id < (unsigned)k ? id : k; }
 
 // Up to kSortRankMax slots: the place of slot p is the number of slots with a
-// smaller (key, p), counted against keys in LDS.  (N / 64) N comparisons of a
-// wave, one launch instead of three: 2.6 us at 32 slots.
-__global__ __launch_bounds__(kSortRankMax) void k_sort_rank(SortArgs A) {
-    __shared__ __align__(16) int s_key[kSortRankMax];
-    __shared__ int s_sorted[kSortRankMax];
-    const int p = threadIdx.x, N = A.N, k = A.k;
-    const int key = p < N ? key_of(A.ids[p], k) : INT_MAX;
-    s_key[p] = key;
-    __syncthreads();
-    if (p < N) {
-        int place = 0;
-        const int N4 = (N + 3) & ~3;   // blockDim is a multiple of 64: the padding holds INT_MAX
+// smaller (key, p), and offsets[c] the number with a key below c, so both are
+// one kind of item: 64 of them a block, one a lane, whose waves share the slots
+// in chunks of 64 (broadcast from LDS, a wave's own part).  All slots of a chunk
+// come before an item of equal key, or all after it, but for the item's own
+// chunk: one comparison a slot.  (N + k) N / 64 comparisons of a wave over the
+// chip, one launch instead of three: 4.0 us at 1 to 64 slots, 5.0 at 1024, 8.6
+// at 4096 and 13.4 at 8192, where the three of a counting pass take 10 to 13 us
+// (and 5 more of the host) at any of these; two passes (more than 4095 clusters)
+// 25 us.
+__global__ __launch_bounds__(1024) void k_sort_rank(SortArgs A, int slot_blocks) {
+    __shared__ __align__(16) int s_key[16][64];
+    __shared__ int s_count[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int N = A.N, k = A.k, own = blockIdx.x;
+    const bool slots = own < slot_blocks;
+    const int64_t p = slots ? (int64_t)own * 64 + lane : (int64_t)(own - slot_blocks) * 64 + lane;   // slot or cluster
+    int key = INT_MAX;
+    if (!slots) key = p <= k ? (int)p : k;
+    else if (p < N) key = key_of(A.ids[p], k);
+    const int chunks = (N + 63) / 64;
+    int count = 0;
+    auto load = [&](int c) { return c < chunks && c * 64 + lane < N ? key_of(A.ids[c * 64 + lane], k) : INT_MAX; };
+    int next = load(wave);
+    for (int c = wave; c < chunks; c += waves) {
+        __builtin_amdgcn_wave_barrier();   // a wave's own: its reads of the last chunk come first
+        s_key[wave][lane] = next;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        next = load(c + waves);
+        const int4* o4 = reinterpret_cast<const int4*>(s_key[wave]);
+        if (slots && c == own) {
 #pragma unroll 4
-        for (int q = 0; q < N4; q += 4) {
-            const int4 o = *reinterpret_cast<const int4*>(s_key + q);
-            place += (o.x < key || (o.x == key && q < p)) ? 1 : 0;
-            place += (o.y < key || (o.y == key && q + 1 < p)) ? 1 : 0;
-            place += (o.z < key || (o.z == key && q + 2 < p)) ? 1 : 0;
-            place += (o.w < key || (o.w == key && q + 3 < p)) ? 1 : 0;
+            for (int q = 0; q < 16; ++q) {
+                const int4 o = o4[q];
+                count += o.x < key || (o.x == key && q * 4 < lane);
+                count += o.y < key || (o.y == key && q * 4 + 1 < lane);
+                count += o.z < key || (o.z == key && q * 4 + 2 < lane);
+                count += o.w < key || (o.w == key && q * 4 + 3 < lane);
+            }
+        } else {
+            const int below = key + (slots && c < own && key < INT_MAX ? 1 : 0);   // k + 1 at most
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const int4 o = o4[q];
+                count += o.x < below;
+                count += o.y < below;
+                count += o.z < below;
+                count += o.w < below;
+            }
         }
-        s_sorted[place] = key;
-        A.order[place] = p;
-        A.pos[p] = place;
-        A.sorted_ids[place] = key < k ? key : -1;
     }
+    s_count[wave][lane] = count;
     __syncthreads();
-    if (k > kSortRankOffsets) return;   // k_sort_offsets, over the chip
-    for (int64_t c = p; c <= k; c += blockDim.x) {   // offsets[c]: slots with a key below c
-        int lo = 0, hi = N;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_sorted[mid] < c) lo = mid + 1; else hi = mid;
-        }
-        A.offsets[c] = lo;
+    if (wave != 0) return;
+    for (int w = 1; w < waves; ++w) count += s_count[w][lane];
+    if (!slots) {
+        if (p <= k) A.offsets[p] = count;
+    } else if (p < N) {
+        A.order[count] = (int)p;
+        A.pos[p] = count;
+        A.sorted_ids[count] = key < k ? key : -1;
     }
 }
 
@@ -274,10 +302,12 @@ SortShape sort_shape(int64_t N, int32_t k) {
 
 hipError_t launch_sort_plan(const SortArgs& A, const SortShape& S, char* ws, hipStream_t s) {
     if (S.passes == 0) {
-        const int threads = A.N < 1 ? 64 : (A.N + 63) / 64 * 64;
-        hipLaunchKernelGGL(k_sort_rank, dim3(1), dim3(threads), 0, s, A);
+        const bool apart = A.k > kSortRankOffsets;   // offsets by search, over the chip
+        const int chunks = (A.N + 63) / 64, waves = chunks < 1 ? 1 : chunks < 16 ? chunks : 16;
+        const int blocks = chunks + (apart ? 0 : A.k / 64 + 1);
+        if (blocks > 0) hipLaunchKernelGGL(k_sort_rank, dim3(blocks), dim3(64 * waves), 0, s, A, chunks);
         hipError_t e = hipGetLastError();
-        return e == hipSuccess && A.k > kSortRankOffsets ? sort_offsets(A, s) : e;
+        return e == hipSuccess && apart ? sort_offsets(A, s) : e;
     }
     // Passes alternate between the workspace's order and A.order and end in A.order.
     int32_t* tmp = reinterpret_cast<int32_t*>(ws + S.off_idx);

@@ -60,6 +60,15 @@ def test_plan_at_the_edge_of_one_pass(n, k):
     _check_plan(_ids(rng, n, 1, k, 0.05), k)
 
 
+@pytest.mark.parametrize("k", [1, 63, 64, 8191, 8192, 8193])
+@pytest.mark.parametrize("n", [64, 128, 129, 960, 1024, 6081, 6144, 6145])
+def test_plan_at_the_edges_of_ranking(n, k):
+    rng = np.random.default_rng(n * 3 + k)
+    _check_plan(_ids(rng, n, 1, k, 0.1), k)
+    _check_plan(np.sort(_ids(rng, n, 1, k, 0.0), axis=0)[::-1].copy(), k)
+    _check_plan(np.full((n,), k - 1, np.int32), k)
+
+
 @pytest.mark.parametrize("n", [1, 100, 5000])
 def test_plan_with_every_slot_empty_or_one_cluster(n):
     _check_plan(np.full((n, 2), -1, np.int32), 9)
