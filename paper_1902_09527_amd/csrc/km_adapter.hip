@@ -1624,6 +1624,13 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
         const int64_t part = (n / 256 + 63) / 64 * 64;
         L.chunk = 16 * r > 512 ? 16 * r : 512;
         if (part > L.chunk) L.chunk = (int32_t)part;
+        // A chunk is a block's run of stages, some 1.5 us each: shorter ones while
+        // the blocks do not fill the chip twice over (4000 x 256 float32, 8
+        // clusters: gradients 45 us without, 30 with; 8192 x 1024 bf16, r = 64:
+        // 90 and 80).  64 rows or twice the blocks only add partial sums (8192 x
+        // 512 bf16, r = 8: 34 us so, 38 then).
+        const int64_t tiles = ((int64_t)di + 127) / 128 + ((int64_t)dout + 127) / 128;
+        while (L.chunk > 128 && L.chunk > 4 * r && (n / L.chunk + (k < n ? k : n)) * tiles < 512) L.chunk /= 2;
         const int64_t cuts = n / L.chunk;
         L.max_items = cuts + (k < n ? k : n);
         // A cluster of several chunks has one that is not full: at most 2 cuts partial sums.
