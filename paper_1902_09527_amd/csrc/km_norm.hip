@@ -8,8 +8,8 @@
 // large sums).  All arithmetic is float32.  L lanes share a row, each lane
 // owning the same columns of every row, so the backward pass keeps its share
 // of dg and db in registers over all rows of a block; a second kernel adds the
-// blocks' sums in a fixed order.  Rows too wide for the registers are read
-// again from cache.
+// blocks' sums in a fixed order.  Rows too wide for the registers of 1024 lanes
+// are read again from cache, and dg and db take a pass over columns.
 //
 // Bound by the memory's rate.  8192 x 4096 bf16: forward 23 us (5.9 TB/s),
 // backward 44 (4.6) and sums 5; 1,000,003 x 250 float32 (two elements a lane):
@@ -22,10 +22,13 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
-// Sum over the L lanes of a row.  L = 256: over the block, through LDS; the
+// Threads of a block whose rows have L lanes each.
+constexpr int norm_threads(int L) { return L > kNormThreads ? L : kNormThreads; }
+
+// Sum over the L lanes of a row.  L >= 256: over the block, through LDS; the
 // caller alternates between two slots so that one barrier a sum is enough.
 template <int L>
-__device__ __forceinline__ float row_sum(float v, float (*s)[4], int slot) {
+__device__ __forceinline__ float row_sum(float v, float (*s)[16], int slot) {
     if constexpr (L <= 64) {
         return group_sum<L>(v);
     } else {
@@ -33,7 +36,11 @@ __device__ __forceinline__ float row_sum(float v, float (*s)[4], int slot) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) s[slot][wave] = v;
         __syncthreads();
-        return (s[slot][0] + s[slot][1]) + (s[slot][2] + s[slot][3]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < L / 64; w += 4)
+            sum += (s[slot][w] + s[slot][w + 1]) + (s[slot][w + 2] + s[slot][w + 3]);
+        return sum;
     }
 }
 
@@ -57,9 +64,9 @@ __device__ __forceinline__ void params(const void* p, int64_t c, float fill, flo
 
 // R steps of V elements a lane: d <= L R V.
 template <class T, class P, int V, int L, int R>
-__global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs A) {
+__global__ __launch_bounds__(norm_threads(L)) void k_norm_fwd(NormArgs A) {
     using W = Vec<T, V>;
-    __shared__ float s_red[2][4];
+    __shared__ float s_red[2][16];
     const int l = threadIdx.x % L, nv = A.d / V;
     const float dim = (float)A.d;
     float g[R][V], b[R][V];
@@ -69,8 +76,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs A) {
         params<P, V>(in ? A.gamma : nullptr, (int64_t)(l + r * L) * V, 1.0f, g[r]);
         params<P, V>(in ? A.beta : nullptr, (int64_t)(l + r * L) * V, 0.0f, b[r]);
     }
-    const int64_t step = (int64_t)gridDim.x * (kNormThreads / L);
-    int64_t i = (int64_t)blockIdx.x * (kNormThreads / L) + threadIdx.x / L;
+    constexpr int kGroups = norm_threads(L) / L;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    int64_t i = (int64_t)blockIdx.x * kGroups + threadIdx.x / L;
     // The next row's loads are in flight while a row is worked on.
     W nx[R];
     auto fetch = [&](int64_t q) {
@@ -123,7 +131,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd(NormArgs A) {
 template <class T, class P, int V>
 __global__ __launch_bounds__(kNormThreads) void k_norm_fwd_wide(NormArgs A) {
     using W = Vec<T, V>;
-    __shared__ float s_red[2][4];
+    __shared__ float s_red[2][16];
     const int nv = A.d / V;
     const float dim = (float)A.d;
     for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
@@ -166,10 +174,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_fwd_wide(NormArgs A) {
 }
 
 template <class T, class P, int V, int L, int R>
-__global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs A) {
+__global__ __launch_bounds__(norm_threads(L)) void k_norm_bwd(NormArgs A) {
     using W = Vec<T, V>;
-    __shared__ float s_red[2][4];
-    constexpr int kGroups = kNormThreads / L;
+    __shared__ float s_red[2][16];
+    constexpr int kGroups = norm_threads(L) / L;
     const int l = threadIdx.x % L, nv = A.d / V;
     const float dim = (float)A.d;
     float g[R][V], dg[R][V], db[R][V];
@@ -277,37 +285,29 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd(NormArgs A) {
             }
 }
 
-// Wide rows: a block a row; its sums of dg and db stay in its own row of
-// part, each column owned by one lane.
+// Wider rows: a block a row, read twice (once from cache); dg and db apart.
 template <class T, class P, int V>
 __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
     using W = Vec<T, V>;
-    __shared__ float s_red[2][4];
+    __shared__ float s_red[2][16];
     const int nv = A.d / V;
     const float dim = (float)A.d;
-    float* out = A.part ? A.part + (int64_t)blockIdx.x * 2 * A.d : nullptr;
-    bool first = true;
-    for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x, first = false) {
+    for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
         const W* __restrict__ x = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx);
         const W* __restrict__ y = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + i * A.lddy);
         W* dx = reinterpret_cast<W*>(static_cast<T*>(A.dX) + i * A.d);
         const float mu = A.mean[i], rs = A.rstd[i];
         float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll 2
+#pragma unroll 4
         for (int c = threadIdx.x; c < nv; c += kNormThreads) {
             const W vx = x[c], vy = y[c];
             float g[V];
             params<P, V>(A.gamma, (int64_t)c * V, 1.0f, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const int64_t q = (int64_t)c * V + e;
-                const float xh = (to_f32(vx.e[e]) - mu) * rs, dy = to_f32(vy.e[e]), h = dy * g[e];
+                const float xh = (to_f32(vx.e[e]) - mu) * rs, h = to_f32(vy.e[e]) * g[e];
                 s1 += h;
                 s2 = fmaf(h, xh, s2);
-                if (out) {
-                    out[q] = first ? dy * xh : fmaf(dy, xh, out[q]);
-                    out[A.d + q] = first ? dy : out[A.d + q] + dy;
-                }
             }
         }
         s1 = row_sum<256>(s1, s_red, 0) / dim;
@@ -325,6 +325,40 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_bwd_wide(NormArgs A) {
             }
             dx[c] = o;
         }
+    }
+}
+
+// Shares of dg and db for the wider rows: V columns a lane, blockIdx.y's run of
+// rows (A.blocks of them), its sums in registers and written once.  Two reads
+// more of the rows: backward of 8192 x 16384 float32 619 us (1100 with sums
+// updated in memory row by row; 337 at a copy's rate).
+template <class T, int V>
+__global__ __launch_bounds__(kNormThreads) void k_norm_cols(NormArgs A) {
+    using W = Vec<T, V>;
+    const int nv = A.d / V, c = blockIdx.x * kNormThreads + threadIdx.x;
+    if (c >= nv) return;
+    const int64_t per = (A.n + A.blocks - 1) / A.blocks, i0 = blockIdx.y * per;
+    const int64_t i1 = i0 + per < A.n ? i0 + per : A.n;
+    float dg[V], db[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) dg[e] = db[e] = 0.0f;
+#pragma unroll 4
+    for (int64_t i = i0; i < i1; ++i) {
+        const W vx = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx)[c];
+        const W vy = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + i * A.lddy)[c];
+        const float mu = A.mean[i], rs = A.rstd[i];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float dy = to_f32(vy.e[e]);
+            dg[e] = fmaf(dy, (to_f32(vx.e[e]) - mu) * rs, dg[e]);
+            db[e] += dy;
+        }
+    }
+    float* out = A.part + (int64_t)blockIdx.y * 2 * A.d + (int64_t)c * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        out[e] = dg[e];
+        out[A.d + e] = db[e];
     }
 }
 
@@ -356,7 +390,11 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs A) {
 struct Shape {
     int L, R;
 };
-Shape norm_shape(int nv) {
+// Beyond 1024 vectors a row is a block's of 1024 lanes where that pays (both
+// sides measured): backward of 18587 x 11456 bf16 286 us (1827 a row read
+// twice), forward 210 (289); 16384 x 2050 bf16, two elements a lane: backward
+// 71 us (232), but forward 65 (43 read three times).
+Shape norm_shape(int nv, int V, bool bwd) {
     if (nv <= 8) return {8, 1};
     if (nv <= 32) return {32, 1};
     if (nv <= 64) return {64, 1};
@@ -364,6 +402,9 @@ Shape norm_shape(int nv) {
     if (nv <= 256) return {64, 4};
     if (nv <= 512) return {256, 2};
     if (nv <= 1024) return {256, 4};
+    if (nv <= 2048 && (bwd || V > 2)) return {1024, 2};
+    // 16 bytes a lane have no room for more of a row.
+    if (nv <= 4096 && V <= 2 && bwd) return {1024, 4};
     return {256, 0};
 }
 
@@ -371,37 +412,46 @@ Shape norm_shape(int nv) {
 // few, and at most 512 (each writes its sums of dg and db). Fewer vectors a
 // row never make more blocks.
 int bwd_blocks(int64_t n, int nv) {
-    const int64_t groups = kNormThreads / norm_shape(nv).L, b = (n + 2 * groups - 1) / (2 * groups);
+    const int L = norm_shape(nv, 1, true).L;   // V matters from 256 lanes on only, where a block has one row anyhow
+    const int64_t groups = norm_threads(L) / L, b = (n + 2 * groups - 1) / (2 * groups);
     return (int)(b < 1 ? 1 : b > 512 ? 512 : b);
 }
 
 template <class T, class P, int V, int L, int R>
 hipError_t norm_go(const NormArgs& A, bool bwd, hipStream_t s) {
-    const int groups = kNormThreads / L;
+    constexpr int kThreads = norm_threads(L), groups = kThreads / L;
     if (bwd) {
         const size_t lds = A.part && groups > 1 ? (size_t)(groups - 1) * 2 * R * V * L * 4 : 0;
-        hipLaunchKernelGGL((k_norm_bwd<T, P, V, L, R>), dim3((unsigned)A.blocks), dim3(kNormThreads), lds, s, A);
+        hipLaunchKernelGGL((k_norm_bwd<T, P, V, L, R>), dim3((unsigned)A.blocks), dim3(kThreads), lds, s, A);
     } else {
         // At most 2048 blocks (8 a compute unit): gamma and beta are loaded once a block.
         int64_t b = (A.n + groups - 1) / groups;
         if (b > 2048) b = 2048;
-        hipLaunchKernelGGL((k_norm_fwd<T, P, V, L, R>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
+        hipLaunchKernelGGL((k_norm_fwd<T, P, V, L, R>), dim3((unsigned)b), dim3(kThreads), 0, s, A);
     }
     return hipGetLastError();
 }
 
 template <class T, class P, int V>
 hipError_t norm_vec(const NormArgs& A, bool bwd, hipStream_t s) {
-    const Shape S = norm_shape(A.d / V);
+    const Shape S = norm_shape(A.d / V, V, bwd);
     if (S.L == 8) return norm_go<T, P, V, 8, 1>(A, bwd, s);
     if (S.L == 32) return norm_go<T, P, V, 32, 1>(A, bwd, s);
     if (S.L == 64 && S.R == 1) return norm_go<T, P, V, 64, 1>(A, bwd, s);
     if (S.L == 64 && S.R == 2) return norm_go<T, P, V, 64, 2>(A, bwd, s);
     if (S.L == 64 && S.R == 4) return norm_go<T, P, V, 64, 4>(A, bwd, s);
-    if (S.R == 2) return norm_go<T, P, V, 256, 2>(A, bwd, s);
-    if (S.R == 4) return norm_go<T, P, V, 256, 4>(A, bwd, s);
+    if (S.L == 256 && S.R == 2) return norm_go<T, P, V, 256, 2>(A, bwd, s);
+    if (S.L == 256 && S.R == 4) return norm_go<T, P, V, 256, 4>(A, bwd, s);
+    if (S.L == 1024 && S.R == 2) return norm_go<T, P, V, 1024, 2>(A, bwd, s);
+    if constexpr (V <= 2)
+        if (S.L == 1024) return norm_go<T, P, V, 1024, 4>(A, bwd, s);
     if (bwd) {
-        hipLaunchKernelGGL((k_norm_bwd_wide<T, P, V>), dim3((unsigned)A.blocks), dim3(kNormThreads), 0, s, A);
+        const int64_t b = A.n < 32768 ? A.n : 32768;
+        hipLaunchKernelGGL((k_norm_bwd_wide<T, P, V>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);
+        if (A.part)
+            hipLaunchKernelGGL((k_norm_cols<T, V>),
+                               dim3((unsigned)((A.d / V + kNormThreads - 1) / kNormThreads), (unsigned)A.blocks),
+                               dim3(kNormThreads), 0, s, A);
     } else {
         const int64_t b = A.n < 32768 ? A.n : 32768;
         hipLaunchKernelGGL((k_norm_fwd_wide<T, P, V>), dim3((unsigned)b), dim3(kNormThreads), 0, s, A);

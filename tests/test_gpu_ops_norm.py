@@ -78,6 +78,15 @@ def test_rows(d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [2049, 2050, 4097, 4098, 8188, 8194, 8196, 11_456, 16_392, 32_768])
+def test_rows_of_many_lanes(d, dtype):
+    rng = np.random.default_rng(d)
+    for n in (1, 77):
+        X, dY, g, b = _case(rng, n, d, dtype, dtype, shift=0.5)
+        _check(X, dY, g, b, 1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("d,pad", [(48, 16), (250, 3), (2048, 8), (9000, 24)])
 def test_strided_rows_and_parameter_types(d, pad, dtype):
     rng = np.random.default_rng(d)
