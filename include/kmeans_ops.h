@@ -110,9 +110,9 @@ int kmeans_norm_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
  *   A      k x r x din                   B  k x dout x r
  *   scale  k float32 or NULL (ones)
  *   Y      n x dout                      H  n x r (for the backward pass)
- * all of one type; h and scale_c h are rounded to it once each where they
- * enter the second product (not for up to 64 rows, where it is formed in
- * float32).  The clusters come as
+ * all of one type; the result H is h rounded to it, scale_c h keeps its float32
+ * value into the second product (to 2^-16 of it in bfloat16 and 2^-22 in
+ * float16, whose range it may leave).  The clusters come as
  *   ids    n int32, with sorted_ids = offsets = order = NULL: the rows are
  *          sorted in the workspace where the form for many rows takes them;
  *   or a plan of kmeans_sort_plan with n slots (ids is not read): sorted_ids,
@@ -136,7 +136,8 @@ int kmeans_adapter_forward(const void* X, int64_t ldx, int64_t n, int32_t din, i
  *   g = scale_c B_c^T dy,  dX = W^T dy + A_c^T g  (n x din),
  *   dA_c = sum g x^T  (k x r x din),  dB_c = scale_c sum dy h^T  (k x dout x r)
  * over the rows of each cluster (zeros for a cluster with none), all of the
- * rows' type; g is rounded to it once.  W has no gradient here: it is frozen
+ * rows' type; g keeps its float32 value as scale_c h does, and h is H as it is
+ * given, rounded as a stored activation is.  W has no gradient here: it is frozen
  * where adapters are trained.
  */
 int kmeans_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* H, int64_t n,

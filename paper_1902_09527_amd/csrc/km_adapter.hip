@@ -13,8 +13,13 @@
 // results.  The adapters' gradients contract over a cluster's rows; long
 // clusters are cut into chunks whose float32 sums are joined in order.
 //
-// Sums are float32 (matrix-core accumulators); h and g are rounded to the
-// rows' type, once, as the matrix cores' operands.
+// Sums are float32 (matrix-core accumulators), and s h and g keep their float32
+// values between the two products: as an operand of the 16-bit matrix cores such
+// a value v is two, v rounded and the remainder rounded (16 bits together in
+// bfloat16, 22 in float16), and float16's narrow exponents are met by a power of
+// two that is taken out first and multiplied back into the float32 product.  H
+// is rounded once, as the result that it is, and dB is the product with that H.
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -113,6 +118,42 @@ __device__ __forceinline__ void store4(T* row, int64_t col0, int64_t P, f32x4 v,
         for (int i = 0; i < 4; ++i)
             if (col0 + i < P) row[col0 + i] = from_f32<T>(v[i]);
     }
+}
+
+// S, the inner products that the second product takes: per place and step of 16
+// indexes of r the 16 values (float32), or their 16 upper and 16 lower parts
+// (16 bits), which meet the same 16 of the adapter; zero past r.
+constexpr int kStep = 16;
+template <class T>
+constexpr int kStepElems = sizeof(T) == 2 ? 2 * kStep : kStep;
+template <class T>
+constexpr bool kShifted = std::is_same_v<T, _Float16>;
+
+// The power of two that is taken out of float16 parts, m the largest finite
+// magnitude among their values: m is left between 2^14 and 2^15, so the two parts
+// of v are off by at most 2^-22 |v| + 2^-39 m.
+__device__ __forceinline__ int f16_shift(float m) {
+    const int e = __builtin_amdgcn_frexp_expf(m);
+    return (e > -100 ? e : -100) - 15;
+}
+__device__ __forceinline__ float finite_max(float m, float v) { return fmaxf(m, fabsf(v) < INFINITY ? fabsf(v) : 0.0f); }
+
+// Consecutive values of a step (`step`: its first element), from index i on.
+// The lower part of what is not finite is nothing.
+template <class T, int N>
+__device__ __forceinline__ void put_step(T* step, int i, const float (&v)[N], int shift) {
+    Vec<T, N> hi, lo;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float x = kShifted<T> ? ldexpf(v[e], -shift) : v[e];
+        hi.e[e] = from_f32<T>(x);
+        if constexpr (sizeof(T) == 2) {
+            const float up = to_f32(hi.e[e]);
+            lo.e[e] = fabsf(up) < INFINITY ? from_f32<T>(x - up) : (T)0.0f;
+        }
+    }
+    *reinterpret_cast<Vec<T, N>*>(step + i) = hi;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<Vec<T, N>*>(step + kStep + i) = lo;
 }
 
 // One asynchronous 16-byte move a lane from `src` to LDS base + 16 lane.
@@ -285,8 +326,8 @@ __device__ __forceinline__ void list_chunks(const ListArgs& A, int* s) {
 }
 
 // --------------------------------------------------------------------------
-// Inner products: S[place] = s_c Q_c u (rounded to T, rp wide, zero past r)
-// and, if H is not null, H[row] = Q_c u.  16 places a block; its four waves
+// Inner products: S[place] = s_c Q_c u (in steps, rp elements a place) and, if H
+// is not null, H[row] = Q_c u.  16 places a block; its four waves
 // share the contraction, their sums are added in wave order through LDS.
 // TR = false: Q_c is r x K (rows along the contraction); true: K x r, brought
 // through LDS, a wave's own part, and read transposed.  The clusters of a block
@@ -300,6 +341,7 @@ struct InnerArgs {
     const int32_t *order, *sids, *offsets;
     const float* scale;
     void *S, *H;
+    int32_t* shift;   // float16: per place and step
     int64_t n;
     int32_t K, r, rp, u16, q16, h4;   // u16 / q16: rows of U / Q can be read 16 bytes at a time; h4: H written by fours
 };
@@ -322,7 +364,7 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
     const int mine = in ? A.sids[place] : -1;
     const int64_t row = in ? row_of(A.order, place) : 0;
     const T* u = static_cast<const T*>(A.U) + row * A.ldu;
-    const int steps = (A.K + KS - 1) / KS;
+    const int steps = (A.K + KS - 1) / KS, steps_r = (A.r + kStep - 1) / kStep;
     int c = __builtin_amdgcn_readfirstlane(A.sids[p0]);
     while (c >= 0) {
         f32x4 acc[RF];
@@ -389,16 +431,25 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
         for (int j = 0; j < RF; ++j) s_red[wave][j][lane] = acc[j];
         __syncthreads();
         const float sc = A.scale ? A.scale[c] : 1.0f;
-        for (int j = wave; j * 16 < A.rp; j += 4) {
-            f32x4 v{0, 0, 0, 0};
-            if (j < RF) v = (s_red[0][j][lane] + s_red[1][j][lane]) + (s_red[2][j][lane] + s_red[3][j][lane]);
-            const int r0 = j * 16 + g * 4;
+        for (int j = wave; j < steps_r; j += 4) {
+            f32x4 v = (s_red[0][j][lane] + s_red[1][j][lane]) + (s_red[2][j][lane] + s_red[3][j][lane]);
+            const int r0 = j * kStep + g * 4;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (r0 + i >= A.r) v[i] = 0.0f;
+            const float w[4] = {v[0] * sc, v[1] * sc, v[2] * sc, v[3] * sc};
+            int shift = 0;
+            if constexpr (kShifted<T>) {
+                float m = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = finite_max(m, w[i]);
+                m = fmaxf(m, __shfl_xor(m, 16));
+                shift = f16_shift(fmaxf(m, __shfl_xor(m, 32)));
+            }
             if (mine == c) {
                 if (A.H) store4(static_cast<T*>(A.H) + row * A.r, r0, A.r, v, A.h4);
-                store4(static_cast<T*>(A.S) + place * A.rp, r0, A.rp, v * sc, true);
+                put_step(static_cast<T*>(A.S) + place * A.rp + j * kStepElems<T>, g * 4, w, shift);
+                if (kShifted<T> && g == 0) A.shift[place * steps_r + j] = shift;
             }
         }
         __syncthreads();
@@ -406,10 +457,10 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
         c = next < p0 + 16 && next < A.n ? __builtin_amdgcn_readfirstlane(A.sids[next]) : -1;
     }
     if (in && mine < 0)   // rows in no cluster
-        for (int j = wave; j * 16 < A.rp; j += 4) {
-            const int r0 = j * 16 + g * 4;
-            if (A.H) store4(static_cast<T*>(A.H) + row * A.r, r0, A.r, f32x4{0, 0, 0, 0}, A.h4);
-            store4(static_cast<T*>(A.S) + place * A.rp, r0, A.rp, f32x4{0, 0, 0, 0}, true);
+        for (int j = wave; j < steps_r; j += 4) {
+            if (A.H) store4(static_cast<T*>(A.H) + row * A.r, j * kStep + g * 4, A.r, f32x4{0, 0, 0, 0}, A.h4);
+            put_step(static_cast<T*>(A.S) + place * A.rp + j * kStepElems<T>, g * 4, {0.0f, 0.0f, 0.0f, 0.0f}, 0);
+            if (kShifted<T> && g == 0) A.shift[place * steps_r + j] = 0;
         }
 }
 
@@ -433,7 +484,8 @@ struct MainArgs {
     const void* U;
     int64_t ldu;
     const void *W, *Q, *S;
-    const int32_t *order, *sids, *offsets;
+    const int32_t* shift;   // float16: per place and step of S
+    const int32_t *order, *sids;
     void* Y;
     int64_t n;
     int32_t K, P, r, rp, q16, y4, y16;   // y4 / y16: Y can be written 4 elements / 16 bytes at a time
@@ -449,12 +501,15 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
     constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
     constexpr int kStage = (TM + TN) * 128;
+    constexpr int kLaterShifts = TM / WR < 64 ? 64 : TM / WR;   // a wave's, whole loads
     // A ring of NS stages: TM rows of U, then TN rows (TR: BK rows) of W; then the
-    // first matrix step of the places' inner products, their rows and clusters.
+    // first step of the places' inner products, their rows and clusters; float16:
+    // the powers of two of the first step, and of a later one by wave.
     extern __shared__ __align__(16) char s_tiles[];
     char* s_inner = s_tiles + NS * kStage;
     int32_t* s_rows = reinterpret_cast<int32_t*>(s_inner + TM * 64);
     int32_t* s_ids = s_rows + TM;
+    int32_t* s_shift = s_ids + TM;
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
 
@@ -488,6 +543,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
         if (tid % 8 == 0) {
             s_rows[(i * NT + tid) / 8] = (int32_t)row;
             s_ids[(i * NT + tid) / 8] = A.sids[place];
+            if constexpr (kShifted<T>) s_shift[(i * NT + tid) / 8] = A.shift[place * (A.rp / KS)];
         }
     }
 #pragma unroll
@@ -657,8 +713,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
     for (; kt + NS < whole && kt + NS < nk; ++kt) stage(kt, false);
     for (; kt + 1 < nk; ++kt) stage(kt, true);
 
-    // The adapters' operand of one cluster and matrix step, the wave's CN
-    // columns, to its part of the buffer of the stage before the last (two
+    // The adapters' operand of one cluster and step of r (16 bits: twice, for the
+    // upper and the lower parts of the inner products), the wave's CN columns, to its part of the buffer of the stage before the last (two
     // places in turn).  The first is loaded beside the last stage.
     constexpr int CN = TN / WC;
     char* s_q = s_tiles + (at == 0 ? NS - 1 : at - 1) * kStage + wave * (2 * CN * 64);
@@ -672,13 +728,13 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
                 const T* src;
                 bool in;
                 if constexpr (TR) {
-                    const int kk = q / (CN / E);
+                    const int kk = q / (CN / E), rr = k0 + kk % kStep;
                     const int64_t col = cb + swz_tr<T, CN / E>(kk, q % (CN / E)) * E;
-                    in = k0 + kk < A.r && col < A.P;
-                    src = static_cast<const T*>(A.Q) + ((int64_t)c * A.r + k0 + kk) * A.P + col;
+                    in = rr < A.r && col < A.P;
+                    src = static_cast<const T*>(A.Q) + ((int64_t)c * A.r + rr) * A.P + col;
                 } else {
                     const int64_t col = cb + q / 4;
-                    const int rr = k0 + swz4(q / 4, q % 4) * E;
+                    const int rr = k0 + swz4(q / 4, q % 4) * E % kStep;
                     in = col < A.P && rr < A.r;
                     src = static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r + rr;
                 }
@@ -689,21 +745,22 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             for (int q = lane; q < CN * 4; q += 64) {
                 u32x4 v;
                 if constexpr (TR) {
-                    const int kk = q / (CN / E), rr = k0 + kk < A.r ? k0 + kk : 0;
-                    v = only_if(k0 + kk < A.r,
-                                chunk_guarded(static_cast<const T*>(A.Q) + ((int64_t)c * A.r + rr) * A.P,
+                    const int kk = q / (CN / E), rr = k0 + kk % kStep;
+                    v = only_if(rr < A.r,
+                                chunk_guarded(static_cast<const T*>(A.Q) + ((int64_t)c * A.r + (rr < A.r ? rr : 0)) * A.P,
                                               cb + swz_tr<T, CN / E>(kk, q % (CN / E)) * E, A.P));
                 } else {
                     const int64_t col = cb + q / 4 < A.P ? cb + q / 4 : 0;   // columns past P are not stored
                     v = chunk_guarded(static_cast<const T*>(A.Q) + ((int64_t)c * A.P + col) * A.r,
-                                      k0 + swz4(q / 4, q % 4) * E, A.r);
+                                      k0 + swz4(q / 4, q % 4) * E % kStep, A.r);
                 }
                 *reinterpret_cast<u32x4*>(to + q * 16) = v;
             }
         }
     };
-    // The adapters' term belongs to the first part of the contraction.  The
-    // wave's first two clusters (its places are in cluster order, -1 last):
+    // The adapters' term belongs to the first part of the contraction.  It goes
+    // over the steps of r, and in each over the clusters of the wave's places
+    // (which are in cluster order, -1 last).  The first two operands:
     constexpr int RM = TM / WR;
     int c_first = -1, c_second = -1;
     if (w0 < A.n && split == 0) {
@@ -716,72 +773,110 @@ __global__ __launch_bounds__(64 * WR * WC) void k_ad_main(MainArgs A) {
             if (m) c_second = __builtin_amdgcn_readlane(id, __builtin_ctzll(m));
         }
     }
+    int k_second = 0;
+    if (c_second < 0 && A.r > kStep) c_second = c_first, k_second = kStep;
     if (c_first >= 0) fetch(c_first, 0, 0);
-    if (c_second >= 0) fetch(c_second, 0, 1);
+    if (c_second >= 0) fetch(c_second, k_second, 1);
+    char* s_later = s_tiles + at * kStage + wave * (RM * 64);   // in the last stage's buffer
+    static_assert(TM * WC * 64 <= kStage, "");
     stage(kt, true);
+    // The wave's inner products of a later step, to its part of the last stage's
+    // buffer, which no wave reads any more.  The second step's are on their way
+    // during the first.
+    constexpr int kLater = RM / 16 + (kShifted<T> ? (RM + 63) / 64 : 0), kOperand = CN * 4 / 64;
+    auto fetch_later = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < RM / 16; ++i) {
+            const int q = i * 64 + lane;
+            const int64_t place = w0 + q / 4 < A.n ? w0 + q / 4 : A.n - 1;
+            load_lds16(static_cast<const T*>(A.S) + place * A.rp + k0 / kStep * KS + q % 4 * E, s_later + i * 1024);
+        }
+        if constexpr (kShifted<T>) {
+#pragma unroll
+            for (int i = 0; i < (RM + 63) / 64; ++i) {
+                const int64_t place = w0 + i * 64 + lane < A.n ? w0 + i * 64 + lane : A.n - 1;
+                __builtin_amdgcn_global_load_lds((const KM_GLOBAL void*)(A.shift + place * (A.rp / KS) + k0 / kStep),
+                                                 (KM_LDS void*)(s_shift + TM + wave * kLaterShifts + i * 64), 4, 0, 0);
+            }
+        }
+    };
+    if (c_first >= 0 && A.r > kStep) fetch_later(kStep);
 
-    // The adapters' term, cluster by cluster of the wave's places (they are in
-    // cluster order): a lane keeps the sum only where its place is of the
-    // cluster, so that nothing of one cluster's adapter reaches another's rows.
-    // The next cluster's operand is loaded during the products of one.
+    // A lane keeps the sum only where its place is of the cluster, so that nothing
+    // of one cluster's adapter reaches another's rows.  The next two operands are
+    // on their way during the products of one.
     int mine[FR];
 #pragma unroll
     for (int f = 0; f < FR; ++f) mine[f] = w0 + f * 16 + li < A.n ? s_ids[w0 - bm + f * 16 + li] : -1;
-    auto after = [&](int c) {   // the lowest cluster above c of the wave's places, -1: none
+    auto after = [&](int& c, int& k0) {   // the next cluster and step; c = -1: none
         int next = -1;
 #pragma unroll
         for (int f = FR - 1; f >= 0; --f) {
             const uint64_t m = __ballot(mine[f] > c);
             if (m) next = __builtin_amdgcn_readlane(mine[f], __builtin_ctzll(m));
         }
-        return next;
+        c = next;
+        if (next < 0 && (k0 += kStep) < A.r) c = c_first;
     };
-    for (int k0 = 0; c_first >= 0 && k0 < A.r; k0 += KS) {
-        if (k0 > 0) {
-            fetch(c_first, k0, 0);
-            if (c_second >= 0) fetch(c_second, k0, 1);
+    const char* s_b = s_inner + (w0 - bm) * 64;
+    const int32_t* s_e = s_shift + (w0 - bm);
+    bool first = true;
+    for (int buf = 0, c = c_first, k0 = 0, next = c_second, k_next = k_second; c >= 0; buf ^= 1, first = false) {
+        // This operand is in the wave's own part of LDS (and the inner products of
+        // its step, which were asked for before the operand that follows it); what
+        // was asked for later may be on its way.
+        if (!A.q16) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        else if (first && A.r > kStep) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kOperand + kLater) : "memory");
+        else if (next >= 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kOperand) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        u32x4 a[FC];
+        const char* q = s_q + buf * CN * 64;
+        if constexpr (TR) {
+            int qa[FC];
+#pragma unroll
+            for (int h = 0; h < FC; ++h) qa[h] = tr_lane<T, CN / E>(h * 16, lane);
+            read_tr_wait<T, CN / E, 0>(a, q, qa);
+        } else {
+#pragma unroll
+            for (int h = 0; h < FC; ++h)
+                a[h] = *reinterpret_cast<const u32x4*>(q + ((h * 16 + li) * 4 + swz4(li, g)) * 16);
         }
-        int buf = 0, c = c_first, next = c_second;
-        while (c >= 0) {
-            // This cluster's operand is in the wave's own part of LDS; the next one's may be on its way.
-            if (next >= 0 && A.q16) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(CN * 4 / 64) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            u32x4 a[FC];
-            const char* q = s_q + buf * CN * 64;
-            if constexpr (TR) {
-                int qa[FC];
+        int c_after = next, k_after = k_next;
+        if (next >= 0) after(c_after, k_after);
+        if (c_after >= 0) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is overwritten
+            fetch(c_after, k_after, buf);
+        }
 #pragma unroll
-                for (int h = 0; h < FC; ++h) qa[h] = tr_lane<T, CN / E>(h * 16, lane);
-                read_tr_wait<T, CN / E, 0>(a, q, qa);
-            } else {
+        for (int f = 0; f < FR; ++f) {
+            const bool is = mine[f] == c;
+            if (!__ballot(is)) continue;
+            const u32x4 b = *reinterpret_cast<const u32x4*>(s_b + (f * 16 + li) * 64 + g * 16);
+            float two = 1.0f;
+            if constexpr (kShifted<T>) two = ldexpf(1.0f, s_e[f * 16 + li]);
 #pragma unroll
-                for (int h = 0; h < FC; ++h)
-                    a[h] = *reinterpret_cast<const u32x4*>(q + ((h * 16 + li) * 4 + swz4(li, g)) * 16);
-            }
-            const int after_next = next >= 0 ? after(next) : -1;
-            if (after_next >= 0) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before it is overwritten
-                fetch(after_next, k0, buf);
-            }
+            for (int h = 0; h < FC; ++h) {
+                f32x4 d = Mma<T>::mma(a[h], b, kShifted<T> ? f32x4{0, 0, 0, 0} : acc[f][h]);
 #pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                const bool is = mine[f] == c;
-                if (!__ballot(is)) continue;
-                const int64_t place = w0 + f * 16 + li < A.n ? w0 + f * 16 + li : A.n - 1;
-                const u32x4 b = k0 == 0
-                                    ? *reinterpret_cast<const u32x4*>(s_inner + (place - bm) * 64 + g * 16)
-                                    : *reinterpret_cast<const u32x4*>(static_cast<const T*>(A.S) + place * A.rp + k0 + g * E);
-#pragma unroll
-                for (int h = 0; h < FC; ++h) {
-                    const f32x4 d = Mma<T>::mma(a[h], b, acc[f][h]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[f][h][i] = is ? d[i] : acc[f][h][i];
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kShifted<T>) d[i] = fmaf(d[i], two, acc[f][h][i]);
+                    acc[f][h][i] = is ? d[i] : acc[f][h][i];
                 }
             }
-            c = next;
-            next = after_next;
-            buf ^= 1;
         }
+        if (next >= 0 && k_next != k0) {   // on to the next step's inner products
+            s_b = s_later;
+            s_e = s_shift + TM + wave * kLaterShifts;
+            if (k_next > kStep) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch_later(k_next);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+        }
+        c = next;
+        k0 = k_next;
+        next = c_after;
+        k_next = k_after;
     }
 
     // 16-bit results go through LDS so that 128 consecutive bytes of a row are
@@ -867,18 +962,35 @@ struct FewArgs {
     const void *W, *A, *B;
     const int32_t *order, *cl;   // cl: the cluster of every place (a plan's), or of every row (order null)
     const float* scale;
-    void *S, *H, *Y;             // S: float32, n x r; PAD: of the rows' type, n x rp, zero past r
+    void *S, *H, *Y;             // S: in steps; forward of few rows: float32, n x r
+    int32_t* shift;              // float16: per place and step
     int64_t ldw;                 // row stride of W
-    int32_t n, K, P, r, rp, k, x16, q16, y4;
+    int32_t n, K, P, r, k, x16, q16, y4;
 };
 
-// h: a wave a (place, index), its lanes along the row.
-template <class T, bool PAD>
-__global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
-    constexpr int E = Mma<T>::E;
-    const int lane = threadIdx.x & 63, wide = PAD ? A.rp : A.r;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= (int64_t)A.n * wide) return;
+// The inner products of a place and step, a lane each of 16 (any others idle).
+template <class T>
+__device__ __forceinline__ void put_lanes(T* S, int32_t* shift, int64_t step, int i, float v) {
+    int e = 0;
+    if constexpr (kShifted<T>) {
+        float m = finite_max(0.0f, v);
+#pragma unroll
+        for (int o = 1; o < kStep; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+        e = f16_shift(m);
+        if (i == 0) shift[step] = e;
+    }
+    put_step(S + step * kStepElems<T>, i, {v}, e);
+}
+
+// h: a wave a (place, index), its lanes along the row.  STEP: a block of 16
+// waves a place and step, for S in steps.
+template <class T, bool STEP>
+__global__ __launch_bounds__(STEP ? 1024 : 256) void k_ad_few_inner(FewArgs A) {
+    constexpr int E = Mma<T>::E, kWaves = STEP ? kStep : 4;
+    __shared__ float s_sum[kStep];
+    const int lane = threadIdx.x & 63, wide = STEP ? (A.r + kStep - 1) / kStep * kStep : A.r;
+    const int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (w >= (int64_t)A.n * wide) return;   // STEP: none, the grid is n wide / 16 blocks
     const int p = (int)(w / wide), j = (int)(w % wide);
     const int c = A.cl[p];
     const int64_t row = row_of(A.order, p);
@@ -904,10 +1016,16 @@ __global__ __launch_bounds__(256) void k_ad_few_inner(FewArgs A) {
     if (lane == 0) {
         if (j < A.r) static_cast<T*>(A.H)[row * A.r + j] = from_f32<T>(sum);
         const float s = in ? sum * (A.scale ? A.scale[c] : 1.0f) : 0.0f;
-        if constexpr (PAD) static_cast<T*>(A.S)[(int64_t)p * A.rp + j] = from_f32<T>(s);
-        else static_cast<float*>(A.S)[(int64_t)p * A.r + j] = s;
+        if constexpr (STEP) s_sum[j % kStep] = s;
+        else static_cast<float*>(A.S)[w] = s;
+    }
+    if constexpr (STEP) {
+        __syncthreads();
+        const int i = threadIdx.x;
+        if (i < kStep) put_lanes(static_cast<T*>(A.S), A.shift, blockIdx.x, i, s_sum[i]);
     }
 }
+
 
 // g: a block a (place, 16 indexes), its threads along the contraction, a row
 // of B_c each.  One more block lists the chunks.
@@ -919,11 +1037,11 @@ __global__ __launch_bounds__(256) void k_ad_few_inner_t(FewArgs A, ListArgs L) {
         list_chunks(L, reinterpret_cast<int*>(s_sum));
         return;
     }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, jc = A.rp / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, jc = (A.r + kStep - 1) / kStep;
     const int p = (int)(blockIdx.x / jc), j0 = (int)(blockIdx.x % jc) * 16;
     const int c = A.cl[p];
     float acc[16] = {};
-    if (c >= 0 && j0 < A.r) {
+    if (c >= 0) {
         const T* x = static_cast<const T*>(A.X) + row_of(A.order, p) * A.ldx;
         const T* b = static_cast<const T*>(A.B) + (int64_t)c * A.K * A.r;
 #pragma unroll 2
@@ -949,8 +1067,7 @@ __global__ __launch_bounds__(256) void k_ad_few_inner_t(FewArgs A, ListArgs L) {
     if (i < 16) {
         const bool in = c >= 0 && j0 + i < A.r;
         const float s = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
-        static_cast<T*>(A.S)[(int64_t)p * A.rp + j0 + i] =
-            from_f32<T>(in ? s * (A.scale ? A.scale[c] : 1.0f) : 0.0f);
+        put_lanes(static_cast<T*>(A.S), A.shift, blockIdx.x, i, in ? s * (A.scale ? A.scale[c] : 1.0f) : 0.0f);
     }
 }
 
@@ -1042,9 +1159,9 @@ __global__ __launch_bounds__(1024) void k_ad_few_main(FewArgs A) {
 struct GradArgs {
     const void* U;
     int64_t ldu;
-    const void* V;
+    const void* V;           // dA: S, by place, in steps; dB: H, by row
     int64_t ldv;
-    int32_t v_by_row;        // V's rows are rows (H), else places (S)
+    const int32_t* shift;    // float16, dA: per place and step
     const int32_t* order;
     const float* scale;      // per cluster, or null
     const int32_t* count;
@@ -1063,11 +1180,19 @@ struct GradArgs {
 // before is multiplied (the skinny operand through registers).  WF: the wide
 // operand comes first (lanes hold four consecutive columns: dA), else second
 // (four consecutive indexes of r: dB).
+//
+// dA's skinny operand is S: RF steps, in 16 bits of two operands each.  In
+// float16 one power of two, the largest of the item's places, is taken out of all.
+template <class T, int RF>
+constexpr int kSkinny = RF * kStepElems<T> * 8 * Mma<T>::E * (int)sizeof(T);   // bytes of a stage
+
 template <class T, int RF, bool WF, bool AL>
-__device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 512], char (*s_v)[RF * 2048]) {
-    constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, TC = 128, CPR = TC / E, VPR = RF * 16 / E;
+__device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 512], char (*s_v)[kSkinny<T, RF>]) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, TC = 128, CPR = TC / E;
+    constexpr int VW = WF ? kStepElems<T> : 16, VPR = RF * VW / E;   // elements of 16 indexes, chunks a place
     constexpr int NU = BK * CPR / 256, NV = (BK * VPR + 255) / 256;
-    static_assert(BK * CPR * 16 == 32 * 512 && BK * VPR * 16 == RF * 2048, "");
+    constexpr bool kShift = WF && kShifted<T>;
+    static_assert(BK * CPR * 16 == 32 * 512 && BK * VPR * 16 <= kSkinny<T, RF>, "");
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t total = (int64_t)A.count[0] * A.tiles;
@@ -1076,6 +1201,24 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
         const int64_t bc = (w % A.tiles) * TC;
         int64_t ur[NU], vr[NV];   // rows of the next stage to load
         u32x4 v[NV];
+        int most = 0, ve[kShift ? NV : 1];
+        const int steps = (A.r + kStep - 1) / kStep;
+        if constexpr (kShift) {
+            __shared__ int s_max[4];
+            const int32_t* p = A.shift + (int64_t)it.p0 * steps;
+            const int64_t size = (int64_t)(it.p1 - it.p0) * steps;
+            most = INT_MIN;
+            for (int64_t i = tid; i < size; i += 256) most = p[i] > most ? p[i] : most;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int other = __shfl_xor(most, o);
+                most = other > most ? other : most;
+            }
+            if (lane == 0) s_max[wave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) most = s_max[q] > most ? s_max[q] : most;
+        }
         auto rows = [&](int64_t p0) {
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
@@ -1085,7 +1228,7 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int64_t p = p0 + (i * 256 + tid) / VPR, q = p < it.p1 ? p : it.p0;
-                vr[i] = A.v_by_row ? row_of(A.order, q) : q;
+                vr[i] = WF ? q : row_of(A.order, q);
             }
         };
         auto load = [&](int64_t p0, int buf) {
@@ -1093,7 +1236,13 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
             for (int i = 0; i < NV; ++i) {
                 const int q = i * 256 + tid;
                 const bool in = p0 + q / VPR < it.p1;
-                v[i] = only_if(in, chunk(static_cast<const T*>(A.V) + vr[i] * A.ldv, q % VPR * E, A.r, A.v16));
+                const T* src = static_cast<const T*>(A.V) + vr[i] * A.ldv;
+                if constexpr (WF) v[i] = only_if(in, chunk_aligned(src, q % VPR * E, A.ldv));
+                else v[i] = only_if(in, chunk(src, q % VPR * E, A.r, A.v16));
+                if constexpr (kShift) {
+                    const int step = q % VPR * E / VW;
+                    ve[i] = A.shift[vr[i] * steps + (step < steps ? step : 0)];
+                }
             }
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
@@ -1112,23 +1261,16 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int q = i * 256 + tid, kk = q / VPR;
+                if constexpr (kShift) {
+                    Vec<T, E> x = __builtin_bit_cast(Vec<T, E>, v[i]);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x.e[e] = from_f32<T>(ldexpf(to_f32(x.e[e]), ve[i] - most));
+                    v[i] = __builtin_bit_cast(u32x4, x);
+                }
                 if (kk < BK) *reinterpret_cast<u32x4*>(s_v[buf] + (kk * VPR + swz_tr<T, VPR>(kk, q % VPR)) * 16) = v[i];
             }
         };
         const int ua[2] = {tr_lane<T, CPR>(wave * 32, lane), tr_lane<T, CPR>(wave * 32 + 16, lane)};
-        auto read_skinny = [&](u32x4 (&b)[RF], const char* tile, auto k0) {   // four at a time
-            constexpr int N = RF < 4 ? RF : 4;
-#pragma unroll
-            for (int j = 0; j < RF; j += N) {
-                u32x4 v[N];
-                int at[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) at[i] = tr_lane<T, VPR>((j + i) * 16, lane);
-                read_tr_wait<T, VPR, decltype(k0)::value>(v, tile, at);
-#pragma unroll
-                for (int i = 0; i < N; ++i) b[j + i] = v[i];
-            }
-        };
         f32x4 acc[2][RF];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -1149,19 +1291,26 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
             }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                u32x4 a[2], b[RF];
-                if (s == 0) {
-                    read_tr_wait<T, CPR, 0>(a, s_u[buf], ua);
-                    read_skinny(b, s_v[buf], std::integral_constant<int, 0>{});
-                } else {
-                    read_tr_wait<T, CPR, KS>(a, s_u[buf], ua);
-                    read_skinny(b, s_v[buf], std::integral_constant<int, KS>{});
+                u32x4 a[2];
+                if (s == 0) read_tr_wait<T, CPR, 0>(a, s_u[buf], ua);
+                else read_tr_wait<T, CPR, KS>(a, s_u[buf], ua);
+                constexpr int all = RF * VW / 16, N = all < 4 ? all : 4;   // skinny operands, four at a time
+#pragma unroll
+                for (int j = 0; j < all; j += N) {
+                    u32x4 b[N];
+                    int at[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) at[i] = tr_lane<T, VPR>((j + i) * 16, lane);
+                    if (s == 0) read_tr_wait<T, VPR, 0>(b, s_v[buf], at);
+                    else read_tr_wait<T, VPR, KS>(b, s_v[buf], at);
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            f32x4& d = acc[h][(j + i) * 16 / VW];
+                            d = WF ? Mma<T>::mma(a[h], b[i], d) : Mma<T>::mma(b[i], a[h], d);
+                        }
                 }
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < RF; ++j)
-                        acc[h][j] = WF ? Mma<T>::mma(a[h], b[j], acc[h][j]) : Mma<T>::mma(b[j], a[h], acc[h][j]);
             }
             if (p + BK < it.p1) put(buf ^ 1);
         }
@@ -1178,10 +1327,12 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
                 const int64_t rows_ = WF ? A.r : A.P, width = WF ? A.P : A.r;
                 if (rr >= rows_) continue;
                 const int64_t at = (slot * rows_ + rr) * width;
-                if (it.slot < 0)
-                    store4(static_cast<T*>(A.out) + at, x0, width, acc[h][j] * sc, A.o4);
-                else
-                    store4(A.part + at, x0, width, acc[h][j] * sc, width % 4 == 0);
+                f32x4 o = acc[h][j] * sc;
+                if constexpr (kShift)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = ldexpf(o[i], most);
+                if (it.slot < 0) store4(static_cast<T*>(A.out) + at, x0, width, o, A.o4);
+                else store4(A.part + at, x0, width, o, width % 4 == 0);
             }
     }
 }
@@ -1190,7 +1341,7 @@ __device__ __forceinline__ void grad_block(const GradArgs& A, char (*s_u)[32 * 5
 template <class T, int RF, bool AL>
 __global__ __launch_bounds__(256) void k_ad_grad(GradArgs A, GradArgs B) {
     __shared__ __align__(16) char s_u[2][32 * 512];
-    __shared__ __align__(16) char s_v[2][RF * 2048];
+    __shared__ __align__(16) char s_v[2][kSkinny<T, RF>];
     if (blockIdx.y == 0)
         grad_block<T, RF, true, AL>(A, s_u, s_v);
     else
@@ -1275,7 +1426,9 @@ hipError_t main_tile(MainArgs A, hipStream_t s) {
     constexpr int BK = 8 * Mma<T>::E;
     const int all = (A.K + BK - 1) / BK, share = (all + A.splits - 1) / A.splits;
     A.splits = (all + share - 1) / share;   // no part without a stage
-    constexpr int lds = NS * (TM + TN) * 128 + TM * 72;
+    constexpr int RM = TM / WR;   // float16: the powers of two of a step, and of a later one by wave
+    constexpr int lds = NS * (TM + TN) * 128 + TM * 72 + (kShifted<T> ? (TM + WR * WC * (RM < 64 ? 64 : RM)) * 4 : 0);
+    static_assert(lds <= 160 * 1024, "");
     if (lds > 65536) {
         const hipError_t e = raise_lds(k_ad_main<T, TM, TN, WR, WC, NS, TR, AL>, lds);
         if (e != hipSuccess) return e;
@@ -1335,9 +1488,9 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     M.ldw = D.di;
     M.Q = D.B;
     M.S = ws + L.off_s;
+    M.shift = reinterpret_cast<const int32_t*>(ws + L.off_shift);
     M.order = D.order;
     M.sids = D.sids;
-    M.offsets = D.offsets;
     M.Y = D.Y;
     M.n = D.n;
     M.K = D.di;
@@ -1378,10 +1531,11 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
         F.k = D.k;
         F.x16 = x16;
         F.y4 = y4;
-        F.rp = L.rp;
         F.q16 = M.q16;
+        F.shift = reinterpret_cast<int32_t*>(ws + L.off_shift);
         if (!L.few) {
-            hipLaunchKernelGGL((k_ad_few_inner<T, true>), dim3((unsigned)((D.n * L.rp + 3) / 4)), dim3(256), 0, s, F);
+            const unsigned steps = (unsigned)((D.r + kStep - 1) / kStep);
+            hipLaunchKernelGGL((k_ad_few_inner<T, true>), dim3((unsigned)D.n * steps), dim3(1024), 0, s, F);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             return main_go<T, false>(M, L.main, u16, s);
         }
@@ -1412,6 +1566,7 @@ hipError_t forward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hipS
     I.offsets = D.offsets;
     I.scale = D.scale;
     I.S = ws + L.off_s;
+    I.shift = reinterpret_cast<int32_t*>(ws + L.off_shift);
     I.H = D.H;
     I.n = D.n;
     I.K = D.di;
@@ -1431,6 +1586,7 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     bool w16 = D.di % E == 0 && a16(D.W);
     hipError_t e;
     char* S = ws + L.off_s;
+    int32_t* shift = reinterpret_cast<int32_t*>(ws + L.off_shift);
     const void *dY = D.dY, *X = D.X, *W = D.W;
     int64_t lddy = D.lddy, ldx = D.ldx, ldw = D.di;
     if (D.n > 0 && L.pad_o != D.dout) {
@@ -1464,6 +1620,7 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     I.offsets = D.offsets;
     I.scale = D.scale;
     I.S = S;
+    I.shift = shift;
     I.n = D.n;
     I.K = D.dout;
     I.r = D.r;
@@ -1479,13 +1636,14 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         F.cl = D.sids;
         F.scale = D.scale;
         F.S = S;
+        F.shift = shift;
         F.n = (int32_t)D.n;
         F.K = D.dout;
         F.r = D.r;
-        F.rp = L.rp;
         F.k = D.k;
         F.q16 = I.q16;
-        hipLaunchKernelGGL((k_ad_few_inner_t<T>), dim3((unsigned)(D.n * (L.rp / 16) + 1)), dim3(256), 0, s, F, Q);
+        hipLaunchKernelGGL((k_ad_few_inner_t<T>), dim3((unsigned)(D.n * ((D.r + kStep - 1) / kStep) + 1)), dim3(256), 0, s,
+                           F, Q);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     } else if ((e = inner_go<T, true>(I, Q, s)) != hipSuccess) {
         return e;
@@ -1498,9 +1656,9 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
         M.ldw = ldw;
         M.Q = D.A;
         M.S = S;
+        M.shift = shift;
         M.order = D.order;
         M.sids = D.sids;
-        M.offsets = D.offsets;
         M.Y = D.dX;
         M.n = D.n;
         M.K = D.dout;
@@ -1527,7 +1685,7 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     G.ldu = ldx;
     G.V = S;
     G.ldv = L.rp;
-    G.v16 = 1;
+    G.shift = shift;
     G.out = D.dA;
     G.P = D.di;
     G.tiles = (D.di + 127) / 128;
@@ -1537,7 +1695,6 @@ hipError_t backward_t(const AdapterArgs& D, char* ws, const AdapterShape& L, hip
     B.ldu = lddy;
     B.V = D.H;
     B.ldv = D.r;
-    B.v_by_row = 1;
     B.v16 = D.r % E == 0 && a16(D.H);
     B.scale = D.scale;
     B.out = D.dB;
@@ -1593,7 +1750,8 @@ MainShape main_shape(int64_t n, int32_t K, int32_t P, int type) {
 AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward) {
     AdapterShape L{};
     const int ks = type == kF32 ? 16 : 32;
-    L.rp = (r + ks - 1) / ks * ks;
+    const int steps = (r + kStep - 1) / kStep;
+    L.rp = steps * ks;
     L.few = !backward && n <= kAdapterFew;
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     size_t o = 0;
@@ -1617,7 +1775,8 @@ AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32
     L.off_x = take(ci ? (size_t)n * L.pad_i * es : 0);
     L.off_w = take(ci ? (size_t)dout * L.pad_i * es : 0);
     L.off_y = take(co ? (size_t)n * L.pad_o * es : 0);
-    L.off_s = take(L.few ? (size_t)n * r * 4 : (size_t)n * L.rp * row_type_bytes(type));
+    L.off_s = take(L.few ? (size_t)n * r * 4 : (size_t)n * L.rp * es);
+    L.off_shift = take(type == kF16 && !L.few ? (size_t)n * steps * 4 : 0);
     if (backward) {
         // Chunks long enough that their float32 sums are a small part of the
         // rows read, and at most 256 or so of them.

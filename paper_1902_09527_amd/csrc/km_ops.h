@@ -150,12 +150,12 @@ struct MainShape {
 };
 struct AdapterShape {
     MainShape main;
-    int32_t rp;          // r padded to a step of the matrix cores
+    int32_t rp;          // elements a row of the inner products, as the matrix cores take them
     int32_t few;         // forward: few rows
     int32_t pad_i, pad_o;   // din and dout padded to 16 bytes
     int32_t chunk;       // backward: rows a chunk
     int64_t max_items, part_a;   // part_a: float32 values of dA's partial sums
-    size_t off_x, off_w, off_y, off_split, off_s, off_count, off_items, off_first, off_part, bytes;   // workspace segments
+    size_t off_x, off_w, off_y, off_split, off_s, off_shift, off_count, off_items, off_first, off_part, bytes;   // workspace segments
 };
 AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward);
 hipError_t launch_adapter_forward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s);
