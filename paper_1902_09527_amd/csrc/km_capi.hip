@@ -2,7 +2,6 @@
 // ownership, launch configuration, the run loop and error reporting.  The
 // declarations and their contracts are in include/kmeans_mti.h.
 #include <math.h>
-#include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -12,7 +11,6 @@
 
 #include "kmeans_mti.h"
 #include "km_internal.h"
-#include "km_ops.h"
 
 namespace {
 
@@ -1396,22 +1394,3 @@ const char* kmeans_mti_strerror(int status) {
 const char* kmeans_mti_last_hip_error(void) { return g_last_hip; }
 
 }  // extern "C"
-
-// The error text and the device checks, for the entry points of km_ops.hip.
-namespace km {
-
-int ops_hip_error(hipError_t e, const char* what) { return hip_fail(e, what); }
-
-int ops_error(int status, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_last_hip, sizeof g_last_hip, fmt, ap);
-    va_end(ap);
-    return status;
-}
-
-int ops_check_range(const void* p, size_t bytes, int device, const char* what) {
-    return check_device_range(p, bytes, device, what);
-}
-
-}  // namespace km

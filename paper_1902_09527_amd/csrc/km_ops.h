@@ -64,7 +64,7 @@ inline bool rows_vec(const void* p, int64_t ld, int64_t d, size_t es, int bytes)
 }
 inline bool rows_vec16(const void* p, int64_t ld, int64_t d, size_t es) { return rows_vec(p, ld, d, es, 16); }
 
-// Error text and device checks of km_capi.hip, for the entry points elsewhere.
+// Error text and device checks of km_capi.hip, for km_ops.hip (km_host.hip).
 int ops_hip_error(hipError_t e, const char* what);
 int ops_error(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int ops_check_range(const void* p, size_t bytes, int device, const char* what);
