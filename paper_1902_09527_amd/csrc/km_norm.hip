@@ -22,6 +22,17 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
+// Rows after which a lane's sums of dg and db are added to its totals: the
+// rounding errors of a sum grow with its terms, so a lane's n rows cost those of
+// kFold + n / kFold terms (1,000,003 x 250 float32, 490 rows a lane: dg off by
+// 2.0e-7 of its norm, 4.4e-7 in one sum; the time is the same).
+constexpr int kFold = 32;
+// The totals of 1024 lanes, or of 32 columns a lane and more, are kept in LDS: in
+// registers they would leave half as many waves on the chip, or none of the
+// registers that the next row is loaded to.
+template <int V, int L, int R>
+constexpr bool kFoldLds = L == 1024 || R * V >= 32;
+
 // Threads of a block whose rows have L lanes each.
 constexpr int norm_threads(int L) { return L > kNormThreads ? L : kNormThreads; }
 
@@ -181,12 +192,41 @@ __global__ __launch_bounds__(norm_threads(L)) void k_norm_bwd(NormArgs A) {
     const int l = threadIdx.x % L, nv = A.d / V;
     const float dim = (float)A.d;
     float g[R][V], dg[R][V], db[R][V];
+    // Totals of dg and db: a lane's own, or its place in LDS, and that of its group.
+    constexpr bool kLds = kFoldLds<V, L, R>;
+    constexpr int kCols = R * V * L;
+    extern __shared__ float s_part[];   // groups (kLds) or groups - 1 times 2 kCols; none without part
+    const int grp = threadIdx.x / L;
+    float tg[kLds ? 1 : R][V], tb[kLds ? 1 : R][V];
+    auto place = [&](int q, int r, int e) { return s_part + q * 2 * kCols + (r * V + e) * L + l; };
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         params<P, V>(l + r * L < nv ? A.gamma : nullptr, (int64_t)(l + r * L) * V, 1.0f, g[r]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) dg[r][e] = db[r][e] = 0.0f;
+        for (int e = 0; e < V; ++e) {
+            dg[r][e] = db[r][e] = 0.0f;
+            if constexpr (!kLds) tg[r][e] = tb[r][e] = 0.0f;
+        }
     }
+    bool folded = false;
+    auto fold = [&]() {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if constexpr (kLds) {
+                    place(grp, r, e)[0] = folded ? place(grp, r, e)[0] + dg[r][e] : dg[r][e];
+                    place(grp, r, e)[kCols] = folded ? place(grp, r, e)[kCols] + db[r][e] : db[r][e];
+                } else {
+                    tg[r][e] += dg[r][e];
+                    tb[r][e] += db[r][e];
+                }
+                dg[r][e] = db[r][e] = 0.0f;
+                if (kLds && e % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few registers at a time
+            }
+        folded = true;
+    };
+    int rows = 0;
     const int64_t step = (int64_t)gridDim.x * kGroups;
     int64_t i = (int64_t)blockIdx.x * kGroups + threadIdx.x / L;
     // The next row's loads are in flight while a row is worked on.
@@ -242,46 +282,50 @@ __global__ __launch_bounds__(norm_threads(L)) void k_norm_bwd(NormArgs A) {
                 }
                 dx[l + r * L] = o;
             }
+        if (++rows == kFold && A.part) {
+            fold();
+            rows = 0;
+        }
     }
     if (!A.part) return;
+    constexpr bool kOwn = kLds && kGroups == 1;   // the last sums have not to go through LDS
+    if constexpr (!kOwn) fold();
     // The block's share: the groups of lanes that own the same columns are
     // added in group order.
-    extern __shared__ float s_part[];   // (kGroups - 1) x 2 x R V L, none for one group
     float* out = A.part + (int64_t)blockIdx.x * 2 * A.d;
-    constexpr int kCols = R * V * L;
-    const int grp = threadIdx.x / L;
+    constexpr int kOthers = kLds ? 0 : 1;   // the first group's place of the others'
     if constexpr (kGroups > 1) {
-        if (grp > 0) {
-            float* m = s_part + (int64_t)(grp - 1) * 2 * kCols;
+        if constexpr (!kLds) {
+            if (grp > 0)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    m[(r * V + e) * L + l] = dg[r][e];
-                    m[kCols + (r * V + e) * L + l] = db[r][e];
-                }
+                    for (int e = 0; e < V; ++e) {
+                        place(grp - 1, r, e)[0] = tg[r][e];
+                        place(grp - 1, r, e)[kCols] = tb[r][e];
+                    }
         }
         __syncthreads();
         if (grp > 0) return;
-        for (int q = 0; q < kGroups - 1; ++q) {
-            const float* m = s_part + (int64_t)q * 2 * kCols;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    dg[r][e] += m[(r * V + e) * L + l];
-                    db[r][e] += m[kCols + (r * V + e) * L + l];
-                }
-        }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (l + r * L < nv)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
+                float sg = kOwn && !folded ? 0.0f : kLds ? place(0, r, e)[0] : tg[kLds ? 0 : r][e];
+                float sb = kOwn && !folded ? 0.0f : kLds ? place(0, r, e)[kCols] : tb[kLds ? 0 : r][e];
+                if constexpr (kOwn) {
+                    sg += dg[r][e];
+                    sb += db[r][e];
+                }
+                for (int q = 1; q < kGroups; ++q) {
+                    sg += place(q - kOthers, r, e)[0];
+                    sb += place(q - kOthers, r, e)[kCols];
+                }
                 const int64_t c = (int64_t)(l + r * L) * V + e;
-                out[c] = dg[r][e];
-                out[A.d + c] = db[r][e];
+                out[c] = sg;
+                out[A.d + c] = sb;
             }
 }
 
@@ -339,26 +383,37 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_cols(NormArgs A) {
     if (c >= nv) return;
     const int64_t per = (A.n + A.blocks - 1) / A.blocks, i0 = blockIdx.y * per;
     const int64_t i1 = i0 + per < A.n ? i0 + per : A.n;
-    float dg[V], db[V];
+    float tg[V], tb[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) dg[e] = db[e] = 0.0f;
+    for (int e = 0; e < V; ++e) tg[e] = tb[e] = 0.0f;
+    for (int64_t q = i0; q < i1; q += kFold) {
+        const int64_t q1 = q + kFold < i1 ? q + kFold : i1;
+        float dg[V], db[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) dg[e] = db[e] = 0.0f;
 #pragma unroll 4
-    for (int64_t i = i0; i < i1; ++i) {
-        const W vx = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx)[c];
-        const W vy = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + i * A.lddy)[c];
-        const float mu = A.mean[i], rs = A.rstd[i];
+        for (int64_t i = q; i < q1; ++i) {
+            const W vx = reinterpret_cast<const W*>(static_cast<const T*>(A.X) + i * A.ldx)[c];
+            const W vy = reinterpret_cast<const W*>(static_cast<const T*>(A.dY) + i * A.lddy)[c];
+            const float mu = A.mean[i], rs = A.rstd[i];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float dy = to_f32(vy.e[e]);
+                dg[e] = fmaf(dy, (to_f32(vx.e[e]) - mu) * rs, dg[e]);
+                db[e] += dy;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float dy = to_f32(vy.e[e]);
-            dg[e] = fmaf(dy, (to_f32(vx.e[e]) - mu) * rs, dg[e]);
-            db[e] += dy;
+            tg[e] += dg[e];
+            tb[e] += db[e];
         }
     }
     float* out = A.part + (int64_t)blockIdx.y * 2 * A.d + (int64_t)c * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        out[e] = dg[e];
-        out[A.d + e] = db[e];
+        out[e] = tg[e];
+        out[A.d + e] = tb[e];
     }
 }
 
@@ -421,7 +476,12 @@ template <class T, class P, int V, int L, int R>
 hipError_t norm_go(const NormArgs& A, bool bwd, hipStream_t s) {
     constexpr int kThreads = norm_threads(L), groups = kThreads / L;
     if (bwd) {
-        const size_t lds = A.part && groups > 1 ? (size_t)(groups - 1) * 2 * R * V * L * 4 : 0;
+        const size_t lds = A.part ? (size_t)(kFoldLds<V, L, R> ? groups : groups - 1) * 2 * R * V * L * 4 : 0;
+        if (lds > 60 * 1024) {   // beyond what a kernel has without asking
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_norm_bwd<T, P, V, L, R>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+        }
         hipLaunchKernelGGL((k_norm_bwd<T, P, V, L, R>), dim3((unsigned)A.blocks), dim3(kThreads), lds, s, A);
     } else {
         // At most 2048 blocks (8 a compute unit): gamma and beta are loaded once a block.
