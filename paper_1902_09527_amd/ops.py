@@ -17,6 +17,11 @@ stride may be anything from the width up.  Every function takes ``stream``:
 work and the memory of its results belong to that stream (default: the
 current one); as with any tensor, wait for it before using results elsewhere.
 Nothing synchronizes.
+
+Gradients are calls of their own (``*_backward``); autograd records none of
+these calls, so a tensor that requires a gradient is refused while grad mode is
+on.  Call them under ``torch.no_grad()``, or in the forward and backward of a
+``torch.autograd.Function``, which run without it.
 """
 from __future__ import annotations
 
@@ -84,12 +89,17 @@ def _p(t: Optional[torch.Tensor]) -> Optional[int]:
 class _On:
     """The device and stream of one call: results and workspaces are allocated
     on that stream, and inputs made on another one are kept until it has
-    used them."""
+    used them.  Inputs that autograd would follow are refused: it cannot."""
 
     __slots__ = ("device", "stream", "inputs", "ctx")
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream],
                  inputs: Tuple[Optional[torch.Tensor], ...]):
+        if torch.is_grad_enabled():
+            for t in inputs:
+                if t is not None and t.requires_grad:
+                    raise ValueError("an input requires a gradient, and autograd does not follow this call: use "
+                                     "torch.no_grad() or a torch.autograd.Function, and the *_backward functions")
         self.device, self.stream, self.inputs, self.ctx = device, stream, inputs, None
 
     def __enter__(self) -> int:
