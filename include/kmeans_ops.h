@@ -124,6 +124,16 @@ int kmeans_norm_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
  */
 size_t kmeans_adapter_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type,
                                       int32_t backward);   /* 0 for bad sizes */
+
+/*
+ * The form that the shared product of such a call takes where its rows and
+ * weights can be read 16 bytes at a time: tiles of *tile x *tile results (256,
+ * 128 or 64; 0: the form for few rows), the contraction in *splits parts.
+ * Returns KM_OK, or KM_ERR_* for bad sizes.
+ */
+int kmeans_adapter_tile(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type, int32_t backward,
+                        int32_t* tile, int32_t* splits);
+
 int kmeans_adapter_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r,
                            int32_t type, const void* W, const void* A, const void* B, const float* scale,
                            const int32_t* ids, const int32_t* order, const int32_t* sorted_ids,

@@ -51,7 +51,7 @@ OPS_EXPORTS = (
     "kmeans_sort_workspace_bytes", "kmeans_sort_plan", "kmeans_sort_gather", "kmeans_sort_combine",
     "kmeans_sort_combine_backward",
     "kmeans_norm_forward", "kmeans_norm_workspace_bytes", "kmeans_norm_backward",
-    "kmeans_adapter_workspace_bytes", "kmeans_adapter_forward", "kmeans_adapter_backward",
+    "kmeans_adapter_workspace_bytes", "kmeans_adapter_tile", "kmeans_adapter_forward", "kmeans_adapter_backward",
 )
 
 #: Size of the static workspace of kmeans_pp_seed_noalloc (KMEANS_PP_STATIC_WORKSPACE_BYTES).
@@ -164,6 +164,8 @@ def load() -> C.CDLL:
     lib.kmeans_norm_backward.restype = C.c_int
     lib.kmeans_adapter_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32]
     lib.kmeans_adapter_workspace_bytes.restype = sz
+    lib.kmeans_adapter_tile.argtypes = [i64] + [i32] * 6 + [P, P]
+    lib.kmeans_adapter_tile.restype = C.c_int
     lib.kmeans_adapter_forward.argtypes = ([P, i64, i64] + [i32] * 5 + [P] * 4 + [P] * 4 + [P, P, P, sz, P])
     lib.kmeans_adapter_forward.restype = C.c_int
     lib.kmeans_adapter_backward.argtypes = ([P, i64, P, i64, P, i64] + [i32] * 5 + [P] * 4 + [P] * 3

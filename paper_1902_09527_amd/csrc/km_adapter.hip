@@ -1423,9 +1423,6 @@ template <class T, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
 hipError_t main_tile(MainArgs A, hipStream_t s) {
     A.tm = (int)((A.n + TM - 1) / TM);
     A.tn = (A.P + TN - 1) / TN;
-    constexpr int BK = 8 * Mma<T>::E;
-    const int all = (A.K + BK - 1) / BK, share = (all + A.splits - 1) / A.splits;
-    A.splits = (all + share - 1) / share;   // no part without a stage
     constexpr int RM = TM / WR;   // float16: the powers of two of a step, and of a later one by wave
     constexpr int lds = NS * (TM + TN) * 128 + TM * 72 + (kShifted<T> ? (TM + WR * WC * (RM < 64 ? 64 : RM)) * 4 : 0);
     static_assert(lds <= 160 * 1024, "");
@@ -1742,6 +1739,8 @@ MainShape main_shape(int64_t n, int32_t K, int32_t P, int type) {
                 best = MainShape{k.tile, splits};
             }
         }
+    const int share = (all + best.splits - 1) / best.splits;
+    best.splits = (all + share - 1) / share;   // no part without a stage
     return best;
 }
 

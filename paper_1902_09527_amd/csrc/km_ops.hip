@@ -290,6 +290,17 @@ size_t kmeans_adapter_workspace_bytes(int64_t n, int32_t din, int32_t dout, int3
     return backward || L.few ? L.bytes : adapter_plan(n, k, L.bytes).bytes;
 }
 
+int kmeans_adapter_tile(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r, int32_t type, int32_t backward,
+                        int32_t* tile, int32_t* splits) {
+    const int rc = adapter_sizes(n, din, dout, k, r, type);
+    if (rc != KM_OK) return rc;
+    if (!tile || !splits) return bad("tile or splits is null");
+    const km::AdapterShape L = km::adapter_shape(n, din, dout, k, r, type, backward != 0);
+    *tile = L.few ? 0 : L.main.tile;
+    *splits = L.few ? 1 : L.main.splits;
+    return KM_OK;
+}
+
 int kmeans_adapter_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t r,
                            int32_t type, const void* W, const void* A, const void* B, const float* scale,
                            const int32_t* ids, const int32_t* order, const int32_t* sorted_ids,
