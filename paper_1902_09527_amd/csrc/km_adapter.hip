@@ -332,8 +332,8 @@ __device__ __forceinline__ void list_chunks(const ListArgs& A, int* s) {
 // TR = false: Q_c is r x K (rows along the contraction); true: K x r, brought
 // through LDS, a wave's own part, and read transposed.  The clusters of a block
 // follow one another.  Bound by the latency of its few rounds of loads: 8192 x
-// 2048 bf16, 64 clusters, r = 16: 18 to 21 us forward, 16 backward (the rows are
-// 7 us of memory time); 16384 x 4096 float16, r = 32: 78 us.
+// 2048 bf16, 64 clusters, r = 16: 18 us forward, 15 backward (the rows are 7 us
+// of memory time); 16384 x 4096 float16, r = 32: 66 to 73 us.
 struct InnerArgs {
     const void* U;
     int64_t ldu;
@@ -473,13 +473,13 @@ __global__ __launch_bounds__(256) void k_ad_inner(InnerArgs A, ListArgs L) {
 //
 // 256 x 256 with 8 waves: the most products a byte loaded that registers and
 // LDS hold (128 accumulators a lane, 128 KB of stages).  16384 x 4096 x 8192
-// float16: 880 to 1040 us by the clock the card keeps (1.06 to 1.25 PFLOP/s; the
-// library's product alone 813 us); 8192 x 2048 x 2048 bf16: 67 to 73 us forward,
-// 69 to 75 backward (0.92 to 1.03 PFLOP/s; library 54), of which some 20 us are a
-// tile's start and end.  The matrix cores are busy 64 % of a clock that falls to
-// 1.6 GHz under this load: half of the stage loads taken out saves 8 %, L2 hits
+// float16: 880 to 1006 us by the clock the card keeps (1.09 to 1.25 PFLOP/s; the
+// library's product alone 813 us); 8192 x 2048 x 2048 bf16: 64 us forward, 64 to
+// 67 backward (1.03 to 1.07 PFLOP/s; library 54), of which some 15 us are a
+// tile's start and end.  The matrix cores are busy 66 % of a clock that falls to
+// 1.7 GHz under this load: half of the stage loads taken out saves 8 %, L2 hits
 // for all of them 6 %, so it is the card's power that is left to save.
-// float32, 100,003 x 256 x 256: 148 us (89 TFLOP/s; 8 stages a tile).
+// float32, 100,003 x 256 x 256: 143 to 150 us (90 TFLOP/s; 8 stages a tile).
 struct MainArgs {
     const void* U;
     int64_t ldu;
@@ -1173,8 +1173,10 @@ struct GradArgs {
 };
 
 // Bound by the latency of a chunk's stages: 8192 x 2048 bf16, 64 clusters, r =
-// 16: 26 us for both gradients (rows: 14 us of memory time); 100,003 x 256
-// float32: 57 us (43).
+// 16: 25 us for both gradients (rows: 14 us of memory time); 100,003 x 256
+// float32: 57 us (43).  The two parts of S take twice the LDS of one: beyond r =
+// 64 a compute unit has one block instead of two (8192 x 2048 float16, r = 128:
+// the whole backward pass 235 us, 206 with g rounded to float16).
 //
 // 128 columns a block, 32 a wave; stages of 2 KS places, loaded while the one
 // before is multiplied (the skinny operand through registers).  WF: the wide
