@@ -8,7 +8,9 @@
  *                     gradients of both;
  *   kmeans_norm_*     layer norm of rows and its gradients;
  *   kmeans_adapter_*  a shared projection with one low-rank adapter per
- *                     cluster, and the gradients of rows and adapters.
+ *                     cluster, and the gradients of rows and adapters;
+ *   kmeans_linear_*   products with one weight per cluster, and the gradients
+ *                     of rows and weights.
  *
  * Common to all.  Status codes and kmeans_mti_last_hip_error() are those of
  * kmeans_mti.h; no entry point throws, allocates device memory or
@@ -155,6 +157,34 @@ int kmeans_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t
                             const void* A, const void* B, const float* scale, const int32_t* order,
                             const int32_t* sorted_ids, const int32_t* offsets, void* dX, void* dA, void* dB,
                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Products with one weight per cluster: y = W_c x for every row x of cluster c,
+ * zeros for a row of no cluster.
+ *   X  n rows of din, ldx apart     W  k x dout x din     Y  n x dout
+ * all of one type.  The clusters come as a plan of kmeans_sort_plan with n
+ * slots: sorted_ids, offsets and order (m = 1), or order = NULL for rows that
+ * are in the plan's order already.  Requires n >= 0, din, dout, k >= 1;
+ * KM_ERR_UNSUPPORTED beyond n = 2^27, din, dout = 2^24 and some 2^31 tiles of 64
+ * rows and columns.  backward: the workspace of the backward pass, else of the
+ * forward pass.
+ */
+size_t kmeans_linear_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type,
+                                     int32_t backward);   /* 0 for bad sizes */
+int kmeans_linear_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type,
+                          const void* W, const int32_t* order, const int32_t* sorted_ids, const int32_t* offsets,
+                          void* Y, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradients of kmeans_linear_forward from dY (n rows of dout): dX = W_c^T dy
+ * (n x din, zeros for a row of no cluster) and dW_c = sum dy x^T over the
+ * cluster's rows (k x dout x din, zeros for a cluster with none).  Either may be
+ * NULL; X is read for dW alone, W for dX alone.
+ */
+int kmeans_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, int64_t n, int32_t din,
+                           int32_t dout, int32_t k, int32_t type, const void* W, const int32_t* order,
+                           const int32_t* offsets, void* dX, void* dW, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
 
 #ifdef __cplusplus
 }

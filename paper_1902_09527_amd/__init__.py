@@ -8,8 +8,10 @@ ops.py holds the operators of a layer conditioned on clusters
 """
 from .kmeans import KMeansMTI, kmeanspp, kmeanspp_workspace_bytes, run, run_pp_best  # noqa: F401
 from .ops import (ClusterPlan, adapter_linear, adapter_linear_backward, cluster_combine,  # noqa: F401
-                  cluster_combine_backward, cluster_gather, cluster_sort, layernorm, layernorm_backward)
+                  cluster_combine_backward, cluster_gather, cluster_linear, cluster_linear_backward, cluster_sort,
+                  layernorm, layernorm_backward)
 
 __all__ = ["KMeansMTI", "kmeanspp", "kmeanspp_workspace_bytes", "run", "run_pp_best",
            "ClusterPlan", "cluster_sort", "cluster_gather", "cluster_combine", "cluster_combine_backward",
-           "layernorm", "layernorm_backward", "adapter_linear", "adapter_linear_backward"]
+           "layernorm", "layernorm_backward", "adapter_linear", "adapter_linear_backward",
+           "cluster_linear", "cluster_linear_backward"]

@@ -52,6 +52,7 @@ OPS_EXPORTS = (
     "kmeans_sort_combine_backward",
     "kmeans_norm_forward", "kmeans_norm_workspace_bytes", "kmeans_norm_backward",
     "kmeans_adapter_workspace_bytes", "kmeans_adapter_tile", "kmeans_adapter_forward", "kmeans_adapter_backward",
+    "kmeans_linear_workspace_bytes", "kmeans_linear_forward", "kmeans_linear_backward",
 )
 
 #: Size of the static workspace of kmeans_pp_seed_noalloc (KMEANS_PP_STATIC_WORKSPACE_BYTES).
@@ -171,6 +172,12 @@ def load() -> C.CDLL:
     lib.kmeans_adapter_backward.argtypes = ([P, i64, P, i64, P, i64] + [i32] * 5 + [P] * 4 + [P] * 3
                                             + [P, P, P, P, sz, P])
     lib.kmeans_adapter_backward.restype = C.c_int
+    lib.kmeans_linear_workspace_bytes.argtypes = [i64] + [i32] * 5
+    lib.kmeans_linear_workspace_bytes.restype = sz
+    lib.kmeans_linear_forward.argtypes = [P, i64, i64] + [i32] * 4 + [P] * 4 + [P, P, sz, P]
+    lib.kmeans_linear_forward.restype = C.c_int
+    lib.kmeans_linear_backward.argtypes = [P, i64, P, i64, i64] + [i32] * 4 + [P] * 3 + [P, P, P, sz, P]
+    lib.kmeans_linear_backward.restype = C.c_int
     lib.kmeans_mti_last_hip_error.argtypes = []
     lib.kmeans_mti_last_hip_error.restype = C.c_char_p
     _lib = lib

@@ -10,8 +10,9 @@ namespace km {
 
 // Row types; the values are KM_F32, KM_BF16, KM_F16 of kmeans_ops.h.
 enum RowType { kF32 = 0, kBF16 = 1, kF16 = 2 };
+constexpr int kF8 = 3;   // e4m3 values with a scale for each 128 (in the grouped products alone)
 
-inline size_t row_type_bytes(int t) { return t == kF32 ? 4 : 2; }
+inline size_t row_type_bytes(int t) { return t == kF32 ? 4 : t == kF8 ? 1 : 2; }
 
 // V elements moved by one load or store.
 template <class T, int V>
@@ -160,5 +161,38 @@ struct AdapterShape {
 AdapterShape adapter_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int32_t r, int type, bool backward);
 hipError_t launch_adapter_forward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s);
 hipError_t launch_adapter_backward(const AdapterArgs& D, char* ws, const AdapterShape& L, int type, hipStream_t s);
+
+// ---- products grouped by cluster (km_group.hip)
+
+constexpr int kGroupFew = 64;   // rows up to which the forward pass takes the form for few rows
+
+struct GroupItem {
+    int32_t c, p0, p1, slot;   // places p0 .. p1 of cluster c; slot: partial sum to write, -1: the result itself
+};
+struct GroupArgs {
+    const void *X, *dY;
+    int64_t ldx, lddy, n;
+    int32_t di, dout, k;
+    const void* W;                            // k x dout x di
+    const uint8_t *XE, *WE;                   // 8 bits: the scales' bytes
+    const int32_t *order, *sids, *offsets;    // the plan; order null: rows are in its order
+    void *Y, *dX, *dW;                        // dX, dW: either may be null
+};
+// A list of items of at most `size` places.
+struct GroupList {
+    int32_t size;
+    int64_t max_items;
+    size_t off_count, off_items, off_first;   // workspace segments
+};
+struct GroupShape {
+    int32_t few, grad_tile;
+    GroupList rows, cuts;
+    size_t off_part, bytes;
+};
+int64_t group_items(int64_t n, int32_t k, int32_t size);   // most items that n places are cut into
+GroupShape group_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int type, bool backward);
+hipError_t launch_group_forward(const GroupArgs& D, char* ws, const GroupShape& L, int type, int out_type,
+                                hipStream_t s);
+hipError_t launch_group_backward(const GroupArgs& D, char* ws, const GroupShape& L, int type, hipStream_t s);
 
 }  // namespace km

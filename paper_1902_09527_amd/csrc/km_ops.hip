@@ -423,4 +423,110 @@ int kmeans_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t
                 "kmeans_adapter_backward");
 }
 
+static int linear_sizes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type) {
+    if (!slots_ok(n, 1, k) || din < 1 || dout < 1 || !type_ok(type)) return bad("n, din, dout, k or type out of range");
+    if (n > (int64_t)1 << 27 || din > 1 << 24 || dout > 1 << 24)
+        return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^27 rows or 2^24 columns");
+    if (!rows_ok(n, din, din) || !rows_ok(n, dout, dout) || !rows_ok((int64_t)k * dout, din, din))
+        return bad("sizes within 63 bits needed");
+    // The grids: tiles of 64 rows and columns at least.
+    const int64_t wide = (din > dout ? din : dout) / 64 + 1, most = INT32_MAX / wide;
+    if (km::group_items(n, k, 64) + 1 >= most || km::group_items(n, k, 256) >= most / (din / 128 + 1) / 2)
+        return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^31 tiles");
+    return KM_OK;
+}
+
+// The plan of a grouped product, checked.
+static void check_group(Checks& C, const int32_t* order, const int32_t* sids, const int32_t* offsets, int64_t n,
+                        int32_t k) {
+    if (order) C.array(order, (size_t)n * 4, "order");
+    if (sids) C.array(sids, (size_t)n * 4, "sorted_ids");
+    C.array(offsets, ((size_t)k + 1) * 4, "offsets");
+}
+
+size_t kmeans_linear_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type, int32_t backward) {
+    if (linear_sizes(n, din, dout, k, type) != KM_OK) return 0;
+    return km::group_shape(n, din, dout, k, type, backward != 0).bytes;
+}
+
+int kmeans_linear_forward(const void* X, int64_t ldx, int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type,
+                          const void* W, const int32_t* order, const int32_t* sorted_ids, const int32_t* offsets,
+                          void* Y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = linear_sizes(n, din, dout, k, type);
+    if (rc != KM_OK) return rc;
+    if (!rows_ok(n, din, ldx)) return bad("ldx >= din needed, and sizes within 63 bits");
+    if (!W) return bad("W is null");
+    if (n > 0 && (!X || !Y || !sorted_ids || !offsets)) return bad("X, Y, sorted_ids or offsets is null");
+    const km::GroupShape L = km::group_shape(n, din, dout, k, type, false);
+    if ((rc = workspace_ok(workspace, workspace_bytes, L.bytes)) != KM_OK) return rc;
+    if (n == 0) return KM_OK;
+    const size_t es = km::row_type_bytes(type);
+    Checks C;
+    C.rows(X, n, din, ldx, type, "X");
+    C.array(W, (size_t)k * din * dout * es, "W");
+    check_group(C, order, sorted_ids, offsets, n, k);
+    C.array(Y, (size_t)n * dout * es, "Y");
+    C.array(workspace, L.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    km::GroupArgs D{};
+    D.X = X;
+    D.ldx = ldx;
+    D.n = n;
+    D.di = din;
+    D.dout = dout;
+    D.k = k;
+    D.W = W;
+    D.order = order;
+    D.sids = sorted_ids;
+    D.offsets = offsets;
+    D.Y = Y;
+    return done(km::launch_group_forward(D, static_cast<char*>(workspace), L, type, type,
+                                         static_cast<hipStream_t>(hip_stream)),
+                "kmeans_linear_forward");
+}
+
+int kmeans_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, int64_t n, int32_t din,
+                           int32_t dout, int32_t k, int32_t type, const void* W, const int32_t* order,
+                           const int32_t* offsets, void* dX, void* dW, void* workspace, size_t workspace_bytes,
+                           void* hip_stream) {
+    int rc = linear_sizes(n, din, dout, k, type);
+    if (rc != KM_OK) return rc;
+    if ((dW && !rows_ok(n, din, ldx)) || !rows_ok(n, dout, lddy)) return bad("ldx >= din and lddy >= dout needed");
+    if (!offsets || (dX && !W)) return bad("offsets or W is null");
+    if (n > 0 && (!dY || (dW && !X))) return bad("dY or X is null");
+    const km::GroupShape L = km::group_shape(n, din, dout, k, type, true);
+    if ((rc = workspace_ok(workspace, workspace_bytes, L.bytes)) != KM_OK) return rc;
+    const size_t es = km::row_type_bytes(type);
+    Checks C;
+    C.rows(dY, n, dout, lddy, type, "dY");
+    if (dW) {
+        C.rows(X, n, din, ldx, type, "X");
+        C.array(dW, (size_t)k * din * dout * es, "dW");
+    }
+    if (dX) {
+        C.array(W, (size_t)k * din * dout * es, "W");
+        C.array(dX, (size_t)n * din * es, "dX");
+    }
+    check_group(C, order, nullptr, offsets, n, k);
+    C.array(workspace, L.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    km::GroupArgs D{};
+    D.dY = dY;
+    D.lddy = lddy;
+    D.X = X;
+    D.ldx = ldx;
+    D.n = n;
+    D.di = din;
+    D.dout = dout;
+    D.k = k;
+    D.W = W;
+    D.order = order;
+    D.offsets = offsets;
+    D.dX = dX;
+    D.dW = dW;
+    return done(km::launch_group_backward(D, static_cast<char*>(workspace), L, type,
+                                          static_cast<hipStream_t>(hip_stream)),
+                "kmeans_linear_backward");
+}
+
 }  // extern "C"

@@ -8,7 +8,9 @@ tokens of a model, embeddings -- to small experts of their clusters:
   layernorm, layernorm_backward
       the normalisation in front of them;
   adapter_linear, adapter_linear_backward
-      a shared projection with one low-rank adapter per cluster.
+      a shared projection with one low-rank adapter per cluster;
+  cluster_linear, cluster_linear_backward
+      products with one weight per cluster.
 
 As in :mod:`.kmeans`, this is argument marshalling only: tensors are checked
 and handed to the kernels of ``libkmeans_mti.so``.  Rows are float32, bfloat16
@@ -388,3 +390,69 @@ def adapter_linear_backward(dY: torch.Tensor, X: torch.Tensor, H: torch.Tensor, 
                                          _p(plan.offsets), _p(dx), _p(da), _p(db), _p(ws), ws.numel(), s)
     N.check(st, "kmeans_adapter_backward")
     return dx, da, db
+
+
+def _experts(X: torch.Tensor, W: torch.Tensor) -> Tuple[int, int, int]:
+    """Check the weights of a product by cluster; (din, dout, k)."""
+    if not isinstance(W, torch.Tensor) or W.dim() != 3 or W.numel() == 0:
+        _gpu(W, "W", X.device)
+        raise ValueError("W must be a non-empty 3-D tensor")
+    k, dout, din = W.shape
+    if X.shape[1] != din:
+        raise ValueError("X must have %d columns" % din)
+    _array(W, "W", X.dtype, (k, dout, din), X.device)
+    return din, dout, k
+
+
+def _linear_workspace(n: int, din: int, dout: int, k: int, type_: int, backward: int) -> int:
+    need = N.load().kmeans_linear_workspace_bytes(n, din, dout, k, type_, backward)
+    if need == 0:
+        raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_linear_workspace_bytes",
+                        "up to 2^27 rows, 2^24 columns and 2^31 tiles of 64 rows and columns")
+    return need
+
+
+def cluster_linear(X: torch.Tensor, W: torch.Tensor, plan: ClusterPlan, sorted_rows: bool = False,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Products with one weight per cluster (kmeans_linear_forward): y = W[c] x
+    for a row x of cluster c, zeros for a row in no cluster; [n, dout].
+
+    W [k, dout, din] and X are of one type.  ``plan``: a plan of one slot a row
+    (``cluster_sort`` of [n] ids), or, with ``sorted_rows``, any plan in whose
+    order X is (the output of :func:`cluster_gather`); results come in X's order.
+    """
+    ld = _rows(X, "X")
+    din, dout, k = _experts(X, W)
+    n, dev = X.shape[0], X.device
+    order = _places(plan, n, k, dev, sorted_rows)
+    need = _linear_workspace(n, din, dout, k, _TYPES[X.dtype], 0)
+    with _On(dev, stream, (X, W, order, plan.sorted_ids, plan.offsets)) as s:
+        y = X.new_empty((n, dout))
+        ws = _workspace(need, dev, "kmeans_linear_workspace_bytes")
+        st = N.load().kmeans_linear_forward(_p(X), ld, n, din, dout, k, _TYPES[X.dtype], _p(W), _p(order),
+                                            _p(plan.sorted_ids), _p(plan.offsets), _p(y), _p(ws), ws.numel(), s)
+    N.check(st, "kmeans_linear_forward")
+    return y
+
+
+def cluster_linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, plan: ClusterPlan,
+                            sorted_rows: bool = False, need_dX: bool = True, need_dW: bool = True,
+                            stream: Optional[torch.cuda.Stream] = None
+                            ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients of :func:`cluster_linear` (kmeans_linear_backward): (dX, dW), of
+    the rows' type; zeros for rows in no cluster and clusters with no rows.  One
+    that is not needed (``need_dX``, ``need_dW``) is None and not computed."""
+    ld = _rows(X, "X")
+    din, dout, k = _experts(X, W)
+    n, dev = X.shape[0], X.device
+    ldy = _rows(dY, "dY", like=X, n=n, d=dout)
+    order = _places(plan, n, k, dev, sorted_rows)
+    need = _linear_workspace(n, din, dout, k, _TYPES[X.dtype], 1)
+    with _On(dev, stream, (dY, X, W, order, plan.offsets)) as s:
+        dx = X.new_empty((n, din)) if need_dX else None
+        dw = torch.empty_like(W) if need_dW else None
+        ws = _workspace(need, dev, "kmeans_linear_workspace_bytes")
+        st = N.load().kmeans_linear_backward(_p(dY), ldy, _p(X), ld, n, din, dout, k, _TYPES[X.dtype], _p(W), _p(order),
+                                             _p(plan.offsets), _p(dx), _p(dw), _p(ws), ws.numel(), s)
+    N.check(st, "kmeans_linear_backward")
+    return dx, dw
