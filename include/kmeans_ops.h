@@ -10,7 +10,10 @@
  *   kmeans_adapter_*  a shared projection with one low-rank adapter per
  *                     cluster, and the gradients of rows and adapters;
  *   kmeans_linear_*   products with one weight per cluster, and the gradients
- *                     of rows and weights.
+ *                     of rows and weights;
+ *   kmeans_fp8_*      rows in 8-bit floating point with a scale for each 128
+ *                     elements, and products of them with one weight per
+ *                     cluster.
  *
  * Common to all.  Status codes and kmeans_mti_last_hip_error() are those of
  * kmeans_mti.h; no entry point throws, allocates device memory or
@@ -37,6 +40,8 @@ extern "C" {
 
 /* Types of rows. */
 enum { KM_F32 = 0, KM_BF16 = 1, KM_F16 = 2 };
+/* e4m3 values (1 sign, 4 exponent, 3 mantissa bits, largest 448, one NaN): kmeans_fp8_forward alone. */
+enum { KM_E4M3 = 3 };
 
 /*
  * The plan that sorts rows by cluster.  ids: n x m int32, row i's m clusters
@@ -185,6 +190,32 @@ int kmeans_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t 
                            int32_t dout, int32_t k, int32_t type, const void* W, const int32_t* order,
                            const int32_t* offsets, void* dX, void* dW, void* workspace, size_t workspace_bytes,
                            void* hip_stream);
+
+/*
+ * Rows in 8-bit floating point.  Of each 128 elements of a row (the last ones
+ * fewer), a being the largest finite magnitude: e = max(-126, the least whole
+ * number with a <= 448 2^e), exponents = e + 127 (n x ceil(d / 128) bytes),
+ * values = x 2^-e rounded to the nearest e4m3 value, ties to even (n x d
+ * bytes); infinities and NaN become NaN.  dequantize: X = values 2^e, rounded to
+ * its type.  Requires 0 <= n <= 2^40, d >= 1.
+ */
+int kmeans_fp8_quantize(const void* X, int64_t ldx, int64_t n, int32_t d, int32_t type, void* values,
+                        uint8_t* exponents, void* hip_stream);
+int kmeans_fp8_dequantize(const void* values, const uint8_t* exponents, int64_t n, int32_t d, int32_t type, void* X,
+                          void* hip_stream);
+
+/*
+ * kmeans_linear_forward with both operands in 8 bits: y = sum of the products of
+ * the values that they stand for, in float32, rounded to y_type (KM_F32, KM_BF16
+ * or KM_F16).  W: k x dout x din values with k x dout x ceil(din / 128)
+ * exponents.  X: of type KM_E4M3 with its exponents (n x ceil(din / 128) bytes),
+ * or of another type with exponents = NULL: quantised in the workspace.
+ */
+size_t kmeans_fp8_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type);   /* 0 for bad sizes */
+int kmeans_fp8_forward(const void* X, int64_t ldx, const uint8_t* exponents, int64_t n, int32_t din, int32_t dout,
+                       int32_t k, int32_t type, const void* W, const uint8_t* w_exponents, const int32_t* order,
+                       const int32_t* sorted_ids, const int32_t* offsets, void* Y, int32_t y_type, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

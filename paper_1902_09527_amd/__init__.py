@@ -7,11 +7,12 @@ ops.py holds the operators of a layer conditioned on clusters
 (include/kmeans_ops.h).
 """
 from .kmeans import KMeansMTI, kmeanspp, kmeanspp_workspace_bytes, run, run_pp_best  # noqa: F401
-from .ops import (ClusterPlan, adapter_linear, adapter_linear_backward, cluster_combine,  # noqa: F401
-                  cluster_combine_backward, cluster_gather, cluster_linear, cluster_linear_backward, cluster_sort,
-                  layernorm, layernorm_backward)
+from .ops import (BlockRows, ClusterPlan, adapter_linear, adapter_linear_backward, cluster_combine,  # noqa: F401
+                  cluster_combine_backward, cluster_gather, cluster_linear, cluster_linear_backward,
+                  cluster_linear_fp8, cluster_sort, dequantize_blocks, quantize_blocks, layernorm, layernorm_backward)
 
 __all__ = ["KMeansMTI", "kmeanspp", "kmeanspp_workspace_bytes", "run", "run_pp_best",
            "ClusterPlan", "cluster_sort", "cluster_gather", "cluster_combine", "cluster_combine_backward",
            "layernorm", "layernorm_backward", "adapter_linear", "adapter_linear_backward",
-           "cluster_linear", "cluster_linear_backward"]
+           "cluster_linear", "cluster_linear_backward",
+           "BlockRows", "quantize_blocks", "dequantize_blocks", "cluster_linear_fp8"]

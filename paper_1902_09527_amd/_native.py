@@ -45,6 +45,7 @@ EXPORTS = (
 KM_F32 = 0
 KM_BF16 = 1
 KM_F16 = 2
+KM_E4M3 = 3
 
 #: Every symbol include/kmeans_ops.h declares.
 OPS_EXPORTS = (
@@ -53,6 +54,7 @@ OPS_EXPORTS = (
     "kmeans_norm_forward", "kmeans_norm_workspace_bytes", "kmeans_norm_backward",
     "kmeans_adapter_workspace_bytes", "kmeans_adapter_tile", "kmeans_adapter_forward", "kmeans_adapter_backward",
     "kmeans_linear_workspace_bytes", "kmeans_linear_forward", "kmeans_linear_backward",
+    "kmeans_fp8_quantize", "kmeans_fp8_dequantize", "kmeans_fp8_workspace_bytes", "kmeans_fp8_forward",
 )
 
 #: Size of the static workspace of kmeans_pp_seed_noalloc (KMEANS_PP_STATIC_WORKSPACE_BYTES).
@@ -178,6 +180,14 @@ def load() -> C.CDLL:
     lib.kmeans_linear_forward.restype = C.c_int
     lib.kmeans_linear_backward.argtypes = [P, i64, P, i64, i64] + [i32] * 4 + [P] * 3 + [P, P, P, sz, P]
     lib.kmeans_linear_backward.restype = C.c_int
+    lib.kmeans_fp8_quantize.argtypes = [P, i64, i64, i32, i32, P, P, P]
+    lib.kmeans_fp8_quantize.restype = C.c_int
+    lib.kmeans_fp8_dequantize.argtypes = [P, P, i64, i32, i32, P, P]
+    lib.kmeans_fp8_dequantize.restype = C.c_int
+    lib.kmeans_fp8_workspace_bytes.argtypes = [i64] + [i32] * 4
+    lib.kmeans_fp8_workspace_bytes.restype = sz
+    lib.kmeans_fp8_forward.argtypes = [P, i64, P, i64] + [i32] * 4 + [P] * 6 + [i32, P, sz, P]
+    lib.kmeans_fp8_forward.restype = C.c_int
     lib.kmeans_mti_last_hip_error.argtypes = []
     lib.kmeans_mti_last_hip_error.restype = C.c_char_p
     _lib = lib

@@ -22,7 +22,8 @@ SOURCES = [os.path.join(CSRC, "km_kernels.hip"), os.path.join(CSRC, "km_large.hi
            os.path.join(CSRC, "km_gen.hip"),
            os.path.join(CSRC, "km_sort.hip"), os.path.join(CSRC, "km_norm.hip"),
            os.path.join(CSRC, "km_adapter.hip"),
-           os.path.join(CSRC, "km_group.hip"), os.path.join(CSRC, "km_ops.hip"),
+           os.path.join(CSRC, "km_group.hip"), os.path.join(CSRC, "km_fp8.hip"),
+           os.path.join(CSRC, "km_ops.hip"),
            os.path.join(CSRC, "km_host.hip")]
 ARCH = "gfx950"
 

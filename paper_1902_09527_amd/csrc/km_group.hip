@@ -25,7 +25,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // What an operand of R rows (or columns) by 64 bytes of the contraction is for a
 // lane, and the product of two: D[m][n] += sum_k first[m][k] second[n][k].  A
 // lane holds runs of four m of its column n = lane % R.
-template <class T>
+// The results' type O matters for 8 bits alone.
+template <class T, class O>
 struct Op {
     static constexpr int R = 16, E = Mma<T>::E;
     using Acc = f32x4;
@@ -40,12 +41,17 @@ struct Op {
         return Mma<T>::mma(a.v, b.v, c);
     }
     static constexpr int kRuns = 1;
-    static __device__ __forceinline__ int run(int j, int lane) { return (lane >> 4) * 4; }   // first m of run j
+    static __device__ __forceinline__ int run(int, int lane) { return (lane >> 4) * 4; }   // first m of run j
 };
 // e4m3 values: 64 of a row, two chunks a lane.  The scale of 64 elements comes as
 // a byte (2^(byte - 127)) of the lane's row; a matrix step takes one for each 32.
-template <>
-struct Op<uint8_t> {
+// The step adds its products to float32 accumulators, but of each 8 consecutive
+// ones it drops the bits more than 13 below the largest one's exponent (measured,
+// one pair of products at a time): 1.3e-5 of the norm of products of 4096 normal
+// values.  That is below a hundredth of a bfloat16 result's own rounding and a
+// tenth of a float16 one's; float32 results take the next form.
+template <class O>
+struct Op<uint8_t, O> {
     static constexpr int R = 32, E = 16;
     using Acc = f32x16;
     struct Frag {
@@ -64,10 +70,45 @@ struct Op<uint8_t> {
     static __device__ __forceinline__ int run(int j, int lane) { return j * 8 + (lane >> 5) * 4; }
 };
 
+// Eight e4m3 values times 2^(byte - 127) as bfloat16, which holds them exactly.
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, int byte) {
+    const float scale = __builtin_bit_cast(float, byte > 0 ? (uint32_t)byte << 23 : 0x400000u);
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    struct Four {
+        bf16x2 v[4];
+    } o{{__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
+         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
+         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)}};
+    return __builtin_bit_cast(u32x4, o);
+}
+// e4m3 values with float32 results: widened to bfloat16, whose products and sums
+// keep float32.  A chunk is the operand of two steps.
+template <>
+struct Op<uint8_t, float> {
+    static constexpr int R = 16, E = 16;
+    using Acc = f32x4;
+    struct Frag {
+        u32x4 v;
+    };
+    static __device__ __forceinline__ int chunk(int lane) { return lane >> 4; }
+    static __device__ __forceinline__ Frag read(const char* buf, int at) {
+        return {*reinterpret_cast<const u32x4*>(buf + at)};
+    }
+    static __device__ __forceinline__ Acc mma(const Frag& a, const Frag& b, Acc c, int sa, int sb) {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2)
+            c = Mma<__bf16>::mma(widen(a.v[i], a.v[i + 1], sa), widen(b.v[i], b.v[i + 1], sb), c);
+        return c;
+    }
+    static constexpr int kRuns = 1;
+    static __device__ __forceinline__ int run(int, int lane) { return (lane >> 4) * 4; }
+};
+
 // 16 bytes of a row from element k0 on, zero past its K elements, at any address.
 template <class T>
 __device__ __forceinline__ u32x4 chunk_any(const T* row, int64_t k0, int64_t K) {
-    constexpr int E = Op<T>::E;
+    constexpr int E = 16 / (int)sizeof(T);
     if (k0 + E <= K) {
         u32x4 v;
         __builtin_memcpy(&v, row + k0, 16);
@@ -160,7 +201,7 @@ constexpr int kWindow = 32;   // stages whose scales are in LDS
 // past them.
 template <class T, class O, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
 __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
-    using P = Op<T>;
+    using P = Op<T, O>;
     constexpr bool F8 = sizeof(T) == 1;
     constexpr int E = P::E, R = P::R, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
     constexpr int FR = TM / WR / R, FC = TN / WC / R;
@@ -656,31 +697,35 @@ struct FewArgs {
 
 // 16 columns and the places of one cluster a block, from the place blockIdx.y on
 // if a cluster starts there; its 16 waves share the contraction.
-template <class T>
+template <class T, class O>
 struct FewOp {
     static constexpr int kBytes = 16;   // of a row a lane and step
-    struct Frag {
-        u32x4 v;
-    };
-    static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, int, int) {
-        return Mma<T>::mma(a.v, b.v, c);
+    using Frag = typename Op<T, O>::Frag;
+    static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, int sa, int sb) {
+        return Op<T, O>::mma(a, b, c, sa, sb);
     }
 };
-template <>
-struct FewOp<uint8_t> {
+template <class O>
+struct FewOp<uint8_t, O> {
     static constexpr int kBytes = 32;
-    struct Frag {
-        u32x4 v, w;
-    };
+    using Frag = typename Op<uint8_t, O>::Frag;
     static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, int sa, int sb) {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, a),
                                                                 __builtin_bit_cast(i32x8, b), c, 0, 0, 0, sa, 0, sb);
     }
 };
+template <>
+struct FewOp<uint8_t, float> {
+    static constexpr int kBytes = 16;
+    using Frag = Op<uint8_t, float>::Frag;
+    static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, int sa, int sb) {
+        return Op<uint8_t, float>::mma(a, b, c, sa, sb);
+    }
+};
 
 template <class T, class O, bool AL, int RF>
 __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int rows, f32x4 (*s_red)[4][64]) {
-    using P = FewOp<T>;
+    using P = FewOp<T, O>;
     constexpr bool F8 = sizeof(T) == 1;
     constexpr int EL = P::kBytes / (int)sizeof(T), KS = 4 * EL, NWAVE = 16;   // elements a lane, of a step
     constexpr int UN = !AL ? 1 : RF <= 2 ? 4 : 2;
@@ -704,19 +749,14 @@ __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int r
     for (int f = 0; f < RF; ++f) acc[f] = f32x4{0, 0, 0, 0};
     auto get = [&](const T* row, int64_t k0) {
         typename P::Frag o;
-        if constexpr (F8) {
-            if constexpr (AL) {
-                o.v = *(k0 < A.K ? reinterpret_cast<const u32x4*>(row + k0) : reinterpret_cast<const u32x4*>(zero_chunk));
+        if constexpr (AL) {
+            o.v = *(k0 < A.K ? reinterpret_cast<const u32x4*>(row + k0) : reinterpret_cast<const u32x4*>(zero_chunk));
+            if constexpr (P::kBytes == 32)
                 o.w = *(k0 + 16 < A.K ? reinterpret_cast<const u32x4*>(row + k0 + 16)
                                       : reinterpret_cast<const u32x4*>(zero_chunk));
-            } else {
-                o.v = chunk_any(row, k0, A.K);
-                o.w = chunk_any(row, k0 + 16, A.K);
-            }
-        } else if constexpr (AL) {
-            o.v = chunk_aligned(row, k0, A.K);
         } else {
             o.v = chunk_any(row, k0, A.K);
+            if constexpr (P::kBytes == 32) o.w = chunk_any(row, k0 + 16, A.K);
         }
         return o;
     };
@@ -730,8 +770,8 @@ __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int r
             a[y] = get(w, k0);
 #pragma unroll
             for (int f = 0; f < RF; ++f) b[y][f] = get(x[f], k0);
-            if constexpr (F8) {
-                const int e = s + y < A.nb ? s + y : 0;
+            if constexpr (F8) {   // KS: 64 or 128
+                const int at = (s + y) / (128 / KS), e = at < A.nb ? at : 0;
                 sa[y] = we[e];
 #pragma unroll
                 for (int f = 0; f < RF; ++f) sb[y][f] = xe[f][e];
@@ -804,11 +844,20 @@ hipError_t main_tile(MainArgs A, int64_t max_items, hipStream_t s) {
     return hipGetLastError();
 }
 
+// 8 bits with float32 results: widened operands take the registers of the larger
+// tiles, so there is one form at any address.
+template <class T, class O>
+constexpr bool kWide = sizeof(T) == 1 && sizeof(O) == 4;
+
 template <class T, class O, bool TR>
 hipError_t main_go(const MainArgs& A, const GroupList& L, bool al, hipStream_t s) {
+    if constexpr (kWide<T, O>) {
+        return main_tile<T, O, 128, 128, 2, 2, 2, TR, false>(A, L.max_items, s);
+    } else {
     if (!al) return main_tile<T, O, 128, 128, 2, 2, 2, TR, false>(A, L.max_items, s);
     if (L.size == 256) return main_tile<T, O, 256, 256, 2, 4, 2, TR, true>(A, L.max_items, s);
     return main_tile<T, O, 64, 64, 2, 2, 2, TR, true>(A, L.max_items, s);
+    }
 }
 
 // The list of row tiles as the launch takes it: tiles of 128 rows where rows or
@@ -851,7 +900,7 @@ hipError_t lists_go(const GroupArgs& D, const GroupList* rows, const GroupList* 
 
 template <class T, class O>
 hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStream_t s) {
-    const bool al = rows16<T>(D.X, D.ldx, D.di) && D.di % Op<T>::E == 0 && a16(D.W);
+    const bool al = rows16<T>(D.X, D.ldx, D.di) && D.di % (16 / (int)sizeof(T)) == 0 && a16(D.W);
     const int32_t y4 = D.dout % 4 == 0 && a16(D.Y);
     if (L.few) {
         FewArgs F{};
@@ -875,7 +924,7 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
         else hipLaunchKernelGGL((k_gr_few<T, O, false>), g, b, 0, s, F);
         return hipGetLastError();
     }
-    const GroupList rows = row_list(D, L.rows, al);
+    const GroupList rows = row_list(D, L.rows, al && !kWide<T, O>);
     const hipError_t e = lists_go(D, &rows, nullptr, ws, s);
     if (e != hipSuccess) return e;
     const ListArgs Q = list_args(D, rows, ws, false);

@@ -195,4 +195,12 @@ hipError_t launch_group_forward(const GroupArgs& D, char* ws, const GroupShape& 
                                 hipStream_t s);
 hipError_t launch_group_backward(const GroupArgs& D, char* ws, const GroupShape& L, int type, hipStream_t s);
 
+// ---- rows in 8 bits (km_fp8.hip)
+
+// Q: n rows of dq >= d values (zeros past d), ldq bytes apart; E: a byte for each 128.
+hipError_t launch_quantize(const void* X, int64_t ldx, int64_t n, int32_t d, int type, uint8_t* Q, int64_t ldq,
+                           int32_t dq, uint8_t* E, hipStream_t s);
+hipError_t launch_dequantize(const uint8_t* Q, const uint8_t* E, int64_t n, int32_t d, int type, void* X,
+                             hipStream_t s);
+
 }  // namespace km

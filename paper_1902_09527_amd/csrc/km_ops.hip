@@ -529,4 +529,112 @@ int kmeans_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t 
                 "kmeans_linear_backward");
 }
 
+static bool blocks_ok(int64_t n, int32_t d) { return rows_ok(n, d, d) && n <= (int64_t)1 << 40; }
+static size_t block_bytes(int64_t n, int32_t d) { return (size_t)n * ((d + (int64_t)127) / 128); }
+
+int kmeans_fp8_quantize(const void* X, int64_t ldx, int64_t n, int32_t d, int32_t type, void* values,
+                        uint8_t* exponents, void* hip_stream) {
+    if (!type_ok(type)) return bad("a type of KM_F32, KM_BF16 or KM_F16 needed");
+    if (!rows_ok(n, d, ldx) || !blocks_ok(n, d)) return bad("n >= 0, d >= 1, ldx >= d needed, and n up to 2^40");
+    if (n == 0) return KM_OK;
+    if (!X || !values || !exponents) return bad("X, values or exponents is null");
+    Checks C;
+    C.rows(X, n, d, ldx, type, "X");
+    C.array(values, (size_t)n * d, "values");
+    C.array(exponents, block_bytes(n, d), "exponents");
+    if (C.rc != KM_OK) return C.rc;
+    return done(km::launch_quantize(X, ldx, n, d, type, static_cast<uint8_t*>(values), d, d, exponents,
+                                    static_cast<hipStream_t>(hip_stream)),
+                "kmeans_fp8_quantize");
+}
+
+int kmeans_fp8_dequantize(const void* values, const uint8_t* exponents, int64_t n, int32_t d, int32_t type, void* X,
+                          void* hip_stream) {
+    if (!type_ok(type)) return bad("a type of KM_F32, KM_BF16 or KM_F16 needed");
+    if (!blocks_ok(n, d)) return bad("n >= 0 and d >= 1 needed, and n up to 2^40");
+    if (n == 0) return KM_OK;
+    if (!X || !values || !exponents) return bad("X, values or exponents is null");
+    Checks C;
+    C.array(X, (size_t)n * d * km::row_type_bytes(type), "X");
+    C.array(values, (size_t)n * d, "values");
+    C.array(exponents, block_bytes(n, d), "exponents");
+    if (C.rc != KM_OK) return C.rc;
+    return done(km::launch_dequantize(static_cast<const uint8_t*>(values), exponents, n, d, type, X,
+                                      static_cast<hipStream_t>(hip_stream)),
+                "kmeans_fp8_dequantize");
+}
+
+// Workspace of a product in 8 bits: the product's own, then rows quantised in the call.
+struct Fp8Plan {
+    km::GroupShape L;
+    int32_t dq;
+    size_t off_q, off_e, bytes;
+};
+static Fp8Plan fp8_plan(int64_t n, int32_t din, int32_t dout, int32_t k, bool quantize) {
+    Fp8Plan P{};
+    P.L = km::group_shape(n, din, dout, k, km::kF8, false);
+    P.dq = (din + 15) / 16 * 16;
+    P.off_q = P.L.bytes;
+    P.off_e = P.off_q + (quantize ? ((size_t)n * P.dq + 255) / 256 * 256 : 0);
+    P.bytes = P.off_e + (quantize ? (block_bytes(n, din) + 255) / 256 * 256 : 0);
+    return P;
+}
+
+size_t kmeans_fp8_workspace_bytes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t type) {
+    if (type != KM_E4M3 && !type_ok(type)) return 0;
+    if (linear_sizes(n, din, dout, k, KM_F32) != KM_OK) return 0;
+    return fp8_plan(n, din, dout, k, type != KM_E4M3).bytes;
+}
+
+int kmeans_fp8_forward(const void* X, int64_t ldx, const uint8_t* exponents, int64_t n, int32_t din, int32_t dout,
+                       int32_t k, int32_t type, const void* W, const uint8_t* w_exponents, const int32_t* order,
+                       const int32_t* sorted_ids, const int32_t* offsets, void* Y, int32_t y_type, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+    int rc = linear_sizes(n, din, dout, k, KM_F32);
+    if (rc != KM_OK) return rc;
+    const bool quantize = type != KM_E4M3;
+    if ((quantize && !type_ok(type)) || !type_ok(y_type)) return bad("type or y_type out of range");
+    if (!rows_ok(n, din, ldx)) return bad("ldx >= din needed, and sizes within 63 bits");
+    if (!W || !w_exponents) return bad("W or w_exponents is null");
+    if (n > 0 && (!X || !Y || !sorted_ids || !offsets || (!quantize && !exponents)))
+        return bad("X, exponents, Y, sorted_ids or offsets is null");
+    const Fp8Plan P = fp8_plan(n, din, dout, k, quantize);
+    if ((rc = workspace_ok(workspace, workspace_bytes, P.bytes)) != KM_OK) return rc;
+    if (n == 0) return KM_OK;
+    Checks C;
+    C.rows(X, n, din, ldx, quantize ? type : km::kF8, "X");
+    if (!quantize) C.array(exponents, block_bytes(n, din), "exponents");
+    C.array(W, (size_t)k * dout * din, "W");
+    C.array(w_exponents, block_bytes((int64_t)k * dout, din), "w_exponents");
+    check_group(C, order, sorted_ids, offsets, n, k);
+    C.array(Y, (size_t)n * dout * km::row_type_bytes(y_type), "Y");
+    C.array(workspace, P.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    char* ws = static_cast<char*>(workspace);
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    km::GroupArgs D{};
+    D.X = X;
+    D.ldx = ldx;
+    D.XE = exponents;
+    if (quantize) {
+        uint8_t *q = reinterpret_cast<uint8_t*>(ws + P.off_q), *e = reinterpret_cast<uint8_t*>(ws + P.off_e);
+        const hipError_t err = km::launch_quantize(X, ldx, n, din, type, q, P.dq, P.dq, e, st);
+        if (err != hipSuccess) return km::ops_hip_error(err, "kmeans_fp8_forward");
+        D.X = q;
+        D.ldx = P.dq;
+        D.XE = e;
+    }
+    D.n = n;
+    D.di = din;
+    D.dout = dout;
+    D.k = k;
+    D.W = W;
+    D.WE = w_exponents;
+    D.order = order;
+    D.sids = sorted_ids;
+    D.offsets = offsets;
+    D.Y = Y;
+    return done(km::launch_group_forward(D, ws, P.L, km::kF8, y_type, st), "kmeans_fp8_forward");
+}
+
 }  // extern "C"

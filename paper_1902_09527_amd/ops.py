@@ -10,7 +10,10 @@ tokens of a model, embeddings -- to small experts of their clusters:
   adapter_linear, adapter_linear_backward
       a shared projection with one low-rank adapter per cluster;
   cluster_linear, cluster_linear_backward
-      products with one weight per cluster.
+      products with one weight per cluster;
+  quantize_blocks, dequantize_blocks, cluster_linear_fp8
+      rows in 8 bits with a scale for each 128 elements, and their products
+      with one weight per cluster.
 
 As in :mod:`.kmeans`, this is argument marshalling only: tensors are checked
 and handed to the kernels of ``libkmeans_mti.so``.  Rows are float32, bfloat16
@@ -456,3 +459,113 @@ def cluster_linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, 
                                              _p(plan.offsets), _p(dx), _p(dw), _p(ws), ws.numel(), s)
     N.check(st, "kmeans_linear_backward")
     return dx, dw
+
+
+_E4M3 = torch.float8_e4m3fn
+
+
+class BlockRows:
+    """Rows in 8-bit floating point (made by :func:`quantize_blocks`).
+
+    ``values`` (float8_e4m3fn [..., d]) and ``exponents`` (uint8 [...,
+    ceil(d / 128)]): 128 elements stand for values * 2^(exponent - 127).
+    """
+
+    __slots__ = ("values", "exponents")
+
+    def __init__(self, values: torch.Tensor, exponents: torch.Tensor):
+        self.values, self.exponents = values, exponents
+
+    @property
+    def shape(self) -> torch.Size:
+        return self.values.shape
+
+
+def _blocks(q: BlockRows, name: str, dims: Tuple[int, ...], device: Optional[torch.device] = None) -> None:
+    if not isinstance(q, BlockRows):
+        raise TypeError("%s must be BlockRows (quantize_blocks)" % name)
+    _gpu(q.values, name + ".values", device)
+    if q.values.dim() not in dims or q.values.shape[-1] < 1:
+        raise ValueError("%s must have %s dimensions and at least one column" % (name, " or ".join(map(str, dims))))
+    shape = tuple(q.values.shape)
+    _array(q.values, name + ".values", _E4M3, shape, q.values.device)
+    _array(q.exponents, name + ".exponents", torch.uint8, shape[:-1] + ((shape[-1] + 127) // 128,), q.values.device)
+
+
+def quantize_blocks(X: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> BlockRows:
+    """Rows in 8 bits (kmeans_fp8_quantize): for each 128 elements of a row the
+    least power of two under which none is beyond 448, and the values divided by
+    it, rounded to e4m3; infinities and NaN become NaN.  X: rows [n, d], or
+    contiguous [k, rows, d] (the weights of clusters)."""
+    if isinstance(X, torch.Tensor) and X.dim() == 3:
+        if not X.is_contiguous():
+            raise ValueError("X must be contiguous")
+        rows = X.view(-1, X.shape[2])
+    else:
+        rows = X
+    ld = _rows(rows, "X")
+    n, d = rows.shape
+    with _On(X.device, stream, (X,)) as s:
+        values = torch.empty(X.shape, dtype=_E4M3, device=X.device)
+        exps = torch.empty(X.shape[:-1] + ((d + 127) // 128,), dtype=torch.uint8, device=X.device)
+        st = N.load().kmeans_fp8_quantize(_p(rows), ld, n, d, _TYPES[X.dtype], _p(values), _p(exps), s)
+    N.check(st, "kmeans_fp8_quantize")
+    return BlockRows(values, exps)
+
+
+def dequantize_blocks(Q: BlockRows, dtype: torch.dtype = torch.float32,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The values that ``Q`` stands for (kmeans_fp8_dequantize), of Q's shape."""
+    _blocks(Q, "Q", (2, 3))
+    if dtype not in _TYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16, got %s" % dtype)
+    d, dev = Q.shape[-1], Q.values.device
+    with _On(dev, stream, (Q.values, Q.exponents)) as s:
+        out = torch.empty(Q.shape, dtype=dtype, device=dev)
+        st = N.load().kmeans_fp8_dequantize(_p(Q.values), _p(Q.exponents), out.numel() // d, d, _TYPES[dtype], _p(out),
+                                            s)
+    N.check(st, "kmeans_fp8_dequantize")
+    return out
+
+
+def cluster_linear_fp8(X, W: BlockRows, plan: ClusterPlan, sorted_rows: bool = False,
+                       dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None
+                       ) -> torch.Tensor:
+    """:func:`cluster_linear` with both operands in 8 bits (kmeans_fp8_forward);
+    sums are float32.
+
+    W: [k, dout, din], quantised once.  X: rows [n, din], quantised in the call
+    as :func:`quantize_blocks` does, or :class:`BlockRows`.  ``dtype``: of the
+    results (default: X's type, bfloat16 for BlockRows).  For serving: the
+    gradients of such a layer are those of :func:`cluster_linear`.
+    """
+    _blocks(W, "W", (3,))
+    k, dout, din = W.shape
+    dev = W.values.device
+    if isinstance(X, BlockRows):
+        _blocks(X, "X", (2,), dev)
+        rows, exps, ld, kind = X.values, X.exponents, X.shape[1], N.KM_E4M3
+    else:
+        ld = _rows(X, "X")
+        _gpu(X, "X", dev)
+        rows, exps, kind = X, None, _TYPES[X.dtype]
+    n = rows.shape[0]
+    if rows.shape[1] != din or k < 1 or dout < 1:
+        raise ValueError("X must have %d columns, and W weights" % din)
+    dtype = dtype if dtype is not None else torch.bfloat16 if exps is not None else X.dtype
+    if dtype not in _TYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16, got %s" % dtype)
+    order = _places(plan, n, k, dev, sorted_rows)
+    lib = N.load()
+    need = lib.kmeans_fp8_workspace_bytes(n, din, dout, k, kind)
+    if need == 0:
+        raise N.KMError(N.KM_ERR_UNSUPPORTED, "kmeans_fp8_workspace_bytes",
+                        "up to 2^27 rows, 2^24 columns and 2^31 tiles of 64 rows and columns")
+    with _On(dev, stream, (rows, exps, W.values, W.exponents, order, plan.sorted_ids, plan.offsets)) as s:
+        y = torch.empty((n, dout), dtype=dtype, device=dev)
+        ws = _workspace(need, dev, "kmeans_fp8_workspace_bytes")
+        st = lib.kmeans_fp8_forward(_p(rows), ld, _p(exps), n, din, dout, k, kind, _p(W.values), _p(W.exponents),
+                                    _p(order), _p(plan.sorted_ids), _p(plan.offsets), _p(y), _TYPES[dtype], _p(ws),
+                                    ws.numel(), s)
+    N.check(st, "kmeans_fp8_forward")
+    return y
