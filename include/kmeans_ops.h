@@ -13,7 +13,9 @@
  *                     of rows and weights;
  *   kmeans_fp8_*      rows in 8-bit floating point with a scale for each 128
  *                     elements, and products of them with one weight per
- *                     cluster.
+ *                     cluster;
+ *   kmeans_table_*    rows of a table by their ids, and the table's gradient;
+ *   kmeans_clip_*     the norm over many tensors, and scaling them to a limit.
  *
  * Common to all.  Status codes and kmeans_mti_last_hip_error() are those of
  * kmeans_mti.h; no entry point throws, allocates device memory or
@@ -216,6 +218,38 @@ int kmeans_fp8_forward(const void* X, int64_t ldx, const uint8_t* exponents, int
                        int32_t k, int32_t type, const void* W, const uint8_t* w_exponents, const int32_t* order,
                        const int32_t* sorted_ids, const int32_t* offsets, void* Y, int32_t y_type, void* workspace,
                        size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows of a table by their ids: Y[i] = scale table[ids[i]] (n x d), zeros for an
+ * id outside [0, k).  table: k rows of d, ld apart.  Requires n >= 0, d >= 1,
+ * k >= 1 and a finite scale.
+ */
+int kmeans_table_forward(const int32_t* ids, int64_t n, int32_t k, int32_t d, int32_t type, const void* table,
+                         int64_t ld, float scale, void* Y, void* hip_stream);
+
+/*
+ * Gradient of kmeans_table_forward: dTable[c] = scale times the sum of dY over
+ * the slots of id c (k x d of the rows' type, zeros for an id without slots),
+ * from dY (n rows) and a plan of kmeans_sort_plan of the ids (n slots).
+ */
+size_t kmeans_table_workspace_bytes(int64_t n, int32_t k, int32_t d, int32_t type);   /* 0 for bad sizes */
+int kmeans_table_backward(const void* dY, int64_t lddy, int64_t n, int32_t k, int32_t d, int32_t type,
+                          const int32_t* order, const int32_t* sorted_ids, const int32_t* offsets, float scale,
+                          void* dTable, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The norm g over `count` tensors: the square root of the sum of all squares,
+ * formed in float64, to *norm (device, float32; infinity beyond its range).  With
+ * out, not NULL, out[i] = tensors[i] min(1, limit / g), rounded once; a norm that
+ * is not finite leaves the values as they are.  tensors, out, sizes (elements)
+ * and types are HOST arrays, read before the call returns; out[i] is tensors[i]
+ * (in place) or does not overlap any tensor.  Requires at most 2^40 elements in
+ * all and a positive limit.
+ */
+size_t kmeans_clip_workspace_bytes(const int64_t* sizes, int32_t count);   /* 0 for bad sizes */
+int kmeans_clip_norm(const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* types,
+                     int32_t count, double limit, float* norm, void* workspace, size_t workspace_bytes,
+                     void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -7,12 +7,14 @@ ops.py holds the operators of a layer conditioned on clusters
 (include/kmeans_ops.h).
 """
 from .kmeans import KMeansMTI, kmeanspp, kmeanspp_workspace_bytes, run, run_pp_best  # noqa: F401
-from .ops import (BlockRows, ClusterPlan, adapter_linear, adapter_linear_backward, cluster_combine,  # noqa: F401
-                  cluster_combine_backward, cluster_gather, cluster_linear, cluster_linear_backward,
-                  cluster_linear_fp8, cluster_sort, dequantize_blocks, quantize_blocks, layernorm, layernorm_backward)
+from .ops import (BlockRows, ClusterPlan, adapter_linear, adapter_linear_backward, clip_global_norm,  # noqa: F401
+                  cluster_combine, cluster_combine_backward, cluster_embedding, cluster_embedding_backward,
+                  cluster_gather, cluster_linear, cluster_linear_backward, cluster_linear_fp8, cluster_sort,
+                  dequantize_blocks, global_norm, layernorm, layernorm_backward, quantize_blocks)
 
 __all__ = ["KMeansMTI", "kmeanspp", "kmeanspp_workspace_bytes", "run", "run_pp_best",
            "ClusterPlan", "cluster_sort", "cluster_gather", "cluster_combine", "cluster_combine_backward",
            "layernorm", "layernorm_backward", "adapter_linear", "adapter_linear_backward",
            "cluster_linear", "cluster_linear_backward",
-           "BlockRows", "quantize_blocks", "dequantize_blocks", "cluster_linear_fp8"]
+           "BlockRows", "quantize_blocks", "dequantize_blocks", "cluster_linear_fp8",
+           "cluster_embedding", "cluster_embedding_backward", "global_norm", "clip_global_norm"]

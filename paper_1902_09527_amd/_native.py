@@ -55,6 +55,8 @@ OPS_EXPORTS = (
     "kmeans_adapter_workspace_bytes", "kmeans_adapter_tile", "kmeans_adapter_forward", "kmeans_adapter_backward",
     "kmeans_linear_workspace_bytes", "kmeans_linear_forward", "kmeans_linear_backward",
     "kmeans_fp8_quantize", "kmeans_fp8_dequantize", "kmeans_fp8_workspace_bytes", "kmeans_fp8_forward",
+    "kmeans_table_forward", "kmeans_table_workspace_bytes", "kmeans_table_backward",
+    "kmeans_clip_workspace_bytes", "kmeans_clip_norm",
 )
 
 #: Size of the static workspace of kmeans_pp_seed_noalloc (KMEANS_PP_STATIC_WORKSPACE_BYTES).
@@ -188,6 +190,16 @@ def load() -> C.CDLL:
     lib.kmeans_fp8_workspace_bytes.restype = sz
     lib.kmeans_fp8_forward.argtypes = [P, i64, P, i64] + [i32] * 4 + [P] * 6 + [i32, P, sz, P]
     lib.kmeans_fp8_forward.restype = C.c_int
+    lib.kmeans_table_forward.argtypes = [P, i64, i32, i32, i32, P, i64, f32, P, P]
+    lib.kmeans_table_forward.restype = C.c_int
+    lib.kmeans_table_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.kmeans_table_workspace_bytes.restype = sz
+    lib.kmeans_table_backward.argtypes = [P, i64, i64, i32, i32, i32, P, P, P, f32, P, P, sz, P]
+    lib.kmeans_table_backward.restype = C.c_int
+    lib.kmeans_clip_workspace_bytes.argtypes = [P, i32]
+    lib.kmeans_clip_workspace_bytes.restype = sz
+    lib.kmeans_clip_norm.argtypes = [P, P, P, P, i32, f64, P, P, sz, P]
+    lib.kmeans_clip_norm.restype = C.c_int
     lib.kmeans_mti_last_hip_error.argtypes = []
     lib.kmeans_mti_last_hip_error.restype = C.c_char_p
     _lib = lib

@@ -23,6 +23,7 @@ SOURCES = [os.path.join(CSRC, "km_kernels.hip"), os.path.join(CSRC, "km_large.hi
            os.path.join(CSRC, "km_sort.hip"), os.path.join(CSRC, "km_norm.hip"),
            os.path.join(CSRC, "km_adapter.hip"),
            os.path.join(CSRC, "km_group.hip"), os.path.join(CSRC, "km_fp8.hip"),
+           os.path.join(CSRC, "km_table.hip"), os.path.join(CSRC, "km_clip.hip"),
            os.path.join(CSRC, "km_ops.hip"),
            os.path.join(CSRC, "km_host.hip")]
 ARCH = "gfx950"

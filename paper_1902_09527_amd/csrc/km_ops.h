@@ -203,4 +203,46 @@ hipError_t launch_quantize(const void* X, int64_t ldx, int64_t n, int32_t d, int
 hipError_t launch_dequantize(const uint8_t* Q, const uint8_t* E, int64_t n, int32_t d, int type, void* X,
                              hipStream_t s);
 
+// ---- rows of a table (km_table.hip)
+
+constexpr int kTableShort = 32;    // slots up to which an id is summed by the lanes of its row
+constexpr int kTableChunk = 1024;  // most places of a chunk
+
+struct TableArgs {
+    const int32_t* ids;                       // forward
+    const int32_t *order, *sids, *offsets;    // backward: the plan
+    const void *table, *dY;
+    int64_t ld, n;                            // of table or dY; slots
+    int32_t d, k;
+    float scale;
+    void* out;                                // rows, or the table's gradient
+    float* part;                              // backward: chunks x 2 x d
+    int32_t chunk, lanes, slices;             // backward, set by the launch
+    uint32_t long_blocks;
+};
+struct TableShape {
+    int32_t chunk, lanes, slices;   // places a chunk; log2 of the lanes of a row's slice; slices
+    int64_t chunks;
+    size_t bytes;
+};
+TableShape table_shape(int64_t n, int32_t d, int type);
+hipError_t launch_table_fwd(const TableArgs& A, int type, hipStream_t s);
+hipError_t launch_table_bwd(const TableArgs& A, const TableShape& L, int type, hipStream_t s);
+
+// ---- the norm over many tensors (km_clip.hip)
+
+struct ClipShape {
+    int32_t step;    // elements a block
+    int64_t parts;   // blocks of all tensors
+    size_t bytes;
+};
+ClipShape clip_shape(const int64_t* sizes, int32_t count);
+hipError_t launch_clip_norm(const void* const* p, const int64_t* sizes, const int32_t* types, int32_t count,
+                            const ClipShape& L, double* part, hipStream_t s);
+hipError_t launch_clip_total(const ClipShape& L, const double* part, float* norm, hipStream_t s);
+// norm may be null (a call without tensors of any element).
+hipError_t launch_clip_scale(const void* const* p, void* const* q, const int64_t* sizes, const int32_t* types,
+                             int32_t count, const ClipShape& L, const double* part, double limit, float* norm,
+                             hipStream_t s);
+
 }  // namespace km

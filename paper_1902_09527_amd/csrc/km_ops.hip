@@ -3,6 +3,10 @@
 // their contracts are in include/kmeans_ops.h.
 #include <math.h>
 
+#include <algorithm>
+#include <new>
+#include <vector>
+
 #include "kmeans_ops.h"
 #include "km_ops.h"
 
@@ -635,6 +639,177 @@ int kmeans_fp8_forward(const void* X, int64_t ldx, const uint8_t* exponents, int
     D.offsets = offsets;
     D.Y = Y;
     return done(km::launch_group_forward(D, ws, P.L, km::kF8, y_type, st), "kmeans_fp8_forward");
+}
+
+int kmeans_table_forward(const int32_t* ids, int64_t n, int32_t k, int32_t d, int32_t type, const void* table,
+                         int64_t ld, float scale, void* Y, void* hip_stream) {
+    if (!type_ok(type)) return bad("a type of KM_F32, KM_BF16 or KM_F16 needed");
+    if (k < 1 || !rows_ok(n, d, d) || !rows_ok(k, d, ld)) return bad("n >= 0, k >= 1, d >= 1, ld >= d needed, and sizes within 63 bits");
+    if (!isfinite(scale)) return bad("scale is not finite");
+    if (n == 0) return KM_OK;
+    if (!ids || !table || !Y) return bad("ids, table or Y is null");
+    Checks C;
+    C.array(ids, (size_t)n * 4, "ids");
+    C.rows(table, k, d, ld, type, "table");
+    C.rows(Y, n, d, d, type, "Y");
+    if (C.rc != KM_OK) return C.rc;
+    km::TableArgs A{};
+    A.ids = ids;
+    A.n = n;
+    A.k = k;
+    A.d = d;
+    A.table = table;
+    A.ld = ld;
+    A.scale = scale;
+    A.out = Y;
+    return done(km::launch_table_fwd(A, type, static_cast<hipStream_t>(hip_stream)), "kmeans_table_forward");
+}
+
+static bool table_ok(int64_t n, int32_t k, int32_t d, int32_t type) {
+    return type_ok(type) && slots_ok(n, 1, k) && rows_ok(n, d, d) && rows_ok(k, d, d);
+}
+
+size_t kmeans_table_workspace_bytes(int64_t n, int32_t k, int32_t d, int32_t type) {
+    return table_ok(n, k, d, type) ? km::table_shape(n, d, type).bytes : 0;
+}
+
+int kmeans_table_backward(const void* dY, int64_t lddy, int64_t n, int32_t k, int32_t d, int32_t type,
+                          const int32_t* order, const int32_t* sorted_ids, const int32_t* offsets, float scale,
+                          void* dTable, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!table_ok(n, k, d, type) || !rows_ok(n, d, lddy))
+        return bad("0 <= n < 2^31, 1 <= k < 2^31 - 1, d >= 1, lddy >= d and a type needed, and sizes within 63 bits");
+    if (!isfinite(scale)) return bad("scale is not finite");
+    if (!offsets || !dTable || (n > 0 && (!dY || !order || !sorted_ids)))
+        return bad("dY, order, sorted_ids, offsets or dTable is null");
+    const km::TableShape L = km::table_shape(n, d, type);
+    if (L.chunks * L.slices >= INT32_MAX / 2) return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^30 chunks");
+    const int rc = workspace_ok(workspace, workspace_bytes, L.bytes);
+    if (rc != KM_OK) return rc;
+    Checks C;
+    C.rows(dY, n, d, lddy, type, "dY");
+    C.array(order, (size_t)n * 4, "order");
+    C.array(sorted_ids, (size_t)n * 4, "sorted_ids");
+    C.array(offsets, ((size_t)k + 1) * 4, "offsets");
+    C.rows(dTable, k, d, d, type, "dTable");
+    C.array(workspace, L.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    km::TableArgs A{};
+    A.order = order;
+    A.sids = sorted_ids;
+    A.offsets = offsets;
+    A.n = n;
+    A.k = k;
+    A.d = d;
+    A.dY = dY;
+    A.ld = lddy;
+    A.scale = scale;
+    A.out = dTable;
+    A.part = static_cast<float*>(workspace);
+    return done(km::launch_table_bwd(A, L, type, static_cast<hipStream_t>(hip_stream)), "kmeans_table_backward");
+}
+
+// Checks of many arrays: the allocations that they lie in are asked for once each
+// (a call's tensors share few).
+struct Ranges {
+    static constexpr int kHeld = 16;
+    uintptr_t lo[kHeld], hi[kHeld];
+    int held = 0, next = 0;
+    int rc = KM_OK;
+    void array(const Checks& C, const void* p, size_t bytes, const char* what) {
+        if (rc != KM_OK || bytes == 0) return;
+        const uintptr_t q = (uintptr_t)p;
+        for (int i = 0; i < held; ++i)
+            if (q >= lo[i] && q + bytes <= hi[i]) return;
+        if ((rc = km::ops_check_range(p, bytes, C.dev, what)) != KM_OK) return;
+        hipDeviceptr_t base = nullptr;
+        size_t size = 0;
+        if (hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)p) != hipSuccess) {
+            (void)hipGetLastError();
+            return;
+        }
+        lo[next] = (uintptr_t)base;
+        hi[next] = (uintptr_t)base + size;
+        next = (next + 1) % kHeld;
+        if (held < kHeld) ++held;
+    }
+};
+
+// Whether no output overlaps another output or another tensor.
+struct Span {
+    uintptr_t lo, hi;
+    bool out;
+};
+static bool apart(const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* types,
+                  int32_t count) {
+    std::vector<Span> v;
+    v.reserve(2 * (size_t)count);
+    for (int32_t i = 0; i < count; ++i) {
+        const size_t b = (size_t)sizes[i] * km::row_type_bytes(types[i]);
+        if (b == 0) continue;
+        v.push_back({(uintptr_t)out[i], (uintptr_t)out[i] + b, true});
+        if (tensors[i] != out[i]) v.push_back({(uintptr_t)tensors[i], (uintptr_t)tensors[i] + b, false});
+    }
+    std::sort(v.begin(), v.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
+    uintptr_t end_in = 0, end_out = 0;
+    for (const Span& x : v) {
+        if (x.lo < end_out || (x.out && x.lo < end_in)) return false;
+        uintptr_t& end = x.out ? end_out : end_in;
+        if (x.hi > end) end = x.hi;
+    }
+    return true;
+}
+
+static bool tensors_ok(const int64_t* sizes, int32_t count) {
+    if (count < 0 || (count > 0 && !sizes)) return false;
+    int64_t total = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || sizes[i] > ((int64_t)1 << 40) || (total += sizes[i]) > (int64_t)1 << 40) return false;
+    }
+    return true;
+}
+
+size_t kmeans_clip_workspace_bytes(const int64_t* sizes, int32_t count) {
+    return tensors_ok(sizes, count) ? km::clip_shape(sizes, count).bytes : 0;
+}
+
+int kmeans_clip_norm(const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* types,
+                     int32_t count, double limit, float* norm, void* workspace, size_t workspace_bytes,
+                     void* hip_stream) {
+    if (!tensors_ok(sizes, count)) return bad("count >= 0, sizes >= 0 and at most 2^40 elements needed");
+    if (!norm || (count > 0 && (!tensors || !types))) return bad("tensors, types or norm is null");
+    if (out && !(limit > 0)) return bad("limit is not positive");
+    const km::ClipShape L = km::clip_shape(sizes, count);
+    int rc = workspace_ok(workspace, workspace_bytes, L.bytes);
+    if (rc != KM_OK) return rc;
+    if (L.parts > INT32_MAX / 2) return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^30 blocks");
+    Checks C;
+    C.array(norm, 4, "norm");
+    C.array(workspace, L.bytes, "workspace");
+    if (C.rc != KM_OK) return C.rc;
+    Ranges R;
+    for (int32_t i = 0; i < count; ++i) {
+        if (!type_ok(types[i])) return bad("types of KM_F32, KM_BF16 or KM_F16 needed");
+        if (sizes[i] > 0 && (!tensors[i] || (out && !out[i]))) return bad("a tensor is null");
+        const size_t b = (size_t)sizes[i] * km::row_type_bytes(types[i]);
+        R.array(C, tensors[i], b, "a tensor");
+        if (out) R.array(C, out[i], b, "an output");
+    }
+    if (R.rc != KM_OK) return R.rc;
+    if (out) {
+        try {
+            if (!apart(tensors, out, sizes, types, count)) return bad("an output overlaps another output or tensor");
+        } catch (const std::bad_alloc&) {
+            return km::ops_error(KM_ERR_OOM, "host memory");
+        }
+    }
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    double* part = static_cast<double*>(workspace);
+    hipError_t e = km::launch_clip_norm(tensors, sizes, types, count, L, part, st);
+    if (e == hipSuccess) {
+        if (out && L.parts > 0) e = km::launch_clip_scale(tensors, out, sizes, types, count, L, part, limit, norm, st);
+        else e = km::launch_clip_total(L, part, norm, st);
+    }
+    return done(e, "kmeans_clip_norm");
 }
 
 }  // extern "C"

@@ -13,7 +13,11 @@ tokens of a model, embeddings -- to small experts of their clusters:
       products with one weight per cluster;
   quantize_blocks, dequantize_blocks, cluster_linear_fp8
       rows in 8 bits with a scale for each 128 elements, and their products
-      with one weight per cluster.
+      with one weight per cluster;
+  cluster_embedding, cluster_embedding_backward
+      rows of a table by their ids (a vocabulary's, the clusters' own);
+  global_norm, clip_global_norm
+      the norm over many tensors, and scaling them to a limit of it.
 
 As in :mod:`.kmeans`, this is argument marshalling only: tensors are checked
 and handed to the kernels of ``libkmeans_mti.so``.  Rows are float32, bfloat16
@@ -30,7 +34,9 @@ on.  Call them under ``torch.no_grad()``, or in the forward and backward of a
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+import ctypes
+import math
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -569,3 +575,116 @@ def cluster_linear_fp8(X, W: BlockRows, plan: ClusterPlan, sorted_rows: bool = F
                                     ws.numel(), s)
     N.check(st, "kmeans_fp8_forward")
     return y
+
+
+def _scale(scale: float) -> float:
+    scale = float(scale)
+    if not math.isfinite(scale):
+        raise ValueError("scale must be finite")
+    return scale
+
+
+def cluster_embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Rows of a table by their ids (kmeans_table_forward): scale * table[id] for
+    each of the ids (int32, any shape: tokens, or ``run``'s assignment), zeros
+    for an id outside [0, k); of shape ids.shape + (d,).  table: rows [k, d]."""
+    ld = _rows(table, "table")
+    k, d = table.shape
+    _gpu(ids, "ids", table.device)
+    if k < 1:
+        raise ValueError("table must have at least one row")
+    _array(ids, "ids", torch.int32, tuple(ids.shape), table.device)
+    scale = _scale(scale)
+    with _On(table.device, stream, (ids, table)) as s:
+        y = table.new_empty(ids.shape + (d,))
+        st = N.load().kmeans_table_forward(_p(ids), ids.numel(), k, d, _TYPES[table.dtype], _p(table), ld, scale, _p(y),
+                                           s)
+    N.check(st, "kmeans_table_forward")
+    return y
+
+
+def cluster_embedding_backward(dY: torch.Tensor, plan: ClusterPlan, scale: float = 1.0,
+                               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of :func:`cluster_embedding` for its table (kmeans_table_backward):
+    [k, d] of dY's type, scale times the sum of dY over each id's slots, zeros
+    for an id without any.  plan: ``cluster_sort(ids, k)``; dY: rows [n m, d], one
+    for each slot.  Sums are float32 and do not depend on the run."""
+    ld = _rows(dY, "dY", n=plan.n * plan.m if isinstance(plan, ClusterPlan) else None)
+    _plan(plan, dY.device)
+    n, d = dY.shape
+    scale = _scale(scale)
+    lib = N.load()
+    with _On(dY.device, stream, (dY, plan.order, plan.sorted_ids, plan.offsets)) as s:
+        out = dY.new_empty((plan.k, d))
+        ws = _workspace(lib.kmeans_table_workspace_bytes(n, plan.k, d, _TYPES[dY.dtype]), dY.device,
+                        "kmeans_table_workspace_bytes")
+        st = lib.kmeans_table_backward(_p(dY), ld, n, plan.k, d, _TYPES[dY.dtype], _p(plan.order), _p(plan.sorted_ids),
+                                       _p(plan.offsets), scale, _p(out), _p(ws), ws.numel(), s)
+    N.check(st, "kmeans_table_backward")
+    return out
+
+
+def _tensors(tensors: Sequence[torch.Tensor], name: str) -> List[torch.Tensor]:
+    """Check a list of contiguous tensors of one device."""
+    given = list(tensors)
+    for t in given:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be torch.Tensors" % name)
+    for t in given:
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+    if len({t.get_device() for t in given}) > 1 or (given and not given[0].is_cuda):
+        raise ValueError("%s must be on one GPU device" % name)
+    if not {t.dtype for t in given} <= _TYPES.keys():
+        raise ValueError("%s must be float32, bfloat16 or float16" % name)
+    return given
+
+
+def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]], inplace: bool,
+          stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    given = _tensors(tensors, "tensors")
+    if not given:
+        raise ValueError("at least one tensor is needed")
+    dev, count = given[0].device, len(given)
+    sizes = [t.numel() for t in given]
+    pointers = [t.data_ptr() for t in given]
+    types = [_TYPES[t.dtype] for t in given]
+    targets, to = None, given if inplace else []
+    if out is not None:
+        to = _tensors(out, "out")
+        if len(to) != count or [t.numel() for t in to] != sizes or [t.dtype for t in to] != [t.dtype for t in given] \
+                or to[0].get_device() != given[0].get_device():
+            raise ValueError("out must have the tensors' sizes, types and device")
+        targets = (ctypes.c_void_p * count)(*[t.data_ptr() for t in to])
+    array = (ctypes.c_void_p * count)(*pointers)
+    if inplace:
+        targets = array
+    sizes_ = (ctypes.c_int64 * count)(*sizes)
+    lib = N.load()
+    with _On(dev, stream, tuple(given) + tuple(to) if out is not None else tuple(given)) as s:
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+        ws = _workspace(lib.kmeans_clip_workspace_bytes(sizes_, count), dev, "kmeans_clip_workspace_bytes")
+        st = lib.kmeans_clip_norm(array, targets, sizes_, (ctypes.c_int32 * count)(*types), count, limit, _p(norm), _p(ws),
+                                  ws.numel(), s)
+    N.check(st, "kmeans_clip_norm")
+    return norm
+
+
+def global_norm(tensors: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The square root of the sum of all squares over contiguous tensors of one
+    device (kmeans_clip_norm), formed in float64: a float32 tensor of no
+    dimensions (infinity beyond its range)."""
+    return _clip(tensors, 1.0, None, False, stream)
+
+
+def clip_global_norm(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Scale tensors so that their :func:`global_norm` is at most ``limit``
+    (kmeans_clip_norm): each times min(1, limit / norm), in place, or to ``out``
+    (tensors of the same sizes and types that overlap none of them).  Returns the
+    norm before.  A norm that is not finite leaves the values as they are."""
+    limit = float(limit)
+    if not limit > 0:
+        raise ValueError("limit must be positive")
+    return _clip(tensors, limit, out, out is None, stream)
