@@ -128,11 +128,10 @@ __device__ __forceinline__ u32x4 chunk_any(const T* row, int64_t k0, int64_t K) 
 // What to list: `size` places at most an item, none of two clusters.
 struct ListArgs {
     const int32_t* offsets;
-    int32_t n, k, size;
+    int32_t k, size;
     int32_t* count;
     GroupItem* items;
-    int32_t *first, *num;   // per cluster: first partial slot, items; null: not wanted, and
-                            // the places of no cluster are listed too, as cluster -1
+    int32_t *first, *num;   // per cluster: first partial slot, items; null: not wanted
 };
 
 // A block a list.  In order of the clusters.
@@ -141,10 +140,9 @@ __global__ __launch_bounds__(1024) void k_gr_list(ListArgs A0, ListArgs A1) {
     __shared__ int s[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int items = 0, slots = 0;   // so far
-    const int end = A.num ? A.k : A.k + 1;
-    for (int c0 = 0; c0 < end; c0 += 1024) {
+    for (int c0 = 0; c0 < A.k; c0 += 1024) {
         const int c = c0 + tid;
-        const int a = c < end ? A.offsets[c] : 0, b = c < A.k ? A.offsets[c + 1] : c < end ? A.n : 0;
+        const int a = c < A.k ? A.offsets[c] : 0, b = c < A.k ? A.offsets[c + 1] : 0;
         const int ni = (b - a + A.size - 1) / A.size, ns = ni > 1 ? ni : 0;
         int xi = ni, xs = ns;
 #pragma unroll
@@ -162,15 +160,14 @@ __global__ __launch_bounds__(1024) void k_gr_list(ListArgs A0, ListArgs A1) {
         }
         bi += xi - ni;
         bs += xs - ns;
-        if (c < end) {
+        if (c < A.k) {
             if (A.num) {
                 A.first[c] = bs;
                 A.num[c] = ni;
             }
             for (int q = 0; q < ni; ++q) {
                 const int p = a + q * A.size;
-                A.items[bi + q] =
-                    GroupItem{c < A.k ? c : -1, p, b - p < A.size ? b : p + A.size, A.num && ni > 1 ? bs + q : -1};
+                A.items[bi + q] = GroupItem{c, p, b - p < A.size ? b : p + A.size, A.num && ni > 1 ? bs + q : -1};
             }
         }
         __syncthreads();
@@ -179,221 +176,531 @@ __global__ __launch_bounds__(1024) void k_gr_list(ListArgs A0, ListArgs A1) {
 }
 
 // --------------------------------------------------------------------------
+// Results.
+
+// Four consecutive results, col0 .. of a row of P, at any address.
+template <class O>
+__device__ __forceinline__ void put4(O* row, int64_t col0, int64_t P, f32x4 v) {
+    Vec<O, 4> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.e[i] = from_f32<O>(v[i]);
+    if (col0 + 4 <= P) {
+        __builtin_memcpy(row + col0, &o, sizeof(o));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col0 + i < P) row[col0 + i] = o.e[i];
+    }
+}
+
+// A lane's part of two neighbouring operands' results (R rows by 2 R columns, from
+// column col0 of its row on) in 16 bits: lanes exchange halves first, so that each
+// writes 16 bytes.
+template <int R, class O>
+__device__ __forceinline__ void put8(O* row, int64_t col, int64_t P, f32x4 v, f32x4 w) {
+    struct Two {
+        uint32_t a, b;
+    };
+    Vec<O, 4> x, y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.e[i] = from_f32<O>(v[i]), y.e[i] = from_f32<O>(w[i]);
+    const Two p = __builtin_bit_cast(Two, x), q = __builtin_bit_cast(Two, y);
+    u32x4 o;
+    // The odd groups' part of the first operand against the even groups' of the second.
+    if constexpr (R == 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(p.a, q.a, false, false);
+        const auto t = __builtin_amdgcn_permlane16_swap(p.b, q.b, false, false);
+        o = u32x4{(uint32_t)s[0], (uint32_t)t[0], (uint32_t)s[1], (uint32_t)t[1]};
+    } else {
+        const auto s = __builtin_amdgcn_permlane32_swap(p.a, q.a, false, false);
+        const auto t = __builtin_amdgcn_permlane32_swap(p.b, q.b, false, false);
+        o = u32x4{(uint32_t)s[0], (uint32_t)t[0], (uint32_t)s[1], (uint32_t)t[1]};
+    }
+    if (col + 8 <= P) {
+        __builtin_memcpy(row + col, &o, 16);
+    } else {
+        const Vec<O, 8> e = __builtin_bit_cast(Vec<O, 8>, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i < P) row[col + i] = e.e[i];
+    }
+}
+
+// The results of a lane's row, FC operands of columns from col0 on.  Every lane of
+// the wave calls it (lanes exchange parts); `in`: the row is there.
+template <class Q, class O, int FC>
+__device__ __forceinline__ void put_row(O* row, int64_t col0, int64_t P, const typename Q::Acc (&acc)[FC], int lane,
+                                        bool in) {
+    const int64_t end = in ? P : 0;   // nothing is written past it
+    auto part = [&](int h, int j) {
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = acc[h][j * 4 + i];
+        return v;
+    };
+    if constexpr (sizeof(O) == 2 && Q::R == 16 && FC % 2 == 0) {
+        const int g = lane >> 4;
+#pragma unroll
+        for (int h = 0; h < FC; h += 2)
+            put8<16>(row, col0 + (h + (g & 1)) * 16 + (g >> 1) * 8, end, part(h, 0), part(h + 1, 0));
+    } else if constexpr (sizeof(O) == 2 && Q::R == 32) {
+#pragma unroll
+        for (int h = 0; h < FC; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2)
+                put8<32>(row, col0 + h * 32 + (j + (lane >> 5)) * 8, end, part(h, j), part(h, j + 1));
+    } else {
+#pragma unroll
+        for (int h = 0; h < FC; ++h)
+#pragma unroll
+            for (int j = 0; j < Q::kRuns; ++j) put4(row, col0 + h * Q::R + Q::run(j, lane), end, part(h, j));
+    }
+}
+
+// --------------------------------------------------------------------------
 // Y[row] = V_c U[row], V = W_c (P x K) forward, W_c^T (W_c is K x P) with TR.
 
 struct MainArgs {
     const void* U;
-    int64_t ldu;
+    int64_t ldu, n;
     const void* W;
     const uint8_t *UE, *WE;   // 8 bits: a byte for each 128 elements of a row, nb a row
-    const int32_t *order, *count;
+    const int32_t *order, *count, *used;   // used: places of clusters
     const GroupItem* items;
     void* Y;
-    int32_t K, P, nb, y4;     // y4: Y can be written 4 elements at a time
+    int32_t K, P, nb;
     int32_t tn;               // tiles of columns
 };
 
-constexpr int kWindow = 32;   // stages whose scales are in LDS
+// Rows of no cluster: zeros, by all blocks, a wave a row.
+template <class O>
+__device__ __forceinline__ void zero_rows(const MainArgs& A, int waves) {
+    constexpr int E = 16 / (int)sizeof(O);
+    const int64_t step = (int64_t)gridDim.x * waves;
+    for (int64_t p = A.used[0] + (int64_t)blockIdx.x * waves + (threadIdx.x >> 6); p < A.n; p += step) {
+        O* y = static_cast<O*>(A.Y) + row_of(A.order, p) * A.P;
+        for (int64_t col = (threadIdx.x & 63) * E; col < A.P; col += 64 * E) {
+            const u32x4 zero{0, 0, 0, 0};
+            if (col + E <= A.P) {
+                __builtin_memcpy(y + col, &zero, 16);
+            } else {
+                for (int i = 0; col + i < A.P; ++i) y[col + i] = from_f32<O>(0.0f);
+            }
+        }
+    }
+}
 
-// A tile is TM places x TN columns, WR x WC waves; the contraction goes in stages
-// of 128 bytes a row, NS of them in LDS.  Rows of a tile are dealt to its waves in
-// kParts turns, so that a tile of few rows leaves out the products of the turns
-// past them.
-template <class T, class O, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
-__global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
+// What the two forms share: a tile is TM places x TN columns, WR x WC waves; the
+// contraction goes in stages of 128 bytes a row.  Rows of a tile are dealt to its
+// waves in kParts turns, so that a tile of few rows leaves out the products of the
+// turns past them.
+template <class T, class O, int TM, int TN, int WR, int WC>
+struct Geo {
     using P = Op<T, O>;
-    constexpr bool F8 = sizeof(T) == 1;
-    constexpr int E = P::E, R = P::R, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
-    constexpr int FR = TM / WR / R, FC = TN / WC / R;
-    constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
-    constexpr int kStage = (TM + TN) * 128;
-    constexpr int kParts = FR < 4 ? FR : 4, FP = FR / kParts;   // turns, and a wave's operands of one
-    constexpr int kTurn = FP * R * WR;                          // rows of a turn
+    static constexpr int E = P::E, R = P::R, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
+    static constexpr int FR = TM / WR / R, FC = TN / WC / R;
+    static constexpr int NU = TM * 8 / NT, NW = TN * 8 / NT, CPR = TN / E;
+    static constexpr int kStage = (TM + TN) * 128;
+    static constexpr int kParts = FR < 4 ? FR : 4, FP = FR / kParts;   // turns, and a wave's operands of one
+    static constexpr int kTurn = FP * R * WR;                          // rows of a turn
     static_assert(FR % kParts == 0 && NT % 128 == 0, "");
+    // The tile's row of operand f, but for the lane's.
+    static __device__ __forceinline__ int row(int f, int wr) { return f / FP * kTurn + wr * (FP * R) + f % FP * R; }
+};
+
+// An item of the list, which nothing writes while a product runs: by way of the
+// scalar unit.
+__device__ __forceinline__ GroupItem item_at(const GroupItem* items, int64_t i) {
+    typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+    const i32x4 v = *reinterpret_cast<const __attribute__((address_space(4))) i32x4*>((uintptr_t)(items + i));
+    return GroupItem{v[0], v[1], v[2], v[3]};
+}
+
+// A tile of the list: places p0 .. of cluster c, columns bn .. .
+struct Tile {
+    int c, p0, rows, bn;
+};
+// Down 4 row tiles before the next columns.
+template <int TN>
+__device__ __forceinline__ Tile tile_at(const MainArgs& A, int items, int t) {
+    const int group = 4 * A.tn, grp = t / group, m0 = grp * 4, in = t - grp * group;
+    const int gm = items - m0 < 4 ? items - m0 : 4;
+    const GroupItem it = item_at(A.items, m0 + in % gm);
+    return Tile{it.c, it.p0, it.p1 - it.p0, in / gm * TN};
+}
+
+constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, twice
+
+// Blocks stay and take tile after tile.  The stages of all of a block's tiles are
+// one sequence: two of them are in LDS, and the next tile's first ones are on their
+// way while the last ones of a tile are multiplied and its results are written.
+template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
+__global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
+    using G = Geo<T, O, TM, TN, WR, WC>;
+    using P = typename G::P;
+    constexpr bool F8 = sizeof(T) == 1;
+    constexpr int E = G::E, R = G::R, KS = G::KS, BK = G::BK, NT = G::NT, FR = G::FR, FC = G::FC, NU = G::NU, NW = G::NW;
+    constexpr int CPR = G::CPR, kStage = G::kStage, kParts = G::kParts, FP = G::FP, kTurn = G::kTurn;
+    static_assert(!F8 || NT >= TM + TN, "");
     extern __shared__ __align__(16) char s_tiles[];
-    uint8_t* s_scale = reinterpret_cast<uint8_t*>(s_tiles + NS * kStage);   // 8 bits: [kWindow][TM + TN]
-    int32_t* s_rows = reinterpret_cast<int32_t*>(s_tiles + NS * kStage + (F8 ? kWindow * (TM + TN) : 0));
+    char* s_scale = s_tiles + 2 * kStage;   // 8 bits: [2][TM + TN][kWindow]
+    int32_t* s_rows = reinterpret_cast<int32_t*>(s_scale + (F8 ? 2 * kWindow * (TM + TN) : 0));   // [3][TM]
     const int tid = threadIdx.x, lane = tid & 63, li = lane % R;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
 
-    // Consecutive tiles go to one XCD (blocks are dealt over 8), down 4 row tiles
-    // before the next columns.
+    // Consecutive tiles go to one XCD (blocks are dealt over 8).
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
-    const int64_t tiles = (int64_t)items * A.tn, per = (tiles + 7) / 8;
-    const int64_t t = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per || t >= tiles) return;
-    const int64_t grp = t / (4 * (int64_t)A.tn), m0 = grp * 4;
-    const int gm = items - m0 < 4 ? (int)(items - m0) : 4;
-    const int64_t in_grp = t - grp * 4 * A.tn;
-    const GroupItem it = A.items[m0 + in_grp % gm];
-    const int64_t bn = in_grp / gm * TN;
-    const int c = __builtin_amdgcn_readfirstlane(it.c), p0 = __builtin_amdgcn_readfirstlane(it.p0);
-    const int rows = __builtin_amdgcn_readfirstlane(it.p1) - p0;
-    O* const Y = static_cast<O*>(A.Y);
-    if (c < 0) {   // rows of no cluster
-        for (int q = tid; q < rows * TN; q += NT) {
-            const int64_t col = bn + q % TN;
-            if (col < A.P) Y[row_of(A.order, p0 + q / TN) * A.P + col] = from_f32<O>(0.0f);
-        }
-        return;
-    }
-    const int nk = (A.K + BK - 1) / BK, live = (rows + kTurn - 1) / kTurn;
-    const int64_t ldw = TR ? A.P : A.K;
-    const T* const W = static_cast<const T*>(A.W) + (int64_t)c * A.K * A.P;
-
-    // Where a thread's chunks of a stage come from: pointers that move on with the
-    // stages (AL), the place in the stage being fixed.
-    const T* up[NU];
-    const T* wp[NW];
-    const int uc = swz(tid / 8, tid % 8) * E;   // NT / 8 rows further on the swizzle is the same
+    const int tiles = items * A.tn, per = (tiles + 7) / 8, step = gridDim.x / 8;
+    const int x0 = (blockIdx.x % 8) * per, x1 = x0 + per < tiles ? x0 + per : tiles;
+    int t = x0 + blockIdx.x / 8;
+    if (t < x1) {
+        const int stages = (A.K + BK - 1) / BK, nk = stages < 2 ? 2 : stages;
+        // Where a thread's chunks of the next stage come from: bases that move on with
+        // the stages, the thread's places behind them being fixed (below 4 GB, as the
+        // host sees to).
+        const char *ub = nullptr, *wb = nullptr;
+        uint32_t uo[NU], wo[TR ? 2 : NW];   // TR: of even and odd chunks
+        int lk = 0, whole = 0, bn_load = 0;   // that stage, the stages without a chunk past an end, and its columns
+        const int uc = swz(tid / 8, tid % 8) * E;   // NT / 8 rows further on the swizzle is the same
+        const uint32_t es = sizeof(T), ldub = (uint32_t)A.ldu * es, ldwb = (uint32_t)(TR ? A.P : A.K) * es;
+        constexpr int kDown = NT / CPR;   // TR: rows from one chunk of a thread to its next (16 of them swizzle alike)
+        static_assert(!TR || kDown % 8 == 0, "");
+        // The rows of a tile, a thread each, by way of LDS (rows past the last: not stored).
+        auto fetch_row = [&](const Tile& q) {
+            return tid < TM ? (int32_t)row_of(A.order, q.p0 + (tid < q.rows ? tid : q.rows - 1)) : 0;
+        };
+        auto point = [&](const Tile& q, const int32_t* rows) {
+            ub = static_cast<const char*>(A.U) + (A.order ? 0 : (int64_t)q.p0 * A.ldu * es);
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        const int r = (i * NT + tid) / 8;
-        const int64_t row = row_of(A.order, p0 + (r < rows ? r : rows - 1));   // past the last: not stored
-        up[i] = static_cast<const T*>(A.U) + row * A.ldu + (AL ? uc : 0);
-        if (tid % 8 == 0) s_rows[r] = (int32_t)row;
-    }
+            for (int i = 0; i < NU; ++i)
+                uo[i] = (uint32_t)(rows[(i * NT + tid) / 8] - (A.order ? 0 : q.p0)) * ldub + uc * es;
+            const char* const W = static_cast<const char*>(A.W) + (int64_t)q.c * A.K * A.P * es;
+            if constexpr (TR) {
+                wb = W + q.bn * es;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        const int q = i * NT + tid;
-        if constexpr (TR) {
-            wp[i] = W + (int64_t)(q / CPR) * ldw + (AL ? bn + swz_tr<T, CPR>(q / CPR, q % CPR) * E : 0);
-        } else {
-            const int64_t col = bn + q / 8 < A.P ? bn + q / 8 : A.P - 1;   // past the last: not stored
-            wp[i] = W + col * ldw + (AL ? uc : 0);
-        }
-    }
-    // Stages without a chunk past the contraction's end or the last column.
-    const int whole = !TR || bn + TN <= A.P ? A.K / BK : 0;
-
-    // Chunk i of stage kt (of NU + NW a thread) to LDS; guard: it may lie past an end.
-    auto load = [&](int i, int kt, char* buf, bool guard) {
-        if (i < NU) {
-            const void* src = !guard || kt * BK + uc < A.K ? (const void*)up[i] : (const void*)zero_chunk;
-            load_lds16(src, buf + (i * NT + wave * 64) * 16);
-            up[i] += BK;
-            return;
-        }
-        i -= NU;
-        const int q = i * NT + tid;
-        char* wb = buf + TM * 128;
-        if constexpr (TR) {
-            const int kk = q / CPR;
-            const bool in = !guard || (kt * BK + kk < A.K && bn + swz_tr<T, CPR>(kk, q % CPR) * E < A.P);
-            load_lds16(in ? (const void*)wp[i] : (const void*)zero_chunk, wb + (i * NT + wave * 64) * 16);
-            wp[i] += BK * ldw;
-        } else {
-            const void* src = !guard || kt * BK + uc < A.K ? (const void*)wp[i] : (const void*)zero_chunk;
-            load_lds16(src, wb + (i * NT + wave * 64) * 16);
-            wp[i] += BK;
-        }
-    };
-    // The same through registers, at any address.
-    auto fetch = [&](int i, int kt) -> u32x4 {
-        if (i < NU) return chunk_any(up[i], (int64_t)kt * BK + uc, A.K);
-        i -= NU;
-        if constexpr (TR) {
-            const int q = i * NT + tid, kk = q / CPR;
-            const bool in = kt * BK + kk < A.K;
-            return only_if(in, chunk_any(in ? wp[i] + (int64_t)kt * BK * ldw : W,
-                                         bn + swz_tr<T, CPR>(kk, q % CPR) * E, A.P));
-        } else {
-            return chunk_any(wp[i], (int64_t)kt * BK + uc, A.K);
-        }
-    };
-
-    // 8 bits: the scales of the stages from k0 on, a row a thread.
-    auto scales = [&](int k0) {
-        if constexpr (F8) {
-            for (int r = tid; r < TM + TN; r += NT) {
-                const uint8_t* e;
-                if (r < TM) {
-                    e = A.UE + row_of(A.order, p0 + (r < rows ? r : rows - 1)) * A.nb;
-                } else {
-                    const int64_t col = bn + r - TM < A.P ? bn + r - TM : A.P - 1;
-                    e = A.WE + ((int64_t)c * A.P + col) * A.nb;
+                for (int i = 0; i < 2; ++i)
+                    wo[i] = tid / CPR * ldwb + swz_tr<T, CPR>(i * kDown + tid / CPR, tid % CPR) * E * es;
+            } else {
+                wb = W + (int64_t)q.bn * ldwb;
+                const int last = A.P - 1 - q.bn;   // columns past it: not stored
+#pragma unroll
+                for (int i = 0; i < NW; ++i) {
+                    const int col = (i * NT + tid) / 8;
+                    wo[i] = (uint32_t)(col < last ? col : last) * ldwb + uc * es;
                 }
-                const int left = A.nb - k0 < kWindow ? A.nb - k0 : kWindow;
-                uint8_t v[kWindow];
-                if (left == kWindow) {
-                    __builtin_memcpy(v, e + k0, kWindow);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < kWindow; ++q) v[q] = e[k0 + (q < left ? q : 0)];
-                }
-#pragma unroll
-                for (int q = 0; q < kWindow; ++q) s_scale[q * (TM + TN) + r] = v[q];
             }
-        }
-    };
+            bn_load = q.bn;
+            lk = 0;
+            whole = !TR || q.bn + TN <= A.P ? A.K / BK : 0;
+        };
+        // Chunk i (of NU + NW a thread) of the next stage to LDS; guard: it may lie past an end.
+        auto load = [&](int i, char* buf, bool guard) {
+            const char* src;
+            bool in = true;
+            char* to = buf + (i * NT + wave * 64) * 16;   // W's chunks follow U's
+            if (i < NU) {
+                src = ub + uo[i];
+                if (guard) in = lk * BK + uc < A.K;
+            } else if constexpr (TR) {
+                const int x = (i - NU) * NT + tid, kk = x / CPR;
+                src = wb + (uint64_t)((i - NU) * kDown) * ldwb + wo[(i - NU) % 2];
+                if (guard) in = lk * BK + kk < A.K && bn_load + swz_tr<T, CPR>(kk, x % CPR) * E < A.P;
+            } else {
+                src = wb + wo[i - NU];
+                if (guard) in = lk * BK + uc < A.K;
+            }
+            load_lds16(in ? (const void*)src : (const void*)zero_chunk, to);
+        };
+        auto load_part = [&](int q, char* buf) {   // of kParts
+            constexpr int N = NU + NW;
+            if (lk < whole) {
+#pragma unroll
+                for (int i = q * N / kParts; i < (q + 1) * N / kParts; ++i) load(i, buf, false);
+            } else {
+#pragma unroll
+                for (int i = q * N / kParts; i < (q + 1) * N / kParts; ++i) load(i, buf, true);
+            }
+            if (q == kParts - 1) {
+                ub += 128;
+                wb += TR ? (int64_t)BK * ldwb : 128;
+                ++lk;
+            }
+        };
+        // 8 bits: the scales of window w of this thread's row of tile q, to registers
+        // and from there to LDS.
+        uint32_t sv[2] = {0, 0};
+        auto fetch_scales = [&](const Tile& q, const int32_t* rows, int w) {
+            if constexpr (F8) {
+                const int64_t col = q.bn + tid - TM < A.P ? q.bn + tid - TM : A.P - 1;
+                const uint8_t* e = (tid < TM ? A.UE + (int64_t)rows[tid < TM ? tid : 0] * A.nb
+                                             : A.WE + ((int64_t)q.c * A.P + col) * A.nb) + w * kWindow;
+                const int left = A.nb - w * kWindow;
+                if (left >= kWindow) {
+                    __builtin_memcpy(sv, e, 8);
+                } else {
+                    sv[0] = sv[1] = 0x7f7f7f7f;
+#pragma unroll
+                    for (int x = 0; x < kWindow - 1; ++x)
+                        if (x < left) sv[x / 4] = (sv[x / 4] & ~(0xffu << x % 4 * 8)) | (uint32_t)e[x] << x % 4 * 8;
+                }
+            }
+        };
+        int window = 0;   // the one in use
+        auto put_scales = [&](int b) {
+            if constexpr (F8)
+                if (tid < TM + TN) __builtin_memcpy(s_scale + (b * (TM + TN) + tid) * kWindow, sv, 8);
+        };
 
-    typename P::Acc acc[FR][FC];
-#pragma unroll
-    for (int f = 0; f < FR; ++f)
-#pragma unroll
-        for (int h = 0; h < FC; ++h)
-#pragma unroll
-            for (int i = 0; i < 4 * P::kRuns; ++i) acc[f][h][i] = 0.0f;
-
-    // A lane's places in a stage; the second half of a row is 64 bytes off (one bit
-    // of the swizzled chunk).
-    auto tile_row = [&](int f) { return f / FP * kTurn + wr * (FP * R) + f % FP * R + li; };
-    const int ua = tile_row(0) * 128 + swz(li, P::chunk(lane)) * 16;
-    int wa[TR ? FC : 1];
-    if constexpr (TR) {
-#pragma unroll
-        for (int h = 0; h < FC; ++h) wa[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
-    } else {
-        wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, P::chunk(lane)) * 16;
-    }
-    struct Frags {
-        typename P::Frag b[FR], a[FC];
-    };
-    int sa[F8 ? FC : 1], sb[F8 ? FR : 1];   // 8 bits: the stage's scales
-    // Operand i of half s of a stage: first the columns' (TR: read_cols), then the rows'.
-    auto read = [&](Frags& F, int i, const char* buf, int s) {
-        if (i < FC) {
-            if constexpr (!TR) F.a[i] = P::read(buf, (wa[0] ^ (s * 64)) + i * (R * 128));
-        } else {
-            const int f = i - FC;
-            F.b[f] = P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128);
+        Tile cur = tile_at<TN>(A, items, t);
+        {
+            const int32_t row = fetch_row(cur);
+            if (tid < TM) s_rows[tid] = row;
+            __syncthreads();
         }
-    };
-    auto read_cols = [&](Frags& F, const char* buf, int s) {
+        point(cur, s_rows);
+        fetch_scales(cur, s_rows, 0);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) load_part(q, s_tiles + kt * kStage);
+        put_scales(0);
+
+        typename P::Acc acc[FR][FC];
+        auto clear = [&]() {
+#pragma unroll
+            for (int f = 0; f < FR; ++f)
+#pragma unroll
+                for (int h = 0; h < FC; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4 * P::kRuns; ++i) acc[f][h][i] = 0.0f;
+        };
+        // A lane's places in a stage; the second half of a row is 64 bytes off (one
+        // bit of the swizzled chunk).
+        const int ua = (G::row(0, wr) + li) * 128 + swz(li, P::chunk(lane)) * 16;
+        int wa[TR ? FC : 1];
         if constexpr (TR) {
-            u32x4 v[FC];
-            if (s == 0) read_tr_wait<T, CPR, 0>(v, buf, wa);
-            else read_tr_wait<T, CPR, KS>(v, buf, wa);
 #pragma unroll
-            for (int h = 0; h < FC; ++h) F.a[h].v = v[h];
+            for (int h = 0; h < FC; ++h) wa[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
+        } else {
+            wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, P::chunk(lane)) * 16;
         }
-    };
-    auto read_scales = [&](int kt) {
-        if constexpr (F8) {
-            const uint8_t* s = s_scale + kt % kWindow * (TM + TN);
+        // Operands: the rows' are replaced in place, each as soon as its products are
+        // under way; the columns' are held twice.
+        struct Cols {
+            typename P::Frag v[FC];
+        };
+        typename P::Frag rf[FR];
+        uint32_t sa[F8 ? FC : 1], sb[F8 ? FR : 1];   // 8 bits: the scales of four stages, this one's lowest
+        auto read_row = [&](int f, const char* buf, int s) {
+            rf[f] = P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128);
+        };
+        auto read_cols = [&](Cols& C, const char* buf, int s) {
+            if constexpr (TR) {
+                u32x4 v[FC];
+                if (s == 0) read_tr_wait<T, CPR, 0>(v, buf, wa);
+                else read_tr_wait<T, CPR, KS>(v, buf, wa);
 #pragma unroll
-            for (int h = 0; h < FC; ++h) sa[h] = s[TM + wc * (TN / WC) + h * R + li];
+                for (int h = 0; h < FC; ++h) C.v[h].v = v[h];
+            } else {
 #pragma unroll
-            for (int f = 0; f < FR; ++f) sb[f] = s[tile_row(f)];
+                for (int h = 0; h < FC; ++h) C.v[h] = P::read(buf, (wa[0] ^ (s * 64)) + h * (R * 128));
+            }
+        };
+        auto read_scales = [&](int kt) {
+            if constexpr (F8) {
+                if (kt % 4 == 0) {
+                    const char* s = s_scale + window * (TM + TN) * kWindow + kt % kWindow;
+#pragma unroll
+                    for (int h = 0; h < FC; ++h)
+                        sa[h] = *reinterpret_cast<const uint32_t*>(s + (TM + wc * (TN / WC) + h * R + li) * kWindow);
+#pragma unroll
+                    for (int f = 0; f < FR; ++f)
+                        sb[f] = *reinterpret_cast<const uint32_t*>(s + (G::row(f, wr) + li) * kWindow);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < FC; ++h) sa[h] >>= 8;
+#pragma unroll
+                    for (int f = 0; f < FR; ++f) sb[f] >>= 8;
+                }
+            }
+        };
+        int live = 0;
+        // Loads of a stage, reads of a half stage and the products of the one before
+        // are issued in turns, so that the matrix cores do not wait for either: the
+        // products of C; C2 and the rows' operands read from buf2 (half s2); the next
+        // stage loaded into bufl, if not null.
+        auto half = [&](const Cols& C, Cols& C2, const char* buf2, int s2, char* bufl) {
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+                if (bufl) load_part(q, bufl);
+                if (!TR && q == 0) read_cols(C2, buf2, s2);
+                if (q < live) {
+#pragma unroll
+                    for (int f = q * FP; f < (q + 1) * FP; ++f)
+#pragma unroll
+                        for (int h = 0; h < FC; ++h)
+                            acc[f][h] = P::mma(C.v[h], rf[f], acc[f][h], (int)sa[F8 ? h : 0], (int)sb[F8 ? f : 0]);
+                }
+#pragma unroll
+                for (int f = q * FP; f < (q + 1) * FP; ++f) read_row(f, buf2, s2);
+                __builtin_amdgcn_sched_barrier(0);
+                if (TR && q == 0) {   // while the first products are at work
+                    read_cols(C2, buf2, s2);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
+        // Every wave's reads of one stage and its loads of the next have ended.
+        auto turn = [&]() {
+            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        Cols C0, C1;
+        turn();
+#pragma unroll
+        for (int f = 0; f < FR; ++f) read_row(f, s_tiles, 0);
+        read_cols(C0, s_tiles, 0);
+        // Rows of three tiles are in LDS: a wave may write the next tile's while another
+        // still reads those of the tile before this one.
+        for (int at = 0, slot = 0, ahead = 1;; slot = ahead, ahead = ahead == 2 ? 0 : ahead + 1) {
+            const bool more = t + step < x1;
+            Tile next = cur;
+            int32_t row = 0;
+            if (more) {
+                next = tile_at<TN>(A, items, t + step);
+                row = fetch_row(next);
+            }
+            live = (cur.rows + kTurn - 1) / kTurn;
+            clear();
+            for (int kt = 0; kt < nk; ++kt, at ^= 1) {
+                char* here = s_tiles + at * kStage;
+                const char* there = s_tiles + (at ^ 1) * kStage;
+                read_scales(kt);
+                half(C0, C1, here, 1, nullptr);
+                if (kt == 0 && more && tid < TM) s_rows[ahead * TM + tid] = row;
+                if constexpr (F8) {
+                    // The scales of the next window, asked for a stage before (the next
+                    // tile's: with its pointers), go to LDS in the last stage of this one.
+                    const bool last = kt + 1 == nk;
+                    if (last ? more : (kt + 1) % kWindow == 0) put_scales(window ^= 1);
+                }
+                turn();
+                __builtin_amdgcn_sched_barrier(0);
+                if (kt + 2 == nk && more) point(next, s_rows + ahead * TM);
+                if constexpr (F8) {
+                    if (kt + 2 == nk ? more : (kt + 2) % kWindow == 0 && kt + 2 < nk) {
+                        const bool mine = kt + 2 < nk;
+                        fetch_scales(mine ? cur : next, s_rows + (mine ? slot : ahead) * TM,
+                                     mine ? (kt + 2) / kWindow : 0);
+                    }
+                }
+                // After the last stage the reads are of what the buffer held before, and are not used.
+                half(C1, C0, there, 0, kt + 2 < nk || more ? here : nullptr);
+            }
+#pragma unroll
+            for (int f = 0; f < FR; ++f) {
+                const int r = G::row(f, wr) + li;
+                O* y = static_cast<O*>(A.Y) + (int64_t)s_rows[slot * TM + r] * A.P;
+                put_row<P>(y, cur.bn + wc * (TN / WC), A.P, acc[f], lane, r < cur.rows);
+            }
+            if (!more) break;
+            t += step;
+            cur = next;
         }
-    };
-    auto products = [&](const Frags& F, int q) {
-        if (q >= live) return;
+    }
+    zero_rows<O>(A, WR * WC);
+}
+
+// The same at any address: a tile a block, a stage in registers while the one
+// before it is multiplied.
+template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
+__global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
+    using G = Geo<T, O, TM, TN, WR, WC>;
+    using P = typename G::P;
+    constexpr bool F8 = sizeof(T) == 1;
+    constexpr int E = G::E, R = G::R, KS = G::KS, BK = G::BK, NT = G::NT, FR = G::FR, FC = G::FC, NU = G::NU, NW = G::NW;
+    constexpr int CPR = G::CPR, kStage = G::kStage, kParts = G::kParts, FP = G::FP, kTurn = G::kTurn;
+    constexpr int kScales = 16;   // 8 bits: stages whose scales are in LDS
+    extern __shared__ __align__(16) char s_tiles[];
+    uint8_t* s_scale = reinterpret_cast<uint8_t*>(s_tiles + 2 * kStage);   // 8 bits: [TM + TN][kScales]
+    int32_t* s_rows = reinterpret_cast<int32_t*>(s_tiles + 2 * kStage + (F8 ? kScales * (TM + TN) : 0));
+    const int tid = threadIdx.x, lane = tid & 63, li = lane % R;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
+    const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
+    const int tiles = items * A.tn, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    if ((int)(blockIdx.x / 8) < per && t < tiles) {
+        const Tile q = tile_at<TN>(A, items, t);
+        const int nk = (A.K + BK - 1) / BK, live = (q.rows + kTurn - 1) / kTurn;
+        const int64_t ldw = TR ? A.P : A.K;
+        const T* const W = static_cast<const T*>(A.W) + (int64_t)q.c * A.K * A.P;
+        const T* up[NU];
+        const T* wp[NW];
+        const int uc = swz(tid / 8, tid % 8) * E;
 #pragma unroll
-        for (int f = q * FP; f < (q + 1) * FP; ++f)
+        for (int i = 0; i < NU; ++i) {
+            const int r = (i * NT + tid) / 8;
+            const int64_t row = row_of(A.order, q.p0 + (r < q.rows ? r : q.rows - 1));
+            up[i] = static_cast<const T*>(A.U) + row * A.ldu;
+            if (tid % 8 == 0) s_rows[r] = (int32_t)row;
+        }
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const int x = i * NT + tid;
+            if constexpr (TR) wp[i] = W + (int64_t)(x / CPR) * ldw;
+            else wp[i] = W + (q.bn + x / 8 < A.P ? q.bn + x / 8 : A.P - 1) * ldw;
+        }
+        auto fetch = [&](int i, int kt) -> u32x4 {
+            if (i < NU) return chunk_any(up[i], (int64_t)kt * BK + uc, A.K);
+            i -= NU;
+            if constexpr (TR) {
+                const int x = i * NT + tid, kk = x / CPR;
+                const bool in = kt * BK + kk < A.K;
+                return only_if(in, chunk_any(in ? wp[i] + (int64_t)kt * BK * ldw : W,
+                                             q.bn + swz_tr<T, CPR>(kk, x % CPR) * E, A.P));
+            } else {
+                return chunk_any(wp[i], (int64_t)kt * BK + uc, A.K);
+            }
+        };
+        // 8 bits: the scales of the stages from k0 on, a row a thread.
+        auto scales = [&](int k0) {
+            if constexpr (F8) {
+                for (int r = tid; r < TM + TN; r += NT) {
+                    const uint8_t* e;
+                    if (r < TM) {
+                        e = A.UE + row_of(A.order, q.p0 + (r < q.rows ? r : q.rows - 1)) * A.nb;
+                    } else {
+                        const int64_t col = q.bn + r - TM < A.P ? q.bn + r - TM : A.P - 1;
+                        e = A.WE + ((int64_t)q.c * A.P + col) * A.nb;
+                    }
+#pragma unroll
+                    for (int x = 0; x < kScales; ++x)
+                        if (k0 + x < A.nb) s_scale[r * kScales + x] = e[k0 + x];
+                }
+            }
+        };
+        typename P::Acc acc[FR][FC];
+#pragma unroll
+        for (int f = 0; f < FR; ++f)
 #pragma unroll
             for (int h = 0; h < FC; ++h)
-                acc[f][h] = P::mma(F.a[h], F.b[f], acc[f][h], sa[F8 ? h : 0], sb[F8 ? f : 0]);
-    };
-
-    if constexpr (!AL) {
-        // One stage in registers while the one before is multiplied.
+#pragma unroll
+                for (int i = 0; i < 4 * P::kRuns; ++i) acc[f][h][i] = 0.0f;
+        const int ua = (G::row(0, wr) + li) * 128 + swz(li, P::chunk(lane)) * 16;
+        int wa[TR ? FC : 1];
+        if constexpr (TR) {
+#pragma unroll
+            for (int h = 0; h < FC; ++h) wa[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
+        } else {
+            wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, P::chunk(lane)) * 16;
+        }
         u32x4 v[NU + NW];
         scales(0);
 #pragma unroll
         for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, 0);
         for (int kt = 0; kt < nk; ++kt) {
-            char* buf = s_tiles + kt % NS * kStage;
+            char* buf = s_tiles + (kt & 1) * kStage;
 #pragma unroll
             for (int i = 0; i < NU + NW; ++i) *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) = v[i];
             __syncthreads();
@@ -401,110 +708,52 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
 #pragma unroll
                 for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, kt + 1);
             }
-            read_scales(kt);
+            int sa[F8 ? FC : 1], sb[F8 ? FR : 1];
+            if constexpr (F8) {
+#pragma unroll
+                for (int h = 0; h < FC; ++h)
+                    sa[h] = s_scale[(TM + wc * (TN / WC) + h * R + li) * kScales + kt % kScales];
+#pragma unroll
+                for (int f = 0; f < FR; ++f) sb[f] = s_scale[(G::row(f, wr) + li) * kScales + kt % kScales];
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                Frags F;
+                typename P::Frag b[FR], a[FC];
 #pragma unroll
-                for (int i = 0; i < FR + FC; ++i) read(F, i, buf, s);
-                read_cols(F, buf, s);
+                for (int f = 0; f < FR; ++f) b[f] = P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128);
+                if constexpr (TR) {
+                    u32x4 x[FC];
+                    if (s == 0) read_tr_wait<T, CPR, 0>(x, buf, wa);
+                    else read_tr_wait<T, CPR, KS>(x, buf, wa);
 #pragma unroll
-                for (int q = 0; q < kParts; ++q) products(F, q);
+                    for (int h = 0; h < FC; ++h) a[h].v = x[h];
+                } else {
+#pragma unroll
+                    for (int h = 0; h < FC; ++h) a[h] = P::read(buf, (wa[0] ^ (s * 64)) + h * (R * 128));
+                }
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) {
+                    if (p >= live) continue;
+#pragma unroll
+                    for (int f = p * FP; f < (p + 1) * FP; ++f)
+#pragma unroll
+                        for (int h = 0; h < FC; ++h)
+                            acc[f][h] = P::mma(a[h], b[f], acc[f][h], sa[F8 ? h : 0], sb[F8 ? f : 0]);
+                }
             }
-            if (F8 && (kt + 1) % kWindow == 0 && kt + 1 < nk) {
+            if (F8 && (kt + 1) % kScales == 0 && kt + 1 < nk) {
                 __syncthreads();
                 scales(kt + 1);
             }
         }
-    } else {
-        auto load_all = [&](int kt, char* buf) {
 #pragma unroll
-            for (int i = 0; i < NU + NW; ++i) load(i, kt, buf, kt >= whole);
-        };
-#pragma unroll
-        for (int kt = 0; kt < NS; ++kt)
-            if (kt < nk) load_all(kt, s_tiles + kt * kStage);
-        scales(0);
-        // Operands are read from LDS half a stage ahead of their products, and a
-        // stage is loaded while the one before it is multiplied.  The barrier of a
-        // stage stands between its two halves of products, when the second half's
-        // operands are in registers, and loads, reads and products are issued in
-        // turns, so that the matrix cores do not wait for either.
-        // The products of F; F2 read from buf2 (half s2); kl >= 0: stage kl loaded into bufl.
-        auto half = [&](const Frags& F, Frags& F2, const char* buf2, int s2, int kl, char* bufl, bool guard) {
-#pragma unroll
-            for (int q = 0; q < kParts; ++q) {
-                if (kl >= 0) {
-#pragma unroll
-                    for (int i = q * (NU + NW) / kParts; i < (q + 1) * (NU + NW) / kParts; ++i) load(i, kl, bufl, guard);
-                }
-#pragma unroll
-                for (int i = q * (FR + FC) / kParts; i < (q + 1) * (FR + FC) / kParts; ++i) read(F2, i, buf2, s2);
-                products(F, q);
-                __builtin_amdgcn_sched_barrier(0);
-                if (TR && q == 0) {   // while the first products are at work
-                    read_cols(F2, buf2, s2);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        };
-        // This wave's operands have arrived (F2 of the half before).
-        auto arrived = [&]() { __builtin_amdgcn_s_waitcnt(0xc07f); };   // lgkmcnt(0)
-        // Every wave's reads of one stage and its loads of the next have ended; the
-        // loads of the stages behind that one (kBehind) may be on their way.
-        constexpr int kBehind = (NS - 2) * (NU + NW);
-        static_assert(kBehind < 64, "");
-        auto turn = [&](bool all) {
-            if (all) __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
-            else __builtin_amdgcn_s_waitcnt(0x0070 | (kBehind & 15) | (kBehind >> 4) << 14);
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        };
-        Frags F0, F1;
-        turn(true);
-#pragma unroll
-        for (int i = 0; i < FR + FC; ++i) read(F0, i, s_tiles, 0);
-        read_cols(F0, s_tiles, 0);
-        int at = 0;   // the stage's place in the ring
-        auto stage = [&](int kt, bool last) {
-            char* cur = s_tiles + at * kStage;
-            at = at + 1 == NS ? 0 : at + 1;
-            const char* nxt = s_tiles + at * kStage;
-            read_scales(kt);
-            arrived();
-            __builtin_amdgcn_sched_barrier(0);
-            half(F0, F1, cur, 1, -1, cur, false);
-            turn(last);
-            __builtin_amdgcn_sched_barrier(0);
-            // Every wave has the scales of this stage in registers: the window may move on.
-            if (F8 && (kt + 1) % kWindow == 0 && kt + 1 < nk) {
-                scales(kt + 1);
-                __syncthreads();
-            }
-            // After the last stage the reads are of what the buffer held before, and are not used.
-            half(F1, F0, nxt, 0, !last ? kt + NS : kt + NS < nk ? kt + NS : -1, cur, last);
-        };
-        int kt = 0;
-        for (; kt + NS < whole && kt + NS < nk; ++kt) stage(kt, false);
-        for (; kt < nk; ++kt) stage(kt, true);
+        for (int f = 0; f < FR; ++f) {
+            const int r = G::row(f, wr) + li;
+            O* y = static_cast<O*>(A.Y) + (int64_t)s_rows[r] * A.P;
+            put_row<P>(y, q.bn + wc * (TN / WC), A.P, acc[f], lane, r < q.rows);
+        }
     }
-
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int r = tile_row(f);
-        if (r >= rows) continue;
-        O* y = Y + (int64_t)s_rows[r] * A.P;
-#pragma unroll
-        for (int h = 0; h < FC; ++h)
-#pragma unroll
-            for (int j = 0; j < P::kRuns; ++j) {
-                f32x4 v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = acc[f][h][j * 4 + i];
-                store4(y, bn + wc * (TN / WC) + h * R + P::run(j, lane), A.P, v, A.y4);
-            }
-    }
+    zero_rows<O>(A, WR * WC);
 }
 
 // --------------------------------------------------------------------------
@@ -523,114 +772,239 @@ struct GradArgs {
     int32_t tq, tp;          // tiles
 };
 
-template <class T, int TM, int TN, int WR, int WC, bool AL>
-__global__ __launch_bounds__(64 * WR * WC) void k_gr_grad(GradArgs A) {
+// An item's tile: V's columns from bm, U's from bn.
+struct GradTile {
+    int c, p0, p1, slot, bm, bn;
+};
+template <int TM, int TN>
+__device__ __forceinline__ GradTile grad_tile_at(const GradArgs& A, int64_t t) {
+    const int each = A.tq * A.tp;
+    const int64_t item = t / each;
+    const GroupItem it = item_at(A.items, item);
+    // Down 4 tiles of V's columns before the next of U's.
+    const int in = (int)(t - item * each), group = 4 * A.tp, grp = in / group, m0 = grp * 4, at = in - grp * group;
+    const int gm = A.tq - m0 < 4 ? A.tq - m0 : 4;
+    return GradTile{it.c, it.p0, it.p1, it.slot, (m0 + at % gm) * TM, at / gm * TN};
+}
+// The j-th tile of an XCD: eight consecutive ones go to one, the next eight to the
+// next, so that all share the tiles of a long cluster.
+__device__ __forceinline__ int64_t grad_index(int64_t j) { return (j / 8 * 8 + blockIdx.x % 8) * 8 + j % 8; }
+
+template <class T, int TM, int TN, int WR, int WC>
+__device__ __forceinline__ void grad_put(const GradArgs& A, const GradTile& q,
+                                         const f32x4 (&acc)[TM / WR / 16][TN / WC / 16], int wr, int wc, int lane) {
+    const int64_t slot = q.slot < 0 ? q.c : q.slot, col = q.bn + wc * (TN / WC);
+#pragma unroll
+    for (int f = 0; f < TM / WR / 16; ++f) {
+        const int64_t r = q.bm + wr * (TM / WR) + f * 16 + (lane & 15), at = (slot * A.Q + r) * A.P;
+        if (q.slot < 0) put_row<Op<T, T>>(static_cast<T*>(A.out) + at, col, A.P, acc[f], lane, r < A.Q);
+        else put_row<Op<T, T>>(A.part + at, col, A.P, acc[f], lane, r < A.Q);
+    }
+}
+
+// Blocks stay and take tile after tile, two stages of 128 bytes a column being on
+// their way or in LDS, as in k_gr_main: a tile has few stages where clusters are
+// short, and what it starts and ends with is what they would wait for.
+template <class T, int TM, int TN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad(GradArgs A) {
+    constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC, es = sizeof(T);
+    constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
+    constexpr int CPR = TM / E, kDown = NT / CPR, N = BK / kDown;   // chunks a place; places from one chunk of a
+                                                                    // thread to its next; a thread's of a stage
+    constexpr int kStage = (TM + TN) * 128;
+    static_assert(TM == TN && FR % 4 == 0 && FC % 2 == 0 && kDown % 8 == 0, "");
+    extern __shared__ __align__(16) char s_tiles[];   // two stages: V, then U
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
+    const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp, step = gridDim.x / 8;
+    int64_t j = blockIdx.x / 8;
+    if (grad_index(j) >= tiles) return;
+    // This tile and the three after it (of no places where there are none).
+    auto tile = [&](int64_t x) {
+        const int64_t t = grad_index(x);
+        return t < tiles ? grad_tile_at<TM, TN>(A, t) : GradTile{0, 0, 0, 0, 0, 0};
+    };
+    GradTile q0 = tile(j), q1 = tile(j + step), q2 = tile(j + 2 * step), q3 = tile(j + 3 * step);
+
+    // The next stage to load: places lp .. of tile L, the ahead-th after this one.
+    GradTile L = q0;
+    int lp = L.p0, ahead = 0;
+    int32_t row[N];
+    const int kk = tid / CPR;
+    // The column of even and odd chunks (16 places further on the swizzle is the same).
+    const uint32_t colb[2] = {(uint32_t)swz_tr<T, CPR>(kk, tid % CPR) * 16,
+                              (uint32_t)swz_tr<T, CPR>(kDown + kk, tid % CPR) * 16};
+    const uint32_t ldub = (uint32_t)A.ldu * es, ldvb = (uint32_t)A.ldv * es;
+    auto rows = [&]() {   // of that stage, behind the bases of load()
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = lp + i * kDown + kk < L.p1 ? lp + i * kDown + kk : L.p0;
+            row[i] = A.order ? A.order[p] : p - L.p0;
+        }
+    };
+    auto load = [&](char* buf) {
+        const int64_t base = A.order ? 0 : L.p0;
+        const char* v = static_cast<const char*>(A.V) + (base * A.ldv + L.bm) * es;
+        const char* u = static_cast<const char*>(A.U) + (base * A.ldu + L.bn) * es;
+        char* to = buf + wave * 1024;
+        if (lp + BK <= L.p1 && L.bm + TM <= A.Q && L.bn + TN <= A.P) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                load_lds16(v + (uint32_t)((uint32_t)row[i] * ldvb + colb[i % 2]), to + i * (NT * 16));
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                load_lds16(u + (uint32_t)((uint32_t)row[i] * ldub + colb[i % 2]), to + TM * 128 + i * (NT * 16));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool in = lp + i * kDown + kk < L.p1;
+                const int c = (int)colb[i % 2] / es;
+                const char* a = v + (uint32_t)((uint32_t)row[i] * ldvb + colb[i % 2]);
+                const char* b = u + (uint32_t)((uint32_t)row[i] * ldub + colb[i % 2]);
+                load_lds16(in && L.bm + c < A.Q ? (const void*)a : (const void*)zero_chunk, to + i * (NT * 16));
+                load_lds16(in && L.bn + c < A.P ? (const void*)b : (const void*)zero_chunk, to + TM * 128 + i * (NT * 16));
+            }
+        }
+        lp += BK;
+        if (lp >= L.p1) {
+            ++ahead;
+            auto pick = [&](int a, int b, int c) { return ahead == 1 ? a : ahead == 2 ? b : c; };
+            L = GradTile{pick(q1.c, q2.c, q3.c),    pick(q1.p0, q2.p0, q3.p0), pick(q1.p1, q2.p1, q3.p1),
+                         pick(q1.slot, q2.slot, q3.slot), pick(q1.bm, q2.bm, q3.bm), pick(q1.bn, q2.bn, q3.bn)};
+            lp = L.p0;
+        }
+        if (L.p1 > L.p0) rows();
+    };
+    rows();
+    load(s_tiles);
+    if (L.p1 > L.p0) load(s_tiles + kStage);
+    int va[FR], ua[FC];
+#pragma unroll
+    for (int f = 0; f < FR; ++f) va[f] = tr_lane<T, CPR>(wr * (TM / WR) + f * 16, lane);
+#pragma unroll
+    for (int h = 0; h < FC; ++h) ua[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
+    auto turn = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    turn();
+    for (int at = 0;;) {
+        f32x4 acc[FR][FC];
+#pragma unroll
+        for (int f = 0; f < FR; ++f)
+#pragma unroll
+            for (int h = 0; h < FC; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
+        for (int p = q0.p0; p < q0.p1; p += BK, at ^= 1) {
+            char* buf = s_tiles + at * kStage;
+            auto half = [&](auto s) {
+                constexpr int K0 = decltype(s)::value;
+                u32x4 a[FC];
+#pragma unroll
+                for (int h = 0; h < FC; h += 2) {
+                    u32x4 v[2];
+                    const int q[2] = {ua[h], ua[h + 1]};
+                    read_tr_wait<T, CPR, K0>(v, buf, q);
+                    a[h] = v[0], a[h + 1] = v[1];
+                }
+#pragma unroll
+                for (int f = 0; f < FR; f += 4) {
+                    u32x4 b[4];
+                    const int q[4] = {va[f], va[f + 1], va[f + 2], va[f + 3]};
+                    read_tr_wait<T, CPR, K0>(b, buf, q);
+                    if (K0 != 0 && f + 4 == FR) {
+                        // All of the stage is in registers or multiplied: once every wave is
+                        // here, and the next stage has landed, the one behind it may come.
+                        turn();
+                        if (L.p1 > L.p0) load(buf);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int h = 0; h < FC; ++h) acc[f + i][h] = Mma<T>::mma(a[h], b[i], acc[f + i][h]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            half(std::integral_constant<int, 0>{});
+            half(std::integral_constant<int, KS>{});
+        }
+        grad_put<T, TM, TN, WR, WC>(A, q0, acc, wr, wc, lane);
+        if (q1.p1 <= q1.p0) break;
+        j += step;
+        q0 = q1, q1 = q2, q2 = q3;
+        q3 = tile(j + 3 * step);
+        --ahead;
+    }
+}
+
+// The same at any address: a tile a block, a stage in registers while the one
+// before it is multiplied.
+template <class T, int TM, int TN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
     constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
     constexpr int FR = TM / WR / 16, FC = TN / WC / 16;
-    constexpr int CM = TM / E, CN = TN / E;               // chunks a place of V and of U
-    constexpr int NV = BK * CM / NT, NU = BK * CN / NT;   // chunks a thread of a stage
+    constexpr int CPR = TM / E, N = BK * CPR / NT;
     constexpr int kStage = (TM + TN) * 128;
-    static_assert(FR % 4 == 0 && FC % 2 == 0, "");
-    extern __shared__ __align__(16) char s_tiles[];       // two stages: V, then U
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, li = lane & 15;
+    static_assert(TM == TN && FR % 4 == 0 && FC % 4 == 0, "");
+    extern __shared__ __align__(16) char s_tiles[];   // two stages: V, then U
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
-    const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
-    const int64_t each = (int64_t)A.tq * A.tp, tiles = items * each, per = (tiles + 7) / 8;
-    const int64_t t = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per || t >= tiles) return;
-    const GroupItem it = A.items[t / each];
-    // Down 4 tiles of V's columns before the next of U's.
-    const int64_t in = t % each, grp = in / (4 * (int64_t)A.tp), m0 = grp * 4;
-    const int gm = A.tq - m0 < 4 ? (int)(A.tq - m0) : 4;
-    const int64_t in_grp = in - grp * 4 * A.tp;
-    const int64_t bm = (m0 + in_grp % gm) * TM, bn = in_grp / gm * TN;
-    const int p1 = it.p1;
-
-    int64_t vr[NV], ur[NU];   // rows of the next stage to load
+    const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp, t = grad_index(blockIdx.x / 8);
+    if (t >= tiles) return;
+    const GradTile q = grad_tile_at<TM, TN>(A, t);
+    int64_t row[N];   // of the next stage to load
     auto rows = [&](int p) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int q = p + (i * NT + tid) / CM;
-            vr[i] = row_of(A.order, q < p1 ? q : it.p0);
-        }
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int q = p + (i * NT + tid) / CN;
-            ur[i] = row_of(A.order, q < p1 ? q : it.p0);
+        for (int i = 0; i < N; ++i) {
+            const int x = p + (i * NT + tid) / CPR;
+            row[i] = row_of(A.order, x < q.p1 ? x : q.p0);
         }
     };
-    // Where chunk i of V (v) or U comes from, and whether it is there.
-    auto chunk_of = [&](bool v, int i, int p, const T*& row, int64_t& col) {
-        const int q = i * NT + tid, cpr = v ? CM : CN, kk = q / cpr;
-        row = v ? static_cast<const T*>(A.V) + vr[i] * A.ldv : static_cast<const T*>(A.U) + ur[i] * A.ldu;
-        col = (v ? bm + swz_tr<T, CM>(kk, q % CM) * E : bn + swz_tr<T, CN>(kk, q % CN) * E);
-        return p + kk < p1;
-    };
-    u32x4 held[AL ? 1 : NV + NU];
-    auto load = [&](int p, char* buf) {
+    u32x4 held[2 * N];
+    auto load = [&](int p) {
 #pragma unroll
-        for (int i = 0; i < NV + NU; ++i) {
-            const bool v = i < NV;
-            const T* row;
-            int64_t col;
-            const bool in = chunk_of(v, v ? i : i - NV, p, row, col);
-            const int64_t width = v ? A.Q : A.P;
-            if constexpr (AL)
-                load_lds16(in && col < width ? (const void*)(row + col) : (const void*)zero_chunk,
-                           buf + (v ? 0 : TM * 128) + ((v ? i : i - NV) * NT + wave * 64) * 16);
-            else
-                held[i] = only_if(in, chunk_any(row, col, width));
+        for (int i = 0; i < N; ++i) {
+            const int x = i * NT + tid, k = x / CPR, c = swz_tr<T, CPR>(k, x % CPR) * E;
+            const bool in = p + k < q.p1;
+            held[i] = only_if(in, chunk_any(static_cast<const T*>(A.V) + row[i] * A.ldv, q.bm + c, A.Q));
+            held[N + i] = only_if(in, chunk_any(static_cast<const T*>(A.U) + row[i] * A.ldu, q.bn + c, A.P));
         }
-    };
-    auto put = [&](char* buf) {
-        if constexpr (!AL)
-#pragma unroll
-            for (int i = 0; i < NV + NU; ++i)
-                *reinterpret_cast<u32x4*>(buf + (i < NV ? 0 : TM * 128) + ((i < NV ? i : i - NV) * NT + tid) * 16) =
-                    held[i];
     };
     int va[FR], ua[FC];
 #pragma unroll
-    for (int f = 0; f < FR; ++f) va[f] = tr_lane<T, CM>(wr * (TM / WR) + f * 16, lane);
+    for (int f = 0; f < FR; ++f) va[f] = tr_lane<T, CPR>(wr * (TM / WR) + f * 16, lane);
 #pragma unroll
-    for (int h = 0; h < FC; ++h) ua[h] = TM * 128 + tr_lane<T, CN>(wc * (TN / WC) + h * 16, lane);
+    for (int h = 0; h < FC; ++h) ua[h] = TM * 128 + tr_lane<T, CPR>(wc * (TN / WC) + h * 16, lane);
     f32x4 acc[FR][FC];
 #pragma unroll
     for (int f = 0; f < FR; ++f)
 #pragma unroll
         for (int h = 0; h < FC; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
-
+    rows(q.p0);
+    load(q.p0);
+    rows(q.p0 + BK);
     int at = 0;
-    rows(it.p0);
-    load(it.p0, s_tiles);
-    rows(it.p0 + BK);
-    put(s_tiles);
-    for (int p = it.p0; p < p1; p += BK, at ^= 1) {
-        const char* buf = s_tiles + at * kStage;
-        char* other = s_tiles + (at ^ 1) * kStage;
-        // The stage has landed, and every wave is done with the other buffer.
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+    for (int p = q.p0; p < q.p1; p += BK, at ^= 1) {
+        char* buf = s_tiles + at * kStage;
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i)
+            *reinterpret_cast<u32x4*>(buf + (i < N ? 0 : TM * 128) + ((i % N) * NT + tid) * 16) = held[i];
         __syncthreads();
-        if (p + BK < p1) {
-            load(p + BK, other);
+        if (p + BK < q.p1) {
+            load(p + BK);
             rows(p + 2 * BK);
         }
-        __builtin_amdgcn_sched_barrier(0);
         auto half = [&](auto s) {
             constexpr int K0 = decltype(s)::value;
             u32x4 a[FC];
-#pragma unroll
-            for (int h = 0; h < FC; h += 2) {
-                u32x4 v[2];
-                const int q[2] = {ua[h], ua[h + 1]};
-                read_tr_wait<T, CN, K0>(v, buf, q);
-                a[h] = v[0], a[h + 1] = v[1];
-            }
+            read_tr_wait<T, CPR, K0>(a, buf, ua);
 #pragma unroll
             for (int f = 0; f < FR; f += 4) {
                 u32x4 b[4];
-                const int q[4] = {va[f], va[f + 1], va[f + 2], va[f + 3]};
-                read_tr_wait<T, CM, K0>(b, buf, q);
+                const int y[4] = {va[f], va[f + 1], va[f + 2], va[f + 3]};
+                read_tr_wait<T, CPR, K0>(b, buf, y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -639,21 +1013,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_grad(GradArgs A) {
         };
         half(std::integral_constant<int, 0>{});
         half(std::integral_constant<int, KS>{});
-        if (p + BK < p1) put(other);
     }
-    const int64_t slot = it.slot < 0 ? it.c : it.slot;
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int64_t q = bm + wr * (TM / WR) + f * 16 + li;
-        if (q >= A.Q) continue;
-        const int64_t at_row = (slot * A.Q + q) * A.P;
-#pragma unroll
-        for (int h = 0; h < FC; ++h) {
-            const int64_t col = bn + wc * (TN / WC) + h * 16 + g * 4;
-            if (it.slot < 0) store4(static_cast<T*>(A.out) + at_row, col, A.P, acc[f][h], A.o4);
-            else store4(A.part + at_row, col, A.P, acc[f][h], A.P % 4 == 0);
-        }
-    }
+    grad_put<T, TM, TN, WR, WC>(A, q, acc, wr, wc, lane);
 }
 
 // Clusters of no chunk: zeros; of several: the sum of their parts in order.
@@ -829,19 +1190,46 @@ hipError_t raise_lds(K* kernel, int bytes) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <class T, class O, int TM, int TN, int WR, int WC, int NS, bool TR, bool AL>
+constexpr int kCus = 256;
+
+bool a16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
 hipError_t main_tile(MainArgs A, int64_t max_items, hipStream_t s) {
     A.tn = (A.P + TN - 1) / TN;
-    constexpr int lds = NS * (TM + TN) * 128 + (sizeof(T) == 1 ? kWindow * (TM + TN) : 0) + TM * 4;
+    constexpr int lds = 2 * (TM + TN) * 128 + (sizeof(T) == 1 ? 2 * kWindow * (TM + TN) : 0) + 3 * TM * 4;
     static_assert(lds <= 160 * 1024, "");
     if (lds > 65536) {
-        const hipError_t e = raise_lds(k_gr_main<T, O, TM, TN, WR, WC, NS, TR, AL>, lds);
+        const hipError_t e = raise_lds(k_gr_main<T, O, TM, TN, WR, WC, TR>, lds);
         if (e != hipSuccess) return e;
     }
-    const int64_t tiles = max_items * A.tn;
-    hipLaunchKernelGGL((k_gr_main<T, O, TM, TN, WR, WC, NS, TR, AL>), dim3((unsigned)((tiles + 7) / 8 * 8)),
+    // As many blocks as the chip holds at once.
+    const int64_t tiles = (max_items * A.tn + 7) / 8 * 8, most = kCus * (TM == 256 ? 1 : 4);
+    hipLaunchKernelGGL((k_gr_main<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)(tiles < most ? tiles : most)),
                        dim3(64 * WR * WC), lds, s, A);
     return hipGetLastError();
+}
+
+template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
+hipError_t any_tile(MainArgs A, int64_t max_items, hipStream_t s) {
+    A.tn = (A.P + TN - 1) / TN;
+    constexpr int lds = 2 * (TM + TN) * 128 + (sizeof(T) == 1 ? 16 * (TM + TN) : 0) + TM * 4;
+    if (lds > 65536) {
+        const hipError_t e = raise_lds(k_gr_any<T, O, TM, TN, WR, WC, TR>, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_gr_any<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)((max_items * A.tn + 7) / 8 * 8)),
+                       dim3(64 * WR * WC), lds, s, A);
+    return hipGetLastError();
+}
+
+// Whether k_gr_main can take rows of K (ld apart) and weights: 16 bytes at a time,
+// places behind its bases below 4 GB.
+template <class T>
+bool main_ok(const void* U, int64_t ld, int64_t n, int64_t K, const void* W, int64_t w, const int32_t* order) {
+    const int64_t es = sizeof(T), most = (int64_t)1 << 32;
+    return rows_vec16(U, ld, K, es) && w * es % 16 == 0 && a16(W) && (order ? n : 256) * ld * es < most &&
+           256 * w * es < most;
 }
 
 // 8 bits with float32 results: widened operands take the registers of the larger
@@ -851,24 +1239,20 @@ constexpr bool kWide = sizeof(T) == 1 && sizeof(O) == 4;
 
 template <class T, class O, bool TR>
 hipError_t main_go(const MainArgs& A, const GroupList& L, bool al, hipStream_t s) {
-    if constexpr (kWide<T, O>) {
-        return main_tile<T, O, 128, 128, 2, 2, 2, TR, false>(A, L.max_items, s);
-    } else {
-    if (!al) return main_tile<T, O, 128, 128, 2, 2, 2, TR, false>(A, L.max_items, s);
-    if (L.size == 256) return main_tile<T, O, 256, 256, 2, 4, 2, TR, true>(A, L.max_items, s);
-    return main_tile<T, O, 64, 64, 2, 2, 2, TR, true>(A, L.max_items, s);
+    if constexpr (!kWide<T, O>) {
+        if (al && L.size == 256) return main_tile<T, O, 256, 256, 2, 4, TR>(A, L.max_items, s);
+        if (al) return main_tile<T, O, 64, 64, 2, 2, TR>(A, L.max_items, s);
     }
+    return any_tile<T, O, 128, 128, 2, 2, TR>(A, L.max_items, s);
 }
 
 // The list of row tiles as the launch takes it: tiles of 128 rows where rows or
 // weights cannot be read 16 bytes at a time.
 GroupList row_list(const GroupArgs& D, GroupList L, bool al) {
     if (!al) L.size = 128;
-    L.max_items = group_items(D.n, D.k, L.size) + 1;   // one list more: rows of no cluster
+    L.max_items = group_items(D.n, D.k, L.size);
     return L;
 }
-
-bool a16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <class T>
 bool rows16(const void* p, int64_t ld, int64_t d) {
@@ -878,7 +1262,6 @@ bool rows16(const void* p, int64_t ld, int64_t d) {
 ListArgs list_args(const GroupArgs& D, const GroupList& L, char* ws, bool cut) {
     ListArgs A{};
     A.offsets = D.offsets;
-    A.n = (int32_t)D.n;
     A.k = D.k;
     A.size = L.size;
     A.count = reinterpret_cast<int32_t*>(ws + L.off_count);
@@ -900,9 +1283,8 @@ hipError_t lists_go(const GroupArgs& D, const GroupList* rows, const GroupList* 
 
 template <class T, class O>
 hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStream_t s) {
-    const bool al = rows16<T>(D.X, D.ldx, D.di) && D.di % (16 / (int)sizeof(T)) == 0 && a16(D.W);
-    const int32_t y4 = D.dout % 4 == 0 && a16(D.Y);
     if (L.few) {
+        const bool al = rows16<T>(D.X, D.ldx, D.di) && D.di % (16 / (int)sizeof(T)) == 0 && a16(D.W);
         FewArgs F{};
         F.U = D.X;
         F.ldu = D.ldx;
@@ -918,13 +1300,14 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
         F.K = D.di;
         F.P = D.dout;
         F.nb = (D.di + 127) / 128;
-        F.y4 = y4;
+        F.y4 = D.dout % 4 == 0 && a16(D.Y);
         const dim3 g((unsigned)((D.dout + 15) / 16), (unsigned)D.n), b(1024);
         if (al) hipLaunchKernelGGL((k_gr_few<T, O, true>), g, b, 0, s, F);
         else hipLaunchKernelGGL((k_gr_few<T, O, false>), g, b, 0, s, F);
         return hipGetLastError();
     }
-    const GroupList rows = row_list(D, L.rows, al && !kWide<T, O>);
+    const bool al = !kWide<T, O> && main_ok<T>(D.X, D.ldx, D.n, D.di, D.W, D.di, D.order);
+    const GroupList rows = row_list(D, L.rows, al);
     const hipError_t e = lists_go(D, &rows, nullptr, ws, s);
     if (e != hipSuccess) return e;
     const ListArgs Q = list_args(D, rows, ws, false);
@@ -937,34 +1320,45 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
     M.order = D.order;
     M.count = Q.count;
     M.items = Q.items;
+    M.used = D.offsets + D.k;
+    M.n = D.n;
     M.Y = D.Y;
     M.K = D.di;
     M.P = D.dout;
     M.nb = (D.di + 127) / 128;
-    M.y4 = y4;
     return main_go<T, O, false>(M, rows, al, s);
 }
 
-template <class T, int TM, int TN, int WR, int WC, bool AL>
-hipError_t grad_tile(GradArgs A, int64_t max_items, hipStream_t s) {
-    A.tq = (A.Q + TM - 1) / TM;
-    A.tp = (A.P + TN - 1) / TN;
-    constexpr int lds = 2 * (TM + TN) * 128;
-    if (lds > 65536) {
-        const hipError_t e = raise_lds(k_gr_grad<T, TM, TN, WR, WC, AL>, lds);
-        if (e != hipSuccess) return e;
+template <class T, int TILE, int WC>
+hipError_t grad_tile(GradArgs A, int64_t max_items, bool al, hipStream_t s) {
+    A.tq = (A.Q + TILE - 1) / TILE;
+    A.tp = (A.P + TILE - 1) / TILE;
+    constexpr int lds = 2 * 2 * TILE * 128;
+    const int64_t tiles = (max_items * A.tq * A.tp + 63) / 64 * 64, most = kCus * (TILE == 256 ? 1 : 2);
+    if (al) {
+        if (lds > 65536) {
+            const hipError_t e = raise_lds(k_gr_grad<T, TILE, TILE, 2, WC>, lds);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL((k_gr_grad<T, TILE, TILE, 2, WC>), dim3((unsigned)(tiles < most ? tiles : most)),
+                           dim3(128 * WC), lds, s, A);
+    } else {
+        hipLaunchKernelGGL((k_gr_grad_any<T, 128, 128, 2, 2>), dim3((unsigned)tiles), dim3(256), 2 * 2 * 128 * 128, s, A);
     }
-    const int64_t tiles = max_items * A.tq * A.tp;
-    hipLaunchKernelGGL((k_gr_grad<T, TM, TN, WR, WC, AL>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(64 * WR * WC), lds,
-                       s, A);
     return hipGetLastError();
+}
+
+// Whether k_gr_grad can take rows of d, ld apart: 16 bytes at a time, places behind
+// its bases below 4 GB.
+template <class T>
+bool grad_ok(const void* U, int64_t ld, int64_t n, int64_t d, const int32_t* order, int64_t size) {
+    const int64_t es = sizeof(T);
+    return rows_vec16(U, ld, d, es) && (order ? n : size) * ld * es < (int64_t)1 << 32;
 }
 
 template <class T>
 hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStream_t s) {
-    constexpr int E = Mma<T>::E;
-    const bool y16 = rows16<T>(D.dY, D.lddy, D.dout), x16 = rows16<T>(D.X, D.ldx, D.di);
-    const bool al = y16 && D.di % E == 0 && a16(D.W);   // dX
+    const bool al = main_ok<T>(D.dY, D.lddy, D.n, D.dout, D.W, D.di, D.order);   // dX
     const GroupList rows = row_list(D, L.rows, al);
     const bool want = D.dX && D.n > 0;
     hipError_t e = want || D.dW ? lists_go(D, want ? &rows : nullptr, D.dW ? &L.cuts : nullptr, ws, s) : hipSuccess;
@@ -978,10 +1372,11 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
         M.order = D.order;
         M.count = Q.count;
         M.items = Q.items;
+        M.used = D.offsets + D.k;
+        M.n = D.n;
         M.Y = D.dX;
         M.K = D.dout;
         M.P = D.di;
-        M.y4 = D.di % 4 == 0 && a16(D.dX);
         e = main_go<T, T, true>(M, rows, al, s);
         if (e != hipSuccess) return e;
     }
@@ -1004,9 +1399,10 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
         G.Q = D.dout;
         G.o4 = D.di % 4 == 0 && a16(D.dW);
         if (L.cuts.max_items > 0) {
-            if (!(x16 && y16)) e = grad_tile<T, 128, 128, 2, 2, false>(G, L.cuts.max_items, s);
-            else if (L.grad_tile == 256) e = grad_tile<T, 256, 256, 2, 4, true>(G, L.cuts.max_items, s);
-            else e = grad_tile<T, 128, 128, 2, 2, true>(G, L.cuts.max_items, s);
+            const bool whole = grad_ok<T>(D.X, D.ldx, D.n, D.di, D.order, L.cuts.size) &&
+                               grad_ok<T>(D.dY, D.lddy, D.n, D.dout, D.order, L.cuts.size);
+            if (whole && L.grad_tile == 256) e = grad_tile<T, 256, 4>(G, L.cuts.max_items, true, s);
+            else e = grad_tile<T, 128, 2>(G, L.cuts.max_items, whole, s);
             if (e != hipSuccess) return e;
         }
         const int64_t gx = ((int64_t)D.dout * D.di + 1023) / 1024;
@@ -1035,7 +1431,7 @@ GroupShape group_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int type,
     if (!L.few) {
         const int64_t tall = (n + 255) / 256, wide = ((backward ? di : dout) + 255) / 256;
         L.rows.size = n >= 64 * met && tall * wide >= 64 ? 256 : 64;
-        L.rows.max_items = group_items(n, k, 64) + 1;   // 64: the least size of a tile
+        L.rows.max_items = group_items(n, k, 64);   // 64: the least size of a tile
         L.rows.off_count = take(4);
         L.rows.off_items = take((size_t)L.rows.max_items * sizeof(GroupItem));
     }

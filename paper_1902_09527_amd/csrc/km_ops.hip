@@ -435,7 +435,7 @@ static int linear_sizes(int64_t n, int32_t din, int32_t dout, int32_t k, int32_t
         return bad("sizes within 63 bits needed");
     // The grids: tiles of 64 rows and columns at least.
     const int64_t wide = (din > dout ? din : dout) / 64 + 1, most = INT32_MAX / wide;
-    if (km::group_items(n, k, 64) + 1 >= most || km::group_items(n, k, 256) >= most / (din / 128 + 1) / 2)
+    if (km::group_items(n, k, 64) >= most || km::group_items(n, k, 256) >= most / (din / 128 + 1) / 2)
         return km::ops_error(KM_ERR_UNSUPPORTED, "more than 2^31 tiles");
     return KM_OK;
 }
