@@ -12,6 +12,7 @@
 //
 // Sums are float32 (matrix-core accumulators); a result is rounded once.
 #include <limits.h>
+#include <math.h>
 
 #include "km_tile.h"
 
@@ -193,31 +194,37 @@ __device__ __forceinline__ void put4(O* row, int64_t col0, int64_t P, f32x4 v) {
     }
 }
 
-// A lane's part of two neighbouring operands' results (R rows by 2 R columns, from
-// column col0 of its row on) in 16 bits: lanes exchange halves first, so that each
-// writes 16 bytes.
-template <int R, class O>
-__device__ __forceinline__ void put8(O* row, int64_t col, int64_t P, f32x4 v, f32x4 w) {
-    struct Two {
-        uint32_t a, b;
-    };
-    Vec<O, 4> x, y;
+struct Two {
+    uint32_t a, b;
+};
+template <class O>
+__device__ __forceinline__ Two pack4(f32x4 v) {
+    Vec<O, 4> x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.e[i] = from_f32<O>(v[i]), y.e[i] = from_f32<O>(w[i]);
-    const Two p = __builtin_bit_cast(Two, x), q = __builtin_bit_cast(Two, y);
-    u32x4 o;
-    // The odd groups' part of the first operand against the even groups' of the second.
-    if constexpr (R == 16) {
-        const auto s = __builtin_amdgcn_permlane16_swap(p.a, q.a, false, false);
-        const auto t = __builtin_amdgcn_permlane16_swap(p.b, q.b, false, false);
-        o = u32x4{(uint32_t)s[0], (uint32_t)t[0], (uint32_t)s[1], (uint32_t)t[1]};
+    for (int i = 0; i < 4; ++i) x.e[i] = from_f32<O>(v[i]);
+    return __builtin_bit_cast(Two, x);
+}
+// The odd halves (rows of 16 or 32 lanes) of p against the even ones of q.
+template <int W>
+__device__ __forceinline__ void swap_rows(uint32_t& p, uint32_t& q) {
+    if constexpr (W == 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(p, q, false, false);
+        p = s[0], q = s[1];
     } else {
-        const auto s = __builtin_amdgcn_permlane32_swap(p.a, q.a, false, false);
-        const auto t = __builtin_amdgcn_permlane32_swap(p.b, q.b, false, false);
-        o = u32x4{(uint32_t)s[0], (uint32_t)t[0], (uint32_t)s[1], (uint32_t)t[1]};
+        const auto s = __builtin_amdgcn_permlane32_swap(p, q, false, false);
+        p = s[0], q = s[1];
     }
+}
+__device__ __forceinline__ uint32_t other_half16(uint32_t v) {   // of lane + 8 in its 16
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x128, 0xf, 0xf, false);   // row_ror:8
+}
+// 16 bytes to column col of a row of P, at any address.  STREAM: past the caches.
+template <bool STREAM, class O>
+__device__ __forceinline__ void put8(O* row, int64_t col, int64_t P, u32x4 o) {
     if (col + 8 <= P) {
-        __builtin_memcpy(row + col, &o, 16);
+        typedef u32x4 __attribute__((aligned(2))) any4;
+        if constexpr (STREAM) __builtin_nontemporal_store(o, reinterpret_cast<any4*>(row + col));
+        else __builtin_memcpy(row + col, &o, 16);
     } else {
         const Vec<O, 8> e = __builtin_bit_cast(Vec<O, 8>, o);
 #pragma unroll
@@ -226,34 +233,87 @@ __device__ __forceinline__ void put8(O* row, int64_t col, int64_t P, f32x4 v, f3
     }
 }
 
-// The results of a lane's row, FC operands of columns from col0 on.  Every lane of
-// the wave calls it (lanes exchange parts); `in`: the row is there.
-template <class Q, class O, int FC>
-__device__ __forceinline__ void put_row(O* row, int64_t col0, int64_t P, const typename Q::Acc (&acc)[FC], int lane,
-                                        bool in) {
-    const int64_t end = in ? P : 0;   // nothing is written past it
+// A wave's results of one operand of rows (Q::R of them) and FC of columns, from
+// column col0 on.  row(r): where row r of the operand goes, null: nowhere.  In 16
+// bits the lanes exchange parts first, so that 16 rows of 64 bytes are written at
+// once, or (LINES) 8 of 128, past the caches; every lane of the wave calls it.
+template <class Q, class O, bool LINES, int FC, class F>
+__device__ __forceinline__ void put_rows(const typename Q::Acc (&acc)[FC], int64_t col0, int64_t P, int lane, F&& row) {
     auto part = [&](int h, int j) {
         f32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = acc[h][j * 4 + i];
         return v;
     };
-    if constexpr (sizeof(O) == 2 && Q::R == 16 && FC % 2 == 0) {
-        const int g = lane >> 4;
+    if constexpr (sizeof(O) == 2 && FC * Q::R == 64) {
+        // x[s][i], y[s][i]: the first and last 32 columns of 16 rows, lane l holding
+        // row l % 16, eight columns from at on.
+        const int g = lane >> 4, li = lane & 15, at = (g & 1) * 16 + (g >> 1) * 8;
+        constexpr int S = Q::R / 16;
+        uint32_t x[S][4], y[S][4];
+        if constexpr (Q::R == 16) {
 #pragma unroll
-        for (int h = 0; h < FC; h += 2)
-            put8<16>(row, col0 + (h + (g & 1)) * 16 + (g >> 1) * 8, end, part(h, 0), part(h + 1, 0));
-    } else if constexpr (sizeof(O) == 2 && Q::R == 32) {
+            for (int h = 0; h < 4; h += 2) {
+                Two p = pack4<O>(part(h, 0)), q = pack4<O>(part(h + 1, 0));
+                swap_rows<16>(p.a, q.a);
+                swap_rows<16>(p.b, q.b);
+                uint32_t* o = h == 0 ? x[0] : y[0];
+                o[0] = p.a, o[1] = p.b, o[2] = q.a, o[3] = q.b;
+            }
+        } else {
 #pragma unroll
-        for (int h = 0; h < FC; ++h)
+            for (int h = 0; h < 2; ++h) {
+                uint32_t z[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; j += 2)
-                put8<32>(row, col0 + h * 32 + (j + (lane >> 5)) * 8, end, part(h, j), part(h, j + 1));
+                for (int j = 0; j < 4; j += 2) {
+                    Two p = pack4<O>(part(h, j)), q = pack4<O>(part(h, j + 1));
+                    swap_rows<32>(p.a, q.a);
+                    swap_rows<32>(p.b, q.b);
+                    uint32_t* o = z[j / 2];
+                    o[0] = p.a, o[1] = p.b, o[2] = q.a, o[3] = q.b;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    swap_rows<16>(z[0][i], z[1][i]);
+                    (h == 0 ? x : y)[0][i] = z[0][i];
+                    (h == 0 ? x : y)[S - 1][i] = z[1][i];
+                }
+            }
+        }
+        if constexpr (!LINES) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                O* p = row(s * 16 + li);
+                if (!p) continue;
+                put8<false>(p, col0 + at, P, u32x4{x[s][0], x[s][1], x[s][2], x[s][3]});
+                put8<false>(p, col0 + at + 32, P, u32x4{y[s][0], y[s][1], y[s][2], y[s][3]});
+            }
+            return;
+        }
+        const bool low = li < 8;
+        const int64_t col = col0 + at + (low ? 0 : 32);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            u32x4 o[2];   // rows 0 .. 7, 8 .. 15
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t t = other_half16(low ? y[s][i] : x[s][i]);
+                o[0][i] = low ? x[s][i] : t;
+                o[1][i] = low ? t : y[s][i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                O* p = row(s * 16 + i * 8 + (li & 7));
+                if (p) put8<true>(p, col, P, o[i]);
+            }
+        }
     } else {
+        O* p = row(lane % Q::R);
+        if (!p) return;
 #pragma unroll
         for (int h = 0; h < FC; ++h)
 #pragma unroll
-            for (int j = 0; j < Q::kRuns; ++j) put4(row, col0 + h * Q::R + Q::run(j, lane), end, part(h, j));
+            for (int j = 0; j < Q::kRuns; ++j) put4(p, col0 + h * Q::R + Q::run(j, lane), P, part(h, j));
     }
 }
 
@@ -270,6 +330,8 @@ struct MainArgs {
     void* Y;
     int32_t K, P, nb;
     int32_t tn;               // tiles of columns
+    int32_t splits, share;    // parts of the contraction, stages of one; more than one part: sums to part
+    float* part;              // splits x n x P, by place
 };
 
 // Rows of no cluster: zeros, by all blocks, a wave a row.
@@ -316,17 +378,19 @@ __device__ __forceinline__ GroupItem item_at(const GroupItem* items, int64_t i) 
     return GroupItem{v[0], v[1], v[2], v[3]};
 }
 
-// A tile of the list: places p0 .. of cluster c, columns bn .. .
+// A tile of the list: places p0 .. of cluster c, columns bn .. , stages k0 .. of the
+// contraction (part `split`).
 struct Tile {
-    int c, p0, rows, bn;
+    int c, p0, rows, bn, split, k0;
 };
-// Down 4 row tiles before the next columns.
+// A tile's parts, then down 4 row tiles before the next columns.
 template <int TN>
-__device__ __forceinline__ Tile tile_at(const MainArgs& A, int items, int t) {
+__device__ __forceinline__ Tile tile_at(const MainArgs& A, int items, int u) {
+    const int t = u / A.splits, split = u - t * A.splits;
     const int group = 4 * A.tn, grp = t / group, m0 = grp * 4, in = t - grp * group;
     const int gm = items - m0 < 4 ? items - m0 : 4;
     const GroupItem it = item_at(A.items, m0 + in % gm);
-    return Tile{it.c, it.p0, it.p1 - it.p0, in / gm * TN};
+    return Tile{it.c, it.p0, it.p1 - it.p0, in / gm * TN, split, split * A.share};
 }
 
 constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, twice
@@ -350,11 +414,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
 
     // Consecutive tiles go to one XCD (blocks are dealt over 8).
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
-    const int tiles = items * A.tn, per = (tiles + 7) / 8, step = gridDim.x / 8;
+    const int tiles = items * A.tn * A.splits, per = (tiles + 7) / 8, step = gridDim.x / 8;
     const int x0 = (blockIdx.x % 8) * per, x1 = x0 + per < tiles ? x0 + per : tiles;
     int t = x0 + blockIdx.x / 8;
     if (t < x1) {
-        const int stages = (A.K + BK - 1) / BK, nk = stages < 2 ? 2 : stages;
+        const int nk = A.share < 2 ? 2 : A.share;   // stages past the last are of zeros
         // Where a thread's chunks of the next stage come from: bases that move on with
         // the stages, the thread's places behind them being fixed (below 4 GB, as the
         // host sees to).
@@ -370,18 +434,18 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
             return tid < TM ? (int32_t)row_of(A.order, q.p0 + (tid < q.rows ? tid : q.rows - 1)) : 0;
         };
         auto point = [&](const Tile& q, const int32_t* rows) {
-            ub = static_cast<const char*>(A.U) + (A.order ? 0 : (int64_t)q.p0 * A.ldu * es);
+            ub = static_cast<const char*>(A.U) + (A.order ? 0 : (int64_t)q.p0 * A.ldu * es) + (int64_t)q.k0 * 128;
 #pragma unroll
             for (int i = 0; i < NU; ++i)
                 uo[i] = (uint32_t)(rows[(i * NT + tid) / 8] - (A.order ? 0 : q.p0)) * ldub + uc * es;
             const char* const W = static_cast<const char*>(A.W) + (int64_t)q.c * A.K * A.P * es;
             if constexpr (TR) {
-                wb = W + q.bn * es;
+                wb = W + (int64_t)q.bn * es + (int64_t)q.k0 * BK * ldwb;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     wo[i] = tid / CPR * ldwb + swz_tr<T, CPR>(i * kDown + tid / CPR, tid % CPR) * E * es;
             } else {
-                wb = W + (int64_t)q.bn * ldwb;
+                wb = W + (int64_t)q.bn * ldwb + (int64_t)q.k0 * 128;
                 const int last = A.P - 1 - q.bn;   // columns past it: not stored
 #pragma unroll
                 for (int i = 0; i < NW; ++i) {
@@ -390,7 +454,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
                 }
             }
             bn_load = q.bn;
-            lk = 0;
+            lk = q.k0;
             whole = !TR || q.bn + TN <= A.P ? A.K / BK : 0;
         };
         // Chunk i (of NU + NW a thread) of the next stage to LDS; guard: it may lie past an end.
@@ -431,6 +495,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
         uint32_t sv[2] = {0, 0};
         auto fetch_scales = [&](const Tile& q, const int32_t* rows, int w) {
             if constexpr (F8) {
+                w += q.k0 / kWindow;   // a part is of whole windows
                 const int64_t col = q.bn + tid - TM < A.P ? q.bn + tid - TM : A.P - 1;
                 const uint8_t* e = (tid < TM ? A.UE + (int64_t)rows[tid < TM ? tid : 0] * A.nb
                                              : A.WE + ((int64_t)q.c * A.P + col) * A.nb) + w * kWindow;
@@ -601,16 +666,25 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
             }
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
-                const int r = G::row(f, wr) + li;
-                O* y = static_cast<O*>(A.Y) + (int64_t)s_rows[slot * TM + r] * A.P;
-                put_row<P>(y, cur.bn + wc * (TN / WC), A.P, acc[f], lane, r < cur.rows);
+                const int r0 = G::row(f, wr);
+                const int64_t col = cur.bn + wc * (TN / WC);
+                // Lines of 128 bytes take registers that the largest tile does not have.
+                if (TM == 256 || A.splits == 1)
+                    put_rows<P, O, TM == 128>(acc[f], col, A.P, lane, [&](int r) {
+                        return r0 + r < cur.rows ? static_cast<O*>(A.Y) + (int64_t)s_rows[slot * TM + r0 + r] * A.P
+                                                 : nullptr;
+                    });
+                else if constexpr (TM < 256)   // the largest tile is for products of many
+                    put_rows<P, float, false>(acc[f], col, A.P, lane, [&](int r) {
+                        return r0 + r < cur.rows ? A.part + (cur.split * A.n + cur.p0 + r0 + r) * A.P : nullptr;
+                    });
             }
             if (!more) break;
             t += step;
             cur = next;
         }
     }
-    zero_rows<O>(A, WR * WC);
+    if (A.splits == 1) zero_rows<O>(A, WR * WC);
 }
 
 // The same at any address: a tile a block, a stage in registers while the one
@@ -629,10 +703,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
     const int tid = threadIdx.x, lane = tid & 63, li = lane % R;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
-    const int tiles = items * A.tn, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    const int tiles = items * A.tn * A.splits, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if ((int)(blockIdx.x / 8) < per && t < tiles) {
         const Tile q = tile_at<TN>(A, items, t);
-        const int nk = (A.K + BK - 1) / BK, live = (q.rows + kTurn - 1) / kTurn;
+        const int all = (A.K + BK - 1) / BK, end = q.k0 + A.share < all ? q.k0 + A.share : all;
+        const int live = (q.rows + kTurn - 1) / kTurn;
         const int64_t ldw = TR ? A.P : A.K;
         const T* const W = static_cast<const T*>(A.W) + (int64_t)q.c * A.K * A.P;
         const T* up[NU];
@@ -696,15 +771,15 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
             wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, P::chunk(lane)) * 16;
         }
         u32x4 v[NU + NW];
-        scales(0);
+        scales(q.k0);
 #pragma unroll
-        for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, 0);
-        for (int kt = 0; kt < nk; ++kt) {
+        for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, q.k0);
+        for (int kt = q.k0; kt < end; ++kt) {
             char* buf = s_tiles + (kt & 1) * kStage;
 #pragma unroll
             for (int i = 0; i < NU + NW; ++i) *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) = v[i];
             __syncthreads();
-            if (kt + 1 < nk) {
+            if (kt + 1 < end) {
 #pragma unroll
                 for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, kt + 1);
             }
@@ -712,9 +787,9 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
             if constexpr (F8) {
 #pragma unroll
                 for (int h = 0; h < FC; ++h)
-                    sa[h] = s_scale[(TM + wc * (TN / WC) + h * R + li) * kScales + kt % kScales];
+                    sa[h] = s_scale[(TM + wc * (TN / WC) + h * R + li) * kScales + (kt - q.k0) % kScales];
 #pragma unroll
-                for (int f = 0; f < FR; ++f) sb[f] = s_scale[(G::row(f, wr) + li) * kScales + kt % kScales];
+                for (int f = 0; f < FR; ++f) sb[f] = s_scale[(G::row(f, wr) + li) * kScales + (kt - q.k0) % kScales];
             }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -741,19 +816,51 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
                             acc[f][h] = P::mma(a[h], b[f], acc[f][h], sa[F8 ? h : 0], sb[F8 ? f : 0]);
                 }
             }
-            if (F8 && (kt + 1) % kScales == 0 && kt + 1 < nk) {
+            if (F8 && (kt + 1 - q.k0) % kScales == 0 && kt + 1 < end) {
                 __syncthreads();
                 scales(kt + 1);
             }
         }
 #pragma unroll
         for (int f = 0; f < FR; ++f) {
-            const int r = G::row(f, wr) + li;
-            O* y = static_cast<O*>(A.Y) + (int64_t)s_rows[r] * A.P;
-            put_row<P>(y, q.bn + wc * (TN / WC), A.P, acc[f], lane, r < q.rows);
+            const int r0 = G::row(f, wr);
+            const int64_t col = q.bn + wc * (TN / WC);
+            if (A.splits == 1)
+                put_rows<P, O, false>(acc[f], col, A.P, lane, [&](int r) {
+                    return r0 + r < q.rows ? static_cast<O*>(A.Y) + (int64_t)s_rows[r0 + r] * A.P : nullptr;
+                });
+            else
+                put_rows<P, float, false>(acc[f], col, A.P, lane, [&](int r) {
+                    return r0 + r < q.rows ? A.part + (q.split * A.n + q.p0 + r0 + r) * A.P : nullptr;
+                });
         }
     }
-    zero_rows<O>(A, WR * WC);
+    if (A.splits == 1) zero_rows<O>(A, WR * WC);
+}
+
+// The parts of the contraction, added in order: a block a place and 1024 columns.
+template <class O>
+__global__ __launch_bounds__(256) void k_gr_sum(MainArgs A) {
+    const int64_t place = blockIdx.x, col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4, step = A.n * A.P;
+    if (col >= A.P) return;
+    f32x4 v{0, 0, 0, 0};
+    if (place < A.used[0]) {
+        const float* p = A.part + place * A.P + col;
+        if (col + 4 <= A.P) {
+#pragma unroll 4
+            for (int q = 0; q < A.splits; ++q) {
+                f32x4 x;
+                __builtin_memcpy(&x, p + q * step, 16);
+                v += x;
+            }
+        } else {
+            for (int q = 0; q < A.splits; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (col + i < A.P) v[i] += p[q * step + i];
+        }
+    }
+    put4(static_cast<O*>(A.Y) + row_of(A.order, place) * A.P, col, A.P, v);
 }
 
 // --------------------------------------------------------------------------
@@ -796,9 +903,12 @@ __device__ __forceinline__ void grad_put(const GradArgs& A, const GradTile& q,
     const int64_t slot = q.slot < 0 ? q.c : q.slot, col = q.bn + wc * (TN / WC);
 #pragma unroll
     for (int f = 0; f < TM / WR / 16; ++f) {
-        const int64_t r = q.bm + wr * (TM / WR) + f * 16 + (lane & 15), at = (slot * A.Q + r) * A.P;
-        if (q.slot < 0) put_row<Op<T, T>>(static_cast<T*>(A.out) + at, col, A.P, acc[f], lane, r < A.Q);
-        else put_row<Op<T, T>>(A.part + at, col, A.P, acc[f], lane, r < A.Q);
+        const int64_t r0 = q.bm + wr * (TM / WR) + f * 16;
+        auto to = [&](auto* out) {
+            return [=, &A](int r) { return r0 + r < A.Q ? out + (slot * A.Q + r0 + r) * A.P : nullptr; };
+        };
+        if (q.slot < 0) put_rows<Op<T, T>, T, true>(acc[f], col, A.P, lane, to(static_cast<T*>(A.out)));
+        else put_rows<Op<T, T>, float, false>(acc[f], col, A.P, lane, to(A.part));
     }
 }
 
@@ -1192,6 +1302,12 @@ hipError_t raise_lds(K* kernel, int bytes) {
 
 constexpr int kCus = 256;
 
+// Stages of one of `splits` parts of `all` stages: whole windows of scales in 8 bits.
+int part_stages(int all, int splits, bool f8) {
+    const int share = (all + splits - 1) / splits;
+    return splits > 1 && f8 ? (share + 7) / 8 * 8 : share;
+}
+
 bool a16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
@@ -1204,7 +1320,7 @@ hipError_t main_tile(MainArgs A, int64_t max_items, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     // As many blocks as the chip holds at once.
-    const int64_t tiles = (max_items * A.tn + 7) / 8 * 8, most = kCus * (TM == 256 ? 1 : 4);
+    const int64_t tiles = (max_items * A.tn * A.splits + 7) / 8 * 8, most = kCus * (TM == 256 ? 1 : TM == 128 ? 2 : 4);
     hipLaunchKernelGGL((k_gr_main<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)(tiles < most ? tiles : most)),
                        dim3(64 * WR * WC), lds, s, A);
     return hipGetLastError();
@@ -1218,7 +1334,7 @@ hipError_t any_tile(MainArgs A, int64_t max_items, hipStream_t s) {
         const hipError_t e = raise_lds(k_gr_any<T, O, TM, TN, WR, WC, TR>, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_gr_any<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)((max_items * A.tn + 7) / 8 * 8)),
+    hipLaunchKernelGGL((k_gr_any<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)((max_items * A.tn * A.splits + 7) / 8 * 8)),
                        dim3(64 * WR * WC), lds, s, A);
     return hipGetLastError();
 }
@@ -1237,21 +1353,37 @@ bool main_ok(const void* U, int64_t ld, int64_t n, int64_t K, const void* W, int
 template <class T, class O>
 constexpr bool kWide = sizeof(T) == 1 && sizeof(O) == 4;
 
-template <class T, class O, bool TR>
-hipError_t main_go(const MainArgs& A, const GroupList& L, bool al, hipStream_t s) {
-    if constexpr (!kWide<T, O>) {
-        if (al && L.size == 256) return main_tile<T, O, 256, 256, 2, 4, TR>(A, L.max_items, s);
-        if (al) return main_tile<T, O, 64, 64, 2, 2, TR>(A, L.max_items, s);
-    }
-    return any_tile<T, O, 128, 128, 2, 2, TR>(A, L.max_items, s);
+// A product's tiles and parts as the launch takes them: those of any addresses where
+// rows or weights cannot be read 16 bytes at a time.
+struct MainPlan {
+    GroupList list;
+    int32_t splits;
+};
+MainPlan main_plan(const GroupArgs& D, const GroupShape& L, bool al) {
+    MainPlan M{L.rows, al ? L.splits : L.any_splits};
+    if (!al) M.list.size = 128;
+    M.list.max_items = group_items(D.n, D.k, M.list.size);
+    return M;
 }
 
-// The list of row tiles as the launch takes it: tiles of 128 rows where rows or
-// weights cannot be read 16 bytes at a time.
-GroupList row_list(const GroupArgs& D, GroupList L, bool al) {
-    if (!al) L.size = 128;
-    L.max_items = group_items(D.n, D.k, L.size);
-    return L;
+template <class T, class O, bool TR>
+hipError_t main_go(MainArgs A, const MainPlan& M, bool al, hipStream_t s) {
+    const int64_t items = M.list.max_items;
+    const int bk = 128 / (int)sizeof(T), all = (A.K + bk - 1) / bk;
+    A.splits = M.splits;
+    A.share = part_stages(all, M.splits, sizeof(T) == 1);
+    hipError_t e;
+    if constexpr (kWide<T, O>) {
+        e = any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+    } else {
+        if (!al) e = any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+        else if (M.list.size == 256) e = main_tile<T, O, 256, 256, 2, 4, TR>(A, items, s);
+        else if (M.list.size == 128) e = main_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+        else e = main_tile<T, O, 64, 64, 2, 2, TR>(A, items, s);
+    }
+    if (e != hipSuccess || A.splits == 1) return e;
+    hipLaunchKernelGGL((k_gr_sum<O>), dim3((unsigned)A.n, (unsigned)((A.P + 1023) / 1024)), dim3(256), 0, s, A);
+    return hipGetLastError();
 }
 
 template <class T>
@@ -1307,10 +1439,10 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
         return hipGetLastError();
     }
     const bool al = !kWide<T, O> && main_ok<T>(D.X, D.ldx, D.n, D.di, D.W, D.di, D.order);
-    const GroupList rows = row_list(D, L.rows, al);
-    const hipError_t e = lists_go(D, &rows, nullptr, ws, s);
+    const MainPlan plan = main_plan(D, L, al);
+    const hipError_t e = lists_go(D, &plan.list, nullptr, ws, s);
     if (e != hipSuccess) return e;
-    const ListArgs Q = list_args(D, rows, ws, false);
+    const ListArgs Q = list_args(D, plan.list, ws, false);
     MainArgs M{};
     M.U = D.X;
     M.ldu = D.ldx;
@@ -1326,7 +1458,8 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
     M.K = D.di;
     M.P = D.dout;
     M.nb = (D.di + 127) / 128;
-    return main_go<T, O, false>(M, rows, al, s);
+    M.part = reinterpret_cast<float*>(ws + L.off_split);
+    return main_go<T, O, false>(M, plan, al, s);
 }
 
 template <class T, int TILE, int WC>
@@ -1359,12 +1492,12 @@ bool grad_ok(const void* U, int64_t ld, int64_t n, int64_t d, const int32_t* ord
 template <class T>
 hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStream_t s) {
     const bool al = main_ok<T>(D.dY, D.lddy, D.n, D.dout, D.W, D.di, D.order);   // dX
-    const GroupList rows = row_list(D, L.rows, al);
+    const MainPlan plan = main_plan(D, L, al);
     const bool want = D.dX && D.n > 0;
-    hipError_t e = want || D.dW ? lists_go(D, want ? &rows : nullptr, D.dW ? &L.cuts : nullptr, ws, s) : hipSuccess;
+    hipError_t e = want || D.dW ? lists_go(D, want ? &plan.list : nullptr, D.dW ? &L.cuts : nullptr, ws, s) : hipSuccess;
     if (e != hipSuccess) return e;
     if (want) {
-        const ListArgs Q = list_args(D, rows, ws, false);
+        const ListArgs Q = list_args(D, plan.list, ws, false);
         MainArgs M{};
         M.U = D.dY;
         M.ldu = D.lddy;
@@ -1377,7 +1510,8 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
         M.Y = D.dX;
         M.K = D.dout;
         M.P = D.di;
-        e = main_go<T, T, true>(M, rows, al, s);
+        M.part = reinterpret_cast<float*>(ws + L.off_split);
+        e = main_go<T, T, true>(M, plan, al, s);
         if (e != hipSuccess) return e;
     }
     if (D.dW) {
@@ -1415,6 +1549,54 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
 
 }  // namespace
 
+namespace {
+
+// The tile and the parts of the contraction of a product, by an estimate of its time
+// (`met` clusters have rows; main: k_gr_main, else k_gr_any).
+struct MainChoice {
+    int32_t tile, splits;
+};
+MainChoice main_choice(int64_t n, int64_t met, int32_t K, int32_t P, int type, bool main) {
+    const int es = (int)row_type_bytes(type), all = (K + 128 / es - 1) / (128 / es);
+    const int i = type == kF32 ? 1 : type == kF8 ? 2 : 0;
+    // A compute unit holds `held` tiles at once.  A stage of as many takes `busy` us on
+    // a chip at work, and no stage less than `alone`; measured with 64 to 16,384 rows
+    // of 256 to 4096 (16-bit, float32 and 8-bit rows).  A tile starts and ends in the
+    // time of `edge` stages.
+    struct Kind {
+        int tile, held;
+        double busy[3], alone[3], edge[3];
+    };
+    const Kind kinds[3] = {{256, 1, {1.65, 7.2, 1.75}, {1.05, 7.0, 1.1}, {3.5, 1.0, 5.5}},
+                           {128, 2, {1.15, 3.3, 1.15}, {0.85, 1.7, 0.85}, {2.5, 1.0, 2.2}},
+                           {64, 4, {0.96, 1.55, 0.85}, {0.6, 0.6, 0.5}, {2.0, 1.0, 2.0}}};
+    const Kind anywhere{128, 2, {2.4, 4.5, 2.4}, {1.7, 2.6, 1.7}, {3.0, 2.0, 3.0}};
+    MainChoice best{128, 1};
+    double least = 0;
+    for (int q = 0; q < (main ? 3 : 1); ++q) {
+        const Kind& k = main ? kinds[q] : anywhere;
+        // A cluster's last tile is half full, and none has less than one.
+        double items = (double)n / k.tile + 0.5 * met;
+        if (items < met) items = (double)met;
+        for (int splits = 1; splits <= 16 && (splits == 1 || (k.tile < 256 && all / splits >= 4)); splits *= 2) {
+            const int share = part_stages(all, splits, type == kF8);
+            if (splits > 1 && share * (splits - 1) >= all) continue;   // no part without a stage
+            const double tiles = items * ((P + k.tile - 1) / k.tile) * splits, rounds = tiles / (kCus * k.held);
+            const double stage = tiles <= kCus ? k.alone[i] : k.busy[i];
+            // Small tiles make up for each other's waits.
+            double t = (k.tile == 64 && rounds > 1 ? rounds + 0.5 : ceil(rounds)) * stage * (share + k.edge[i]);
+            if (splits > 1) t += 6 + (double)splits * n * P * 8 / 4e6;   // sums at 4 TB/s, and a launch
+            if (least == 0 || t < least) {
+                least = t;
+                best = MainChoice{k.tile, splits};
+            }
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
 // Most items of up to `size` places that n places of k clusters are cut into.
 int64_t group_items(int64_t n, int32_t k, int32_t size) { return n / size + (k < n ? k : n); }
 
@@ -1429,8 +1611,13 @@ GroupShape group_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int type,
     L.few = !backward && n <= kGroupFew;
     const int64_t met = k < n ? k : n;   // most clusters with rows
     if (!L.few) {
-        const int64_t tall = (n + 255) / 256, wide = ((backward ? di : dout) + 255) / 256;
-        L.rows.size = n >= 64 * met && tall * wide >= 64 ? 256 : 64;
+        const int32_t K = backward ? dout : di, P = backward ? di : dout;
+        const MainChoice main = main_choice(n, met, K, P, type, true), any = main_choice(n, met, K, P, type, false);
+        L.rows.size = main.tile;
+        L.splits = main.splits;
+        L.any_splits = any.splits;
+        const int most = L.splits > L.any_splits ? L.splits : L.any_splits;
+        L.off_split = take(most > 1 ? (size_t)most * n * P * 4 : 0);
         L.rows.max_items = group_items(n, k, 64);   // 64: the least size of a tile
         L.rows.off_count = take(4);
         L.rows.off_items = take((size_t)L.rows.max_items * sizeof(GroupItem));

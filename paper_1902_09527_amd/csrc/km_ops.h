@@ -186,8 +186,9 @@ struct GroupList {
 };
 struct GroupShape {
     int32_t few, grad_tile;
+    int32_t splits, any_splits;   // parts of the contraction, and at any addresses
     GroupList rows, cuts;
-    size_t off_part, bytes;
+    size_t off_split, off_part, bytes;
 };
 int64_t group_items(int64_t n, int32_t k, int32_t size);   // most items that n places are cut into
 GroupShape group_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int type, bool backward);
