@@ -18,7 +18,7 @@ namespace km {
 
 namespace {
 
-constexpr int kNormMost = 120, kScaleMost = 90;   // tensors a launch: under 4 KB of arguments
+constexpr int kNormMost = 165, kScaleMost = 120;   // tensors a launch: under 4 KB of arguments
 constexpr int kThreads = 256;
 constexpr int kClipUnroll = 4;                    // loads in flight a lane
 
@@ -147,6 +147,8 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(ScaleSet A) {
     else if (e.type == kBF16) scaled(static_cast<const __bf16*>(e.p), static_cast<__bf16*>(e.q), a, b, f);
     else scaled(static_cast<const _Float16*>(e.p), static_cast<_Float16*>(e.q), a, b, f);
 }
+
+static_assert(sizeof(NormSet) <= 4096 && sizeof(ScaleSet) <= 4096, "");
 
 }  // namespace
 

@@ -399,7 +399,7 @@ constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, 
 // one sequence: two of them are in LDS, and the next tile's first ones are on their
 // way while the last ones of a tile are multiplied and its results are written.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
-__global__ __launch_bounds__(64 * WR * WC) void k_gr_main(MainArgs A) {
+__global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(MainArgs A) {
     using G = Geo<T, O, TM, TN, WR, WC>;
     using P = typename G::P;
     constexpr bool F8 = sizeof(T) == 1;
@@ -1127,28 +1127,40 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
     grad_put<T, TM, TN, WR, WC>(A, q, acc, wr, wc, lane);
 }
 
-// Clusters of no chunk: zeros; of several: the sum of their parts in order.
+// Clusters of no chunk: zeros; of several: the sum of their parts in order.  16
+// bytes a lane, past the caches.
 template <class T>
 __global__ __launch_bounds__(256) void k_gr_join(GradArgs A) {
-    const int64_t size = (int64_t)A.Q * A.P, step = (int64_t)gridDim.x * 1024;
-    const bool by4 = A.o4 && size % 4 == 0;
+    constexpr int E = 16 / (int)sizeof(T);
+    const int64_t size = (int64_t)A.Q * A.P, step = (int64_t)gridDim.x * 256 * E;
+    const int64_t first = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
     for (int c = blockIdx.y; c < A.k; c += gridDim.y) {
         const int num = A.num[c];
         if (num == 1) continue;
         const float* part = A.part + A.first[c] * size;
         T* out = static_cast<T*>(A.out) + c * size;
-        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += step) {
-            f32x4 v{0, 0, 0, 0};
-            if (by4) {
+        for (int64_t i = first; i < size; i += step) {
+            float v[E] = {};
+            if (i + E <= size) {
 #pragma unroll 4
-                for (int q = 0; q < num; ++q) v += *reinterpret_cast<const f32x4*>(part + q * size + i);
-            } else {
-                for (int q = 0; q < num; ++q)
+                for (int q = 0; q < num; ++q) {
+                    float x[E];
+                    __builtin_memcpy(x, part + q * size + i, sizeof(x));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (i + e < size) v[e] += part[q * size + i + e];
+                    for (int e = 0; e < E; ++e) v[e] += x[e];
+                }
+                Vec<T, E> o;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o.e[e] = from_f32<T>(v[e]);
+                typedef u32x4 __attribute__((aligned(2))) any4;
+                __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), reinterpret_cast<any4*>(out + i));
+            } else {
+                for (int e = 0; i + e < size; ++e) {
+                    float x = 0.0f;
+                    for (int q = 0; q < num; ++q) x += part[q * size + i + e];
+                    out[i + e] = from_f32<T>(x);
+                }
             }
-            store4(out, i, size, v, by4);
         }
     }
 }
@@ -1539,9 +1551,9 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
             else e = grad_tile<T, 128, 2>(G, L.cuts.max_items, whole, s);
             if (e != hipSuccess) return e;
         }
-        const int64_t gx = ((int64_t)D.dout * D.di + 1023) / 1024;
-        hipLaunchKernelGGL((k_gr_join<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(D.k < 1024 ? D.k : 1024)),
-                           dim3(256), 0, s, G);
+        // Some 16 blocks a compute unit: most clusters have one chunk, which is no work here.
+        const int64_t gy = D.k < 1024 ? D.k : 1024, wide = ((int64_t)D.dout * D.di + 2047) / 2048, gx = 4096 / gy;
+        hipLaunchKernelGGL((k_gr_join<T>), dim3((unsigned)(wide < gx ? wide : gx), (unsigned)gy), dim3(256), 0, s, G);
         e = hipGetLastError();
     }
     return e;

@@ -34,8 +34,9 @@ on.  Call them under ``torch.no_grad()``, or in the forward and backward of a
 """
 from __future__ import annotations
 
-import ctypes
+import array
 import math
+import operator
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -625,47 +626,52 @@ def cluster_embedding_backward(dY: torch.Tensor, plan: ClusterPlan, scale: float
     return out
 
 
-def _tensors(tensors: Sequence[torch.Tensor], name: str) -> List[torch.Tensor]:
-    """Check a list of contiguous tensors of one device."""
+# A list of many small tensors costs the host more than the GPU: what is asked of
+# each is asked by map over the list.
+_dtype, _grad = operator.attrgetter("dtype"), operator.attrgetter("requires_grad")
+
+
+def _tensors(tensors: Sequence[torch.Tensor], name: str) -> Tuple[list, List[int], list]:
+    """Check a list of contiguous tensors of one device; (tensors, sizes, dtypes)."""
     given = list(tensors)
-    for t in given:
-        if not isinstance(t, torch.Tensor):
-            raise TypeError("%s must be torch.Tensors" % name)
-    for t in given:
-        if not t.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
-    if len({t.get_device() for t in given}) > 1 or (given and not given[0].is_cuda):
+    if not set(map(type, given)) <= {torch.Tensor, torch.nn.Parameter} \
+            and not all(isinstance(t, torch.Tensor) for t in given):
+        raise TypeError("%s must be torch.Tensors" % name)
+    if not given:
+        raise ValueError("%s: at least one is needed" % name)
+    if not all(map(torch.Tensor.is_contiguous, given)):
+        raise ValueError("%s must be contiguous" % name)
+    if len(set(map(torch.Tensor.get_device, given))) > 1 or not given[0].is_cuda:
         raise ValueError("%s must be on one GPU device" % name)
-    if not {t.dtype for t in given} <= _TYPES.keys():
+    dtypes = list(map(_dtype, given))
+    if not set(dtypes) <= _TYPES.keys():
         raise ValueError("%s must be float32, bfloat16 or float16" % name)
-    return given
+    return given, list(map(torch.Tensor.numel, given)), dtypes
 
 
 def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]], inplace: bool,
           stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    given = _tensors(tensors, "tensors")
-    if not given:
-        raise ValueError("at least one tensor is needed")
+    given, sizes, dtypes = _tensors(tensors, "tensors")
     dev, count = given[0].device, len(given)
-    sizes = [t.numel() for t in given]
-    pointers = [t.data_ptr() for t in given]
-    types = [_TYPES[t.dtype] for t in given]
-    targets, to = None, given if inplace else []
+    if torch.is_grad_enabled() and any(map(_grad, given)):
+        _On(dev, stream, tuple(given))   # refuses
+    pointers = array.array("Q", map(torch.Tensor.data_ptr, given))
+    to = []
+    targets = pointers if inplace else None
     if out is not None:
-        to = _tensors(out, "out")
-        if len(to) != count or [t.numel() for t in to] != sizes or [t.dtype for t in to] != [t.dtype for t in given] \
-                or to[0].get_device() != given[0].get_device():
+        to, to_sizes, to_dtypes = _tensors(out, "out")
+        if to_sizes != sizes or to_dtypes != dtypes or to[0].get_device() != given[0].get_device():
             raise ValueError("out must have the tensors' sizes, types and device")
-        targets = (ctypes.c_void_p * count)(*[t.data_ptr() for t in to])
-    array = (ctypes.c_void_p * count)(*pointers)
-    if inplace:
-        targets = array
-    sizes_ = (ctypes.c_int64 * count)(*sizes)
+        targets = array.array("Q", map(torch.Tensor.data_ptr, to))
+    kinds = array.array("i", [_TYPES[dtypes[0]]]) * count if len(set(dtypes)) == 1 else \
+        array.array("i", [_TYPES[t] for t in dtypes])
+    lengths = array.array("q", sizes)
+    at = lambda a: None if a is None else a.buffer_info()[0]
     lib = N.load()
-    with _On(dev, stream, tuple(given) + tuple(to) if out is not None else tuple(given)) as s:
+    with _On(dev, stream, tuple(given + to) if stream is not None else ()) as s:
         norm = torch.empty((), dtype=torch.float32, device=dev)
-        ws = _workspace(lib.kmeans_clip_workspace_bytes(sizes_, count), dev, "kmeans_clip_workspace_bytes")
-        st = lib.kmeans_clip_norm(array, targets, sizes_, (ctypes.c_int32 * count)(*types), count, limit, _p(norm), _p(ws),
+        ws = _workspace(lib.kmeans_clip_workspace_bytes(at(lengths), count), dev, "kmeans_clip_workspace_bytes")
+        st = lib.kmeans_clip_norm(at(pointers), at(targets), at(lengths), at(kinds), count, limit, _p(norm), _p(ws),
                                   ws.numel(), s)
     N.check(st, "kmeans_clip_norm")
     return norm
