@@ -233,8 +233,8 @@ hipError_t launch_table_bwd(const TableArgs& A, const TableShape& L, int type, h
 // ---- the norm over many tensors (km_clip.hip)
 
 struct ClipShape {
-    int32_t step;    // elements a block
-    int64_t parts;   // blocks of all tensors
+    int32_t step, scale_step;   // elements a block, of the first and the second pass
+    int64_t parts;              // blocks of the first pass
     size_t bytes;
 };
 ClipShape clip_shape(const int64_t* sizes, int32_t count);
