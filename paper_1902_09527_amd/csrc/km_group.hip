@@ -106,23 +106,6 @@ struct Op<uint8_t, float> {
     static __device__ __forceinline__ int run(int, int lane) { return (lane >> 4) * 4; }
 };
 
-// 16 bytes of a row from element k0 on, zero past its K elements, at any address.
-template <class T>
-__device__ __forceinline__ u32x4 chunk_any(const T* row, int64_t k0, int64_t K) {
-    constexpr int E = 16 / (int)sizeof(T);
-    if (k0 + E <= K) {
-        u32x4 v;
-        __builtin_memcpy(&v, row + k0, 16);
-        return v;
-    }
-    Vec<T, E> v;
-#pragma unroll
-    for (int e = 0; e < E; ++e) v.e[e] = row[k0 + e < K ? k0 + e : 0];
-#pragma unroll
-    for (int e = 0; e < E; ++e) v.e[e] = k0 + e < K ? v.e[e] : (T)0.0f;
-    return __builtin_bit_cast(u32x4, v);
-}
-
 // --------------------------------------------------------------------------
 // Lists of row tiles and of chunks.
 

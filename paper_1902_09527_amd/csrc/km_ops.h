@@ -206,8 +206,7 @@ hipError_t launch_dequantize(const uint8_t* Q, const uint8_t* E, int64_t n, int3
 
 // ---- rows of a table (km_table.hip)
 
-constexpr int kTableShort = 32;    // slots up to which an id is summed by the lanes of its row
-constexpr int kTableChunk = 1024;  // most places of a chunk
+constexpr int kTableChunk = 32;   // places of a chunk
 
 struct TableArgs {
     const int32_t* ids;                       // forward
@@ -218,11 +217,12 @@ struct TableArgs {
     float scale;
     void* out;                                // rows, or the table's gradient
     float* part;                              // backward: chunks x 2 x d
-    int32_t chunk, lanes, slices;             // backward, set by the launch
-    uint32_t long_blocks;
+    int32_t lanes, slices;                    // set by the launch: log2 of the lanes of a row's slice; slices
+    int32_t tests, by_chunk;                  // backward, as the following
+    uint32_t chunk_blocks;
 };
 struct TableShape {
-    int32_t chunk, lanes, slices;   // places a chunk; log2 of the lanes of a row's slice; slices
+    int32_t lanes, slices;
     int64_t chunks;
     size_t bytes;
 };

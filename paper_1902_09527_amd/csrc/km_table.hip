@@ -2,12 +2,12 @@
 //   y_i = s T[id_i],  dT[c] = s sum over the slots of id c of dy.
 //
 // The gradient goes by the sorted plan, so that no sum depends on the order of
-// atomics.  Ids of few slots are summed by the lanes of their row.  Of an id with
-// more, the places are cut into fixed chunks, whose float32 sums are joined in
-// order.  A chunk is a block, and an id of many slots may begin in one chunk,
-// cover others and end in a last one: every chunk has two places for what it
-// cannot finish, the part of an id that began before it and of one that goes on
-// behind it.
+// atomics.  The places are cut into chunks of kTableChunk, whatever their ids, and
+// the lanes of a row sum a chunk's rows in order, writing an id's sum where its
+// places end.  An id that began before a chunk or goes on behind it leaves a float32
+// part there (a chunk has two places for them), and a second kernel adds the parts
+// of such ids in order.  So every lane's chain of loads that wait for one another is
+// the same few, be the ids even or one of them everything.
 //
 // Bound by the memory's rate: 16 bytes a lane, rows at any address.
 #include "km_tile.h"
@@ -16,29 +16,24 @@ namespace km {
 
 namespace {
 
+constexpr int64_t kStreamBytes = 32 << 20;   // results of more go past the caches
+
 // A lane's 16 bytes of a row of d elements.
 template <class T>
 using Part = Vec<T, 16 / (int)sizeof(T)>;
 
-template <class T>
-__device__ __forceinline__ Part<T> part_get(const T* row, int64_t c, int64_t d) {
-    constexpr int E = 16 / (int)sizeof(T);
-    Part<T> v;
-    if (c + E <= d) {
-        __builtin_memcpy(&v, row + c, 16);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v.e[e] = row[c + e < d ? c + e : 0];
-    }
-    return v;
-}
-template <class T, int E>
+template <bool STREAM, class T, int E>
 __device__ __forceinline__ void part_put(T* row, int64_t c, int64_t d, const float (&v)[E]) {
     Vec<T, E> o;
 #pragma unroll
     for (int e = 0; e < E; ++e) o.e[e] = from_f32<T>(v[e]);
     if (c + E <= d) {
-        __builtin_memcpy(row + c, &o, sizeof(o));
+        if constexpr (STREAM && sizeof(o) == 16) {
+            typedef u32x4 __attribute__((aligned(2))) any4;
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), reinterpret_cast<any4*>(row + c));
+        } else {
+            __builtin_memcpy(row + c, &o, sizeof(o));
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -46,220 +41,252 @@ __device__ __forceinline__ void part_put(T* row, int64_t c, int64_t d, const flo
     }
 }
 
-template <class T>
+// A row is taken by 2^A.lanes lanes, 16 bytes each, in A.slices slices: unit u is
+// slice u % slices of row u / slices.  Divisions by a row's width would cost more than
+// the row (50,000 rows of 1024 bf16 written: 46 us with them, 30 without).
+struct Unit {
+    int64_t row, col;
+};
+template <int E>
+__device__ __forceinline__ Unit unit_at(const TableArgs& A, int64_t u) {
+    int64_t row = u, slice = 0;
+    if (A.slices > 1) {
+        row = u / A.slices;
+        slice = u - row * A.slices;
+    }
+    return Unit{row, ((slice << A.lanes) + (threadIdx.x & ((1 << A.lanes) - 1))) * E};
+}
+
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void k_table_fwd(TableArgs A) {
     constexpr int E = 16 / (int)sizeof(T), UN = 4;
-    const int64_t per = (A.d + E - 1) / E, total = A.n * per, step = (int64_t)gridDim.x * 256;
-    for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += UN * step) {
-        int64_t row[UN], col[UN];
+    const int64_t total = A.n * A.slices, step = (int64_t)gridDim.x << (8 - A.lanes);
+    for (int64_t u0 = ((int64_t)blockIdx.x << (8 - A.lanes)) + (threadIdx.x >> A.lanes); u0 < total; u0 += UN * step) {
+        Unit u[UN];
         int id[UN];
-        Part<T> v[UN];
+        u32x4 v[UN];
 #pragma unroll
         for (int y = 0; y < UN; ++y) {
-            const int64_t i = i0 + y * step < total ? i0 + y * step : i0;
-            row[y] = i / per;
-            col[y] = (i - row[y] * per) * E;
-            id[y] = A.ids[row[y]];
+            u[y] = unit_at<E>(A, u0 + y * step < total ? u0 + y * step : u0);
+            id[y] = A.ids[u[y].row];
         }
 #pragma unroll
         for (int y = 0; y < UN; ++y)
-            v[y] = part_get(static_cast<const T*>(A.table) + ((unsigned)id[y] < (unsigned)A.k ? id[y] : 0) * A.ld, col[y],
-                            A.d);
+            if (u[y].col < A.d)
+                v[y] = chunk_any(static_cast<const T*>(A.table) + ((unsigned)id[y] < (unsigned)A.k ? id[y] : 0) * A.ld,
+                                 u[y].col, A.d);
 #pragma unroll
         for (int y = 0; y < UN; ++y) {
-            if (i0 + y * step >= total) break;
+            if (u0 + y * step >= total) break;
+            if (u[y].col >= A.d) continue;
             float o[E];
             const bool in = (unsigned)id[y] < (unsigned)A.k;
+            const Part<T> x = __builtin_bit_cast(Part<T>, v[y]);
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = in ? to_f32(v[y].e[e]) * A.scale : 0.0f;
-            part_put(static_cast<T*>(A.out) + row[y] * A.d, col[y], A.d, o);
+            for (int e = 0; e < E; ++e) o[e] = in ? to_f32(x.e[e]) * A.scale : 0.0f;
+            part_put<STREAM>(static_cast<T*>(A.out) + u[y].row * A.d, u[y].col, A.d, o);
         }
     }
 }
 
 // --------------------------------------------------------------------------
 
-// By a lane an id and 16 bytes of its row: ids of at most kTableShort slots.
+// Rows of ids without slots: zeros.
 template <class T>
-__device__ __forceinline__ void short_ids(const TableArgs& A, int64_t block, int64_t blocks) {
+__device__ __forceinline__ void no_slots(const TableArgs& A, int64_t block, int64_t blocks) {
     constexpr int E = 16 / (int)sizeof(T), UN = 4;
-    const int64_t per = (A.d + E - 1) / E, total = A.k * per, step = blocks * 256;
-    for (int64_t i0 = block * 256 + threadIdx.x; i0 < total; i0 += UN * step) {
-        int64_t c[UN], col[UN];
-        int a[UN], b[UN];
+    const int64_t total = (int64_t)A.k * A.slices, step = blocks << (8 - A.lanes);
+    for (int64_t at = (block << (8 - A.lanes)) + (threadIdx.x >> A.lanes); at < total; at += UN * step) {
+        Unit u[UN];
+        bool none[UN];
 #pragma unroll
         for (int y = 0; y < UN; ++y) {
-            const int64_t i = i0 + y * step < total ? i0 + y * step : i0;
-            c[y] = i / per;
-            col[y] = (i - c[y] * per) * E;
-            a[y] = A.offsets[c[y]];
-            b[y] = A.offsets[c[y] + 1];
+            u[y] = unit_at<E>(A, at + y * step < total ? at + y * step : at);
+            none[y] = A.offsets[u[y].row] == A.offsets[u[y].row + 1];
         }
-        // The first slot of each is on its way before the others are.
-        int64_t row[UN];
-#pragma unroll
-        for (int y = 0; y < UN; ++y) row[y] = b[y] > a[y] && b[y] - a[y] <= kTableShort ? A.order[a[y]] : -1;
-        Part<T> v[UN];
+        const float zero[E] = {};
 #pragma unroll
         for (int y = 0; y < UN; ++y)
-            if (row[y] >= 0) v[y] = part_get(static_cast<const T*>(A.dY) + row[y] * A.ld, col[y], A.d);
-#pragma unroll
-        for (int y = 0; y < UN; ++y) {
-            if (i0 + y * step >= total) break;
-            const int count = b[y] - a[y];
-            if (count > kTableShort) continue;
-            float sum[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] = count > 0 ? to_f32(v[y].e[e]) : 0.0f;
-            for (int p = a[y] + 1; p < b[y]; p += UN) {
-                Part<T> w[UN];
-#pragma unroll
-                for (int q = 0; q < UN; ++q)
-                    w[q] = part_get(static_cast<const T*>(A.dY) + (int64_t)A.order[p + q < b[y] ? p + q : p] * A.ld, col[y],
-                                    A.d);
-#pragma unroll
-                for (int q = 0; q < UN; ++q)
-                    if (p + q < b[y])
-#pragma unroll
-                        for (int e = 0; e < E; ++e) sum[e] += to_f32(w[q].e[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] *= A.scale;
-            part_put(static_cast<T*>(A.out) + c[y] * A.d, col[y], A.d, sum);
-        }
+            if (none[y] && u[y].col < A.d) part_put<true>(static_cast<T*>(A.out) + u[y].row * A.d, u[y].col, A.d, zero);
     }
 }
 
-// Ids of more slots, by chunks of A.chunk places: 2^A.lanes lanes share a row's
-// slice, the other lanes of a block take other rows.
+// Unit `at`: a chunk's slice.
 template <class T>
-__device__ __forceinline__ void long_ids(const TableArgs& A, int64_t block, float (*s_sum)[16 / sizeof(T) + 1],
-                                         int* s_runs) {
-    constexpr int E = 16 / (int)sizeof(T), UN = 8;
-    const int lanes = 1 << A.lanes, groups = 256 >> A.lanes, slices = A.slices;
-    const int64_t b = block / slices;
-    const int slice = (int)(block - b * slices), l = threadIdx.x & (lanes - 1), group = threadIdx.x >> A.lanes;
-    const int64_t col = ((int64_t)slice * lanes + l) * E, used = A.offsets[A.k];
-    const int64_t p0 = b * A.chunk, p1 = p0 + A.chunk < used ? p0 + A.chunk : used;
-    // Where the ids of many slots begin in this chunk.
-    if (threadIdx.x == 0) s_runs[0] = 0;
-    __syncthreads();
-    for (int64_t p = p0 + threadIdx.x; p < p1; p += 256) {
-        const int c = A.sids[p];
-        if (p > p0 && A.sids[p - 1] == c) continue;
-        if (A.offsets[c + 1] - A.offsets[c] > kTableShort) s_runs[1 + atomicAdd(s_runs, 1)] = (int)(p - p0);
-    }
-    __syncthreads();
-    const int runs = s_runs[0];
-    for (int r = 0; r < runs; ++r) {   // in whatever order: each has a sum of its own
-        const int64_t p = p0 + s_runs[1 + r];
-        const int c = A.sids[p], first = A.offsets[c], last = A.offsets[c + 1];
-        const int64_t end = last < p1 ? last : p1;
-        float sum[E] = {};
-        if (col < A.d) {
-            for (int64_t q0 = p + group; q0 < end; q0 += UN * groups) {
-                int64_t row[UN];
+__device__ __forceinline__ void chunk_sums(const TableArgs& A, int64_t at) {
+    constexpr int E = 16 / (int)sizeof(T), UN = 4;
+    const int64_t used = A.offsets[A.k];
+    const Unit u = unit_at<E>(A, at);
+    const int64_t p0 = u.row * kTableChunk;
+    if (p0 >= used || u.col >= A.d) return;
+    const int64_t p1 = p0 + kTableChunk < used ? p0 + kTableChunk : used;
+    const int before = p0 > 0 ? A.sids[p0 - 1] : -1, behind = p1 < used ? A.sids[p1] : -1;
+    int32_t id[UN], row[UN];
+    auto ask = [&](int64_t p) {
 #pragma unroll
-                for (int y = 0; y < UN; ++y) row[y] = A.order[q0 + y * groups < end ? q0 + y * groups : q0];
-                Part<T> w[UN];
+        for (int q = 0; q < UN; ++q) {
+            const int64_t x = p + q < p1 ? p + q : p1 - 1;
+            id[q] = A.sids[x];
+            row[q] = A.order[x];
+        }
+    };
+    int c = before;         // the id that is summed
+    bool began = false;     // in this chunk
+    float sum[E] = {};
+    auto done = [&](bool ended) {
+        if (began && ended) {
+            float o[E];
 #pragma unroll
-                for (int y = 0; y < UN; ++y) w[y] = part_get(static_cast<const T*>(A.dY) + row[y] * A.ld, col, A.d);
+            for (int e = 0; e < E; ++e) o[e] = sum[e] * A.scale;
+            part_put<true>(static_cast<T*>(A.out) + (int64_t)c * A.d, u.col, A.d, o);
+        } else {
+            part_put<false>(A.part + (2 * u.row + began) * A.d, u.col, A.d, sum);
+        }
+    };
+    ask(p0);
+    bool some = false;   // places of c in this chunk
+    for (int64_t p = p0; p < p1; p += UN) {
+        u32x4 w[UN];
+        int32_t is[UN];
 #pragma unroll
-                for (int y = 0; y < UN; ++y)
-                    if (q0 + y * groups < end)
+        for (int q = 0; q < UN; ++q) {
+            w[q] = chunk_any(static_cast<const T*>(A.dY) + (int64_t)row[q] * A.ld, u.col, A.d);
+            is[q] = id[q];
+        }
+        if (p + UN < p1) ask(p + UN);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) sum[e] += to_f32(w[y].e[e]);
+        for (int q = 0; q < UN; ++q) {
+            if (p + q >= p1) break;
+            if (is[q] != c) {
+                if (some) done(true);
+                c = is[q];
+                began = true;
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] = 0.0f;
             }
+            some = true;
+            const Part<T> x = __builtin_bit_cast(Part<T>, w[q]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += to_f32(x.e[e]);
         }
-        // The groups' sums, halves added in turn.
-#pragma unroll
-        for (int e = 0; e < E; ++e) s_sum[threadIdx.x][e] = sum[e];
-        __syncthreads();
-        for (int h = groups / 2; h > 0; h /= 2) {
-            if (group < h)
-#pragma unroll
-                for (int e = 0; e < E; ++e) s_sum[threadIdx.x][e] += s_sum[threadIdx.x + h * lanes][e];
-            __syncthreads();
-        }
-        if (group == 0 && col < A.d) {
-            if (first >= p0 && last <= p1) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] = s_sum[threadIdx.x][e] * A.scale;
-                part_put(static_cast<T*>(A.out) + (int64_t)c * A.d, col, A.d, sum);
-            } else {
-                float* part = A.part + (2 * b + (first >= p0)) * A.d;
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col + e < A.d) part[col + e] = s_sum[threadIdx.x][e];
-            }
-        }
-        __syncthreads();
     }
+    done(behind != c);
 }
 
 template <class T>
 __global__ __launch_bounds__(256) void k_table_bwd(TableArgs A) {
-    __shared__ float s_sum[256][16 / sizeof(T) + 1];
-    __shared__ int s_runs[1 + kTableChunk / kTableShort + 2];   // runs of a chunk: all but the ends' are whole
-    if (blockIdx.x < A.long_blocks) long_ids<T>(A, blockIdx.x, s_sum, s_runs);
-    else short_ids<T>(A, blockIdx.x - A.long_blocks, gridDim.x - A.long_blocks);
+    if (blockIdx.x < A.chunk_blocks)
+        chunk_sums<T>(A, ((int64_t)blockIdx.x << (8 - A.lanes)) + (threadIdx.x >> A.lanes));
+    else
+        no_slots<T>(A, blockIdx.x - A.chunk_blocks, gridDim.x - A.chunk_blocks);
 }
 
-// An id that begins in chunk blockIdx.x and goes on behind it: the sum of its
-// parts in order, 16 lanes a column each taking every 16th.
-template <class T>
+// Ids whose places lie in several chunks: the sum of their parts in order, L lanes a
+// column each taking every L-th.  A block tests A.tests ids, or chunks that an id
+// begins in and goes on behind (by_chunk), a thread each, and adds those it finds.
+template <class T, int L>
 __global__ __launch_bounds__(256) void k_table_join(TableArgs A) {
-    __shared__ float s_sum[16][17];
-    const int64_t b = blockIdx.x, p0 = b * A.chunk, p1 = p0 + A.chunk;
-    const int64_t used = A.offsets[A.k];
-    if (p1 >= used) return;
-    const int c = A.sids[p1 - 1], first = A.offsets[c], last = A.offsets[c + 1];
-    if (first < p0 || last <= p1 || last - first <= kTableShort) return;
-    const int64_t behind = (last - 1) / A.chunk - b;   // chunks after this one
-    const int l = threadIdx.x & 15, y = threadIdx.x >> 4;
-    for (int64_t col0 = (int64_t)blockIdx.y * 16; col0 < A.d; col0 += (int64_t)gridDim.y * 16) {
-        const int64_t col = col0 + l < A.d ? col0 + l : A.d - 1;
-        float sum = y == 0 ? A.part[(2 * b + 1) * A.d + col] : 0.0f;
-#pragma unroll 8
-        for (int64_t q = 1 + y; q <= behind; q += 16) sum += A.part[2 * (b + q) * A.d + col];
-        s_sum[y][l] = sum;
-        __syncthreads();
-        if (y == 0 && col0 + l < A.d) {
-            float all = 0.0f;
-#pragma unroll
-            for (int q = 0; q < 16; ++q) all += s_sum[q][l];
-            static_cast<T*>(A.out)[(int64_t)c * A.d + col] = from_f32<T>(all * A.scale);
+    constexpr int kCols = 256 / L;
+    __shared__ float s_sum[L][kCols + 1];
+    __shared__ int s_found[257];
+    if (threadIdx.x == 0) s_found[0] = 0;
+    __syncthreads();
+    const int64_t i = (int64_t)blockIdx.x * A.tests + threadIdx.x;
+    if ((int)threadIdx.x < A.tests) {
+        int c = -1;
+        if (!A.by_chunk) {
+            if (i < A.k) c = (int)i;
+        } else {
+            const int64_t p1 = (i + 1) * kTableChunk;
+            if (p1 < A.offsets[A.k]) {
+                c = A.sids[p1];
+                if (A.sids[p1 - 1] != c || A.offsets[c] / kTableChunk != i) c = -1;
+            }
         }
-        __syncthreads();
+        if (c >= 0) {
+            const int first = A.offsets[c], last = A.offsets[c + 1];
+            if (last > first && first / kTableChunk != (last - 1) / kTableChunk) s_found[1 + atomicAdd(s_found, 1)] = c;
+        }
+    }
+    __syncthreads();
+    // This block's columns.
+    const int width = (int)((A.d + gridDim.y - 1) / gridDim.y), lo = (int)blockIdx.y * width;
+    const int hi = lo + width < A.d ? lo + width : A.d;
+    const int found = s_found[0], cols = hi > lo ? hi - lo : 0;
+    // The ids of few parts: a lane a column of one.  In whatever order: each has a sum of
+    // its own.
+    constexpr int kFewParts = 8;
+    for (int x = threadIdx.x; x < found * cols; x += 256) {
+        const int c = s_found[1 + x / cols], col = lo + x % cols, first = A.offsets[c], last = A.offsets[c + 1];
+        const int64_t b = first / kTableChunk;
+        const int more = (int)((last - 1) / kTableChunk - b);   // chunks after the first
+        if (more > kFewParts) continue;
+        float sum = A.part[(2 * b + 1) * A.d + col];
+        for (int q = 1; q <= more; ++q) sum += A.part[2 * (b + q) * A.d + col];
+        static_cast<T*>(A.out)[(int64_t)c * A.d + col] = from_f32<T>(sum * A.scale);
+    }
+    const int l = threadIdx.x % kCols, y = threadIdx.x / kCols;
+    for (int f = 0; f < found; ++f) {
+        const int c = s_found[1 + f], first = A.offsets[c], last = A.offsets[c + 1];
+        const int64_t b = first / kTableChunk, more = (last - 1) / kTableChunk - b;
+        if (more <= kFewParts) continue;
+        for (int col0 = lo; col0 < hi; col0 += kCols) {
+            const int col = col0 + l < hi ? col0 + l : hi - 1;
+            float sum = y == 0 ? A.part[(2 * b + 1) * A.d + col] : 0.0f;
+#pragma unroll 8
+            for (int64_t q = 1 + y; q <= more; q += L) sum += A.part[2 * (b + q) * A.d + col];
+            s_sum[y][l] = sum;
+            __syncthreads();
+            if (y == 0 && col0 + l < hi) {
+                float all = 0.0f;
+#pragma unroll
+                for (int q = 0; q < L; ++q) all += s_sum[q][l];
+                static_cast<T*>(A.out)[(int64_t)c * A.d + col] = from_f32<T>(all * A.scale);
+            }
+            __syncthreads();
+        }
     }
 }
 
-unsigned some_blocks(int64_t lanes, int64_t most) {
-    const int64_t b = (lanes + 255) / 256;
-    return (unsigned)(b < 1 ? 1 : b < most ? b : most);
+// Blocks whose lanes take `units` units, four each, or as many as are of use.
+unsigned some_blocks(int64_t units, int lanes) {
+    const int64_t b = ((units << lanes) + 1023) / 1024;
+    return (unsigned)(b < 1 ? 1 : b < 16384 ? b : 16384);
 }
 
 template <class T>
-hipError_t forward_t(const TableArgs& A, hipStream_t s) {
-    constexpr int E = 16 / (int)sizeof(T);
-    const int64_t chunks = A.n * ((A.d + E - 1) / E);
-    hipLaunchKernelGGL((k_table_fwd<T>), dim3(some_blocks((chunks + 3) / 4, 16384)), dim3(256), 0, s, A);
+hipError_t forward_t(TableArgs A, const TableShape& L, hipStream_t s) {
+    A.lanes = L.lanes;
+    A.slices = L.slices;
+    // Few rows: a unit a lane, all at once.
+    const int64_t units = A.n * A.slices, few = (units << A.lanes) <= 256 * 1024 ? 4 : 1;
+    const dim3 g(some_blocks(units * few, A.lanes)), b(256);
+    if (A.n * A.d * (int64_t)sizeof(T) > kStreamBytes) hipLaunchKernelGGL((k_table_fwd<T, true>), g, b, 0, s, A);
+    else hipLaunchKernelGGL((k_table_fwd<T, false>), g, b, 0, s, A);
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t backward_t(TableArgs A, const TableShape& L, hipStream_t s) {
-    constexpr int E = 16 / (int)sizeof(T);
-    A.chunk = L.chunk;
     A.lanes = L.lanes;
     A.slices = L.slices;
-    A.long_blocks = (uint32_t)(L.chunks * L.slices);
-    const int64_t parts = (int64_t)A.k * ((A.d + E - 1) / E);
-    hipLaunchKernelGGL((k_table_bwd<T>), dim3(A.long_blocks + some_blocks((parts + 3) / 4, 16384)), dim3(256), 0, s, A);
+    const int64_t rows = 256 >> L.lanes;   // of a block
+    A.chunk_blocks = (uint32_t)((L.chunks * L.slices + rows - 1) / rows);
+    hipLaunchKernelGGL((k_table_bwd<T>), dim3(A.chunk_blocks + some_blocks((int64_t)A.k * L.slices, L.lanes)), dim3(256),
+                       0, s, A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || L.chunks < 2) return e;
-    const int64_t gy = (A.d + 15) / 16;
-    hipLaunchKernelGGL((k_table_join<T>), dim3((unsigned)L.chunks, (unsigned)(gy < 64 ? gy : 64)), dim3(256), 0, s, A);
+    // The fewer of ids and chunks, up to 256 tests a block while there are 1024 blocks.
+    A.by_chunk = L.chunks < A.k;
+    const int64_t all = A.by_chunk ? L.chunks : A.k, tests = all / 1024;
+    A.tests = (int32_t)(tests < 1 ? 1 : tests < 256 ? tests : 256);
+    const unsigned gx = (unsigned)((all + A.tests - 1) / A.tests);
+    if (A.d < 256) {
+        hipLaunchKernelGGL((k_table_join<T, 32>), dim3(gx, (unsigned)((A.d + 7) / 8)), dim3(256), 0, s, A);
+    } else {
+        const int64_t gy = (A.d + 63) / 64;
+        hipLaunchKernelGGL((k_table_join<T, 4>), dim3(gx, (unsigned)(gy < 64 ? gy : 64)), dim3(256), 0, s, A);
+    }
     return hipGetLastError();
 }
 
@@ -271,10 +298,7 @@ TableShape table_shape(int64_t n, int32_t d, int type) {
     const int64_t per = ((int64_t)d + e - 1) / e;
     while (L.lanes < 8 && (1 << L.lanes) < per) ++L.lanes;
     L.slices = (int32_t)((per + 255) / 256);
-    // Four rounds of a block's rows in flight.
-    const int rows = 4 * 8 * (256 >> L.lanes);
-    L.chunk = rows < 64 ? 64 : rows > kTableChunk ? kTableChunk : rows;
-    L.chunks = (n + L.chunk - 1) / L.chunk;
+    L.chunks = (n + kTableChunk - 1) / kTableChunk;
     L.bytes = ((size_t)L.chunks * 2 * d * 4 + 255) / 256 * 256;
     if (L.bytes == 0) L.bytes = 256;
     return L;
@@ -282,9 +306,10 @@ TableShape table_shape(int64_t n, int32_t d, int type) {
 
 hipError_t launch_table_fwd(const TableArgs& A, int type, hipStream_t s) {
     if (A.n == 0) return hipSuccess;
-    if (type == kF32) return forward_t<float>(A, s);
-    if (type == kBF16) return forward_t<__bf16>(A, s);
-    return forward_t<_Float16>(A, s);
+    const TableShape L = table_shape(A.n, A.d, type);
+    if (type == kF32) return forward_t<float>(A, L, s);
+    if (type == kBF16) return forward_t<__bf16>(A, L, s);
+    return forward_t<_Float16>(A, L, s);
 }
 
 hipError_t launch_table_bwd(const TableArgs& A, const TableShape& L, int type, hipStream_t s) {

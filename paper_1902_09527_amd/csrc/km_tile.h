@@ -85,6 +85,24 @@ __device__ __forceinline__ u32x4 chunk(const T* row, int64_t k0, int64_t K, bool
     return aligned ? chunk_aligned(row, k0, K) : chunk_guarded(row, k0, K);   // `aligned` is uniform
 }
 
+// 16 bytes of a row from element k0 on, zero past its K elements, at any address.
+// One value of four words: as elements, the compiler would load both branches' so.
+template <class T>
+__device__ __forceinline__ u32x4 chunk_any(const T* row, int64_t k0, int64_t K) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if (k0 + E <= K) {
+        u32x4 v;
+        __builtin_memcpy(&v, row + k0, 16);
+        return v;
+    }
+    Vec<T, E> v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v.e[e] = row[k0 + e < K ? k0 + e : 0];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v.e[e] = k0 + e < K ? v.e[e] : (T)0.0f;
+    return __builtin_bit_cast(u32x4, v);
+}
+
 // Four consecutive results, col0 .. of a row of P.
 template <class T>
 __device__ __forceinline__ void store4(T* row, int64_t col0, int64_t P, f32x4 v, bool aligned) {
