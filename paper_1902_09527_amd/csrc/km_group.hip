@@ -438,7 +438,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
             }
             bn_load = q.bn;
             lk = q.k0;
-            whole = !TR || q.bn + TN <= A.P ? A.K / BK : 0;
+            whole = !TR || A.P >= TN ? A.K / BK : 0;
         };
         // Chunk i (of NU + NW a thread) of the next stage to LDS; guard: it may lie past an end.
         auto load = [&](int i, char* buf, bool guard) {
@@ -688,39 +688,66 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
     const int tiles = items * A.tn * A.splits, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if ((int)(blockIdx.x / 8) < per && t < tiles) {
-        const Tile q = tile_at<TN>(A, items, t);
+        Tile q = tile_at<TN>(A, items, t);
+        // The last tile of a width that TN does not divide moves left until it is whole:
+        // it and its neighbour then write the same values.
+        if (TR && A.P >= TN && q.bn > A.P - TN) q.bn = A.P - TN;
         const int all = (A.K + BK - 1) / BK, end = q.k0 + A.share < all ? q.k0 + A.share : all;
         const int live = (q.rows + kTurn - 1) / kTurn;
         const int64_t ldw = TR ? A.P : A.K;
         const T* const W = static_cast<const T*>(A.W) + (int64_t)q.c * A.K * A.P;
-        const T* up[NU];
-        const T* wp[NW];
+        for (int r = tid; r < TM; r += NT) s_rows[r] = (int32_t)row_of(A.order, q.p0 + (r < q.rows ? r : q.rows - 1));
+        __syncthreads();
         const int uc = swz(tid / 8, tid % 8) * E;
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int r = (i * NT + tid) / 8;
-            const int64_t row = row_of(A.order, q.p0 + (r < q.rows ? r : q.rows - 1));
-            up[i] = static_cast<const T*>(A.U) + row * A.ldu;
-            if (tid % 8 == 0) s_rows[r] = (int32_t)row;
-        }
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
+        // Where chunk i of a stage (NU + NW a thread) begins: its row, at stage 0.
+        auto from = [&](int i) -> const T* {
             const int x = i * NT + tid;
-            if constexpr (TR) wp[i] = W + (int64_t)(x / CPR) * ldw;
-            else wp[i] = W + (q.bn + x / 8 < A.P ? q.bn + x / 8 : A.P - 1) * ldw;
-        }
-        auto fetch = [&](int i, int kt) -> u32x4 {
-            if (i < NU) return chunk_any(up[i], (int64_t)kt * BK + uc, A.K);
-            i -= NU;
-            if constexpr (TR) {
-                const int x = i * NT + tid, kk = x / CPR;
-                const bool in = kt * BK + kk < A.K;
-                return only_if(in, chunk_any(in ? wp[i] + (int64_t)kt * BK * ldw : W,
-                                             q.bn + swz_tr<T, CPR>(kk, x % CPR) * E, A.P));
+            if (i < NU) return static_cast<const T*>(A.U) + (int64_t)s_rows[x / 8] * A.ldu;
+            const int y = x - NU * NT;
+            if constexpr (TR) return W + (int64_t)(y / CPR) * ldw;
+            return W + (q.bn + y / 8 < A.P ? q.bn + y / 8 : A.P - 1) * ldw;
+        };
+        const T* p[NU + NW];
+#pragma unroll
+        for (int i = 0; i < NU + NW; ++i) {
+            p[i] = from(i);
+            if (TR && i >= NU) {
+                const int y = (i - NU) * NT + tid;
+                p[i] += (int64_t)q.k0 * BK * ldw + q.bn + swz_tr<T, CPR>(y / CPR, y % CPR) * E;
             } else {
-                return chunk_any(wp[i], (int64_t)kt * BK + uc, A.K);
+                p[i] += (int64_t)q.k0 * BK + uc;
+            }
+        }
+        // Stages without a chunk past the contraction's end or the last column.
+        const int whole = !TR || A.P >= TN ? A.K / BK : 0;
+        typedef u32x4 __attribute__((aligned(1))) any4;
+        u32x4 v[NU + NW];
+        bool held = false;   // the stage is in v, else in its buffer already
+        auto fetch = [&](int kt, char* buf) {
+            held = kt < whole;
+            if (held) {
+#pragma unroll
+                for (int i = 0; i < NU + NW; ++i) {
+                    v[i] = *reinterpret_cast<const any4*>(p[i]);
+                    p[i] += TR && i >= NU ? (int64_t)BK * ldw : BK;
+                }
+                return;
+            }
+#pragma unroll 1
+            for (int i = 0; i < NU + NW; ++i) {
+                u32x4 o;
+                if (!TR || i < NU) {
+                    o = chunk_any(from(i), (int64_t)kt * BK + uc, A.K);
+                } else {
+                    const int y = (i - NU) * NT + tid, kk = y / CPR;
+                    const bool in = kt * BK + kk < A.K;
+                    o = only_if(in, chunk_any(in ? from(i) + (int64_t)kt * BK * ldw : W,
+                                              q.bn + swz_tr<T, CPR>(kk, y % CPR) * E, A.P));
+                }
+                *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) = o;
             }
         };
+
         // 8 bits: the scales of the stages from k0 on, a row a thread.
         auto scales = [&](int k0) {
             if constexpr (F8) {
@@ -753,19 +780,17 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
         } else {
             wa[0] = TM * 128 + (wc * (TN / WC) + li) * 128 + swz(li, P::chunk(lane)) * 16;
         }
-        u32x4 v[NU + NW];
         scales(q.k0);
+        int at = 0;
+        fetch(q.k0, s_tiles);
+        for (int kt = q.k0; kt < end; ++kt, at ^= 1) {
+            char* buf = s_tiles + at * kStage;
+            if (held) {
 #pragma unroll
-        for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, q.k0);
-        for (int kt = q.k0; kt < end; ++kt) {
-            char* buf = s_tiles + (kt & 1) * kStage;
-#pragma unroll
-            for (int i = 0; i < NU + NW; ++i) *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) = v[i];
-            __syncthreads();
-            if (kt + 1 < end) {
-#pragma unroll
-                for (int i = 0; i < NU + NW; ++i) v[i] = fetch(i, kt + 1);
+                for (int i = 0; i < NU + NW; ++i) *reinterpret_cast<u32x4*>(buf + (i * NT + tid) * 16) = v[i];
             }
+            __syncthreads();
+            if (kt + 1 < end) fetch(kt + 1, s_tiles + (at ^ 1) * kStage);
             int sa[F8 ? FC : 1], sb[F8 ? FR : 1];
             if constexpr (F8) {
 #pragma unroll
@@ -1046,23 +1071,43 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp, t = grad_index(blockIdx.x / 8);
     if (t >= tiles) return;
-    const GradTile q = grad_tile_at<TM, TN>(A, t);
-    int64_t row[N];   // of the next stage to load
+    GradTile q = grad_tile_at<TM, TN>(A, t);
+    // The last tile of a width that TM does not divide moves left until it is whole: it and
+    // its neighbour then write the same values.
+    const bool wide = A.Q >= TM && A.P >= TN;
+    if (wide) {
+        q.bm = q.bm < A.Q - TM ? q.bm : A.Q - TM;
+        q.bn = q.bn < A.P - TN ? q.bn : A.P - TN;
+    }
+    int32_t row[N];   // of the next stage to load; behind the last, the first once more
     auto rows = [&](int p) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int x = p + (i * NT + tid) / CPR;
-            row[i] = row_of(A.order, x < q.p1 ? x : q.p0);
+            row[i] = (int32_t)row_of(A.order, x < q.p1 ? x : q.p0);
         }
     };
-    u32x4 held[2 * N];
-    auto load = [&](int p) {
+    typedef u32x4 __attribute__((aligned(1))) any4;
+    u32x4 v[2 * N];   // wide: the stage on its way, else it goes to its buffer at once
+    auto load = [&](int p, char* buf) {
+        if (wide) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int x = i * NT + tid, k = x / CPR, c = swz_tr<T, CPR>(k, x % CPR) * E;
+            for (int i = 0; i < N; ++i) {
+                const int x = i * NT + tid, c = swz_tr<T, CPR>(x / CPR, x % CPR) * E;
+                v[i] = *reinterpret_cast<const any4*>(static_cast<const T*>(A.V) + row[i] * A.ldv + (q.bm + c));
+                v[N + i] = *reinterpret_cast<const any4*>(static_cast<const T*>(A.U) + row[i] * A.ldu + (q.bn + c));
+            }
+            return;
+        }
+#pragma unroll 1
+        for (int i = 0; i < 2 * N; ++i) {
+            const bool first = i < N;
+            const int x = (first ? i : i - N) * NT + tid, k = x / CPR, c = swz_tr<T, CPR>(k, x % CPR) * E;
             const bool in = p + k < q.p1;
-            held[i] = only_if(in, chunk_any(static_cast<const T*>(A.V) + row[i] * A.ldv, q.bm + c, A.Q));
-            held[N + i] = only_if(in, chunk_any(static_cast<const T*>(A.U) + row[i] * A.ldu, q.bn + c, A.P));
+            const int64_t r = row_of(A.order, in ? p + k : q.p0);
+            const u32x4 o = first ? chunk_any(static_cast<const T*>(A.V) + r * A.ldv, q.bm + c, A.Q)
+                                  : chunk_any(static_cast<const T*>(A.U) + r * A.ldu, q.bn + c, A.P);
+            *reinterpret_cast<u32x4*>(buf + (first ? 0 : TM * 128) + x * 16) = only_if(in, o);
         }
     };
     int va[FR], ua[FC];
@@ -1076,17 +1121,21 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
 #pragma unroll
         for (int h = 0; h < FC; ++h) acc[f][h] = f32x4{0, 0, 0, 0};
     rows(q.p0);
-    load(q.p0);
+    load(q.p0, s_tiles);
     rows(q.p0 + BK);
     int at = 0;
     for (int p = q.p0; p < q.p1; p += BK, at ^= 1) {
         char* buf = s_tiles + at * kStage;
+        if (wide) {
 #pragma unroll
-        for (int i = 0; i < 2 * N; ++i)
-            *reinterpret_cast<u32x4*>(buf + (i < N ? 0 : TM * 128) + ((i % N) * NT + tid) * 16) = held[i];
+            for (int i = 0; i < 2 * N; ++i) {
+                const int x = i % N * NT + tid;
+                *reinterpret_cast<u32x4*>(buf + (i < N ? 0 : TM * 128) + x * 16) = only_if(p + x / CPR < q.p1, v[i]);
+            }
+        }
         __syncthreads();
         if (p + BK < q.p1) {
-            load(p + BK);
+            load(p + BK, s_tiles + (at ^ 1) * kStage);
             rows(p + 2 * BK);
         }
         auto half = [&](auto s) {
@@ -1158,11 +1207,12 @@ struct FewArgs {
     const uint8_t *UE, *WE;
     const int32_t *order, *sids, *offsets;
     void* Y;
-    int32_t n, k, K, P, nb, y4;
+    int32_t n, k, K, P, nb;
 };
 
 // 16 columns and the places of one cluster a block, from the place blockIdx.y on
-// if a cluster starts there; its 16 waves share the contraction.
+// if a cluster starts there; its NWAVE waves share the contraction, some four steps
+// each.
 template <class T, class O>
 struct FewOp {
     static constexpr int kBytes = 16;   // of a row a lane and step
@@ -1189,12 +1239,12 @@ struct FewOp<uint8_t, float> {
     }
 };
 
-template <class T, class O, bool AL, int RF>
+template <class T, class O, bool AL, int NWAVE, int RF>
 __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int rows, f32x4 (*s_red)[4][64]) {
     using P = FewOp<T, O>;
     constexpr bool F8 = sizeof(T) == 1;
-    constexpr int EL = P::kBytes / (int)sizeof(T), KS = 4 * EL, NWAVE = 16;   // elements a lane, of a step
-    constexpr int UN = !AL ? 1 : RF <= 2 ? 4 : 2;
+    constexpr int EL = P::kBytes / (int)sizeof(T), KS = 4 * EL;   // elements a lane, of a step
+    constexpr int UN = (RF <= 2 ? 4 : 2) / (F8 && RF == 4 ? 2 : AL ? 1 : 2);
     const int lane = threadIdx.x & 63, g = lane >> 4, li = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t col0 = (int64_t)blockIdx.x * 16;
@@ -1259,32 +1309,32 @@ __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int r
 #pragma unroll
         for (int q = 0; q < RF; ++q) s_red[wave][q][lane] += acc[q];
     __syncthreads();
-    if (wave < RF) {
-        const int r = wave * 16 + li;
-        if (r >= rows) return;
+    for (int q = wave; q < RF; q += NWAVE) {
+        const int r = q * 16 + li;
+        if (r >= rows) continue;
         f32x4 v{0, 0, 0, 0};
 #pragma unroll
-        for (int y = 0; y < H; ++y) v += s_red[y][wave][lane];
-        store4(static_cast<O*>(A.Y) + row_of(A.order, p0 + r) * A.P, col0 + g * 4, A.P, v, A.y4);
+        for (int y = 0; y < H; ++y) v += s_red[y][q][lane];
+        put4(static_cast<O*>(A.Y) + row_of(A.order, p0 + r) * A.P, col0 + g * 4, A.P, v);
     }
 }
 
-template <class T, class O, bool AL>
-__global__ __launch_bounds__(1024) void k_gr_few(FewArgs A) {
-    __shared__ f32x4 s_red[8][4][64];
+template <class T, class O, bool AL, int NWAVE>
+__global__ __launch_bounds__(64 * NWAVE, 4) void k_gr_few(FewArgs A) {
+    __shared__ f32x4 s_red[NWAVE / 2][4][64];
     const int p = blockIdx.y, c = __builtin_amdgcn_readfirstlane(A.sids[p]);
     if (p > 0 && A.sids[p - 1] == c) return;   // not the first place of its cluster
     if (c < 0) {                               // rows of no cluster
         const int64_t col0 = (int64_t)blockIdx.x * 16;
-        for (int q = threadIdx.x; q < (A.n - p) * 16; q += 1024)
+        for (int q = threadIdx.x; q < (A.n - p) * 16; q += 64 * NWAVE)
             if (col0 + q % 16 < A.P)
                 static_cast<O*>(A.Y)[row_of(A.order, p + q / 16) * A.P + col0 + q % 16] = from_f32<O>(0.0f);
         return;
     }
     const int rows = __builtin_amdgcn_readfirstlane(A.offsets[c + 1]) - p;
-    if (rows <= 16) few_block<T, O, AL, 1>(A, c, p, rows, s_red);
-    else if (rows <= 32) few_block<T, O, AL, 2>(A, c, p, rows, s_red);
-    else few_block<T, O, AL, 4>(A, c, p, rows, s_red);
+    if (rows <= 16) few_block<T, O, AL, NWAVE, 1>(A, c, p, rows, s_red);
+    else if (rows <= 32) few_block<T, O, AL, NWAVE, 2>(A, c, p, rows, s_red);
+    else few_block<T, O, AL, NWAVE, 4>(A, c, p, rows, s_red);
 }
 
 // --------------------------------------------------------------------------
@@ -1356,7 +1406,7 @@ struct MainPlan {
 };
 MainPlan main_plan(const GroupArgs& D, const GroupShape& L, bool al) {
     MainPlan M{L.rows, al ? L.splits : L.any_splits};
-    if (!al) M.list.size = 128;
+    if (!al) M.list.size = L.any_tile;
     M.list.max_items = group_items(D.n, D.k, M.list.size);
     return M;
 }
@@ -1369,9 +1419,11 @@ hipError_t main_go(MainArgs A, const MainPlan& M, bool al, hipStream_t s) {
     A.share = part_stages(all, M.splits, sizeof(T) == 1);
     hipError_t e;
     if constexpr (kWide<T, O>) {
-        e = any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+        e = M.list.size == 128 ? any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s)
+                               : any_tile<T, O, 64, 64, 2, 2, TR>(A, items, s);
     } else {
-        if (!al) e = any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+        if (!al && M.list.size == 128) e = any_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
+        else if (!al) e = any_tile<T, O, 64, 64, 2, 2, TR>(A, items, s);
         else if (M.list.size == 256) e = main_tile<T, O, 256, 256, 2, 4, TR>(A, items, s);
         else if (M.list.size == 128) e = main_tile<T, O, 128, 128, 2, 2, TR>(A, items, s);
         else e = main_tile<T, O, 64, 64, 2, 2, TR>(A, items, s);
@@ -1427,10 +1479,16 @@ hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStrea
         F.K = D.di;
         F.P = D.dout;
         F.nb = (D.di + 127) / 128;
-        F.y4 = D.dout % 4 == 0 && a16(D.Y);
-        const dim3 g((unsigned)((D.dout + 15) / 16), (unsigned)D.n), b(1024);
-        if (al) hipLaunchKernelGGL((k_gr_few<T, O, true>), g, b, 0, s, F);
-        else hipLaunchKernelGGL((k_gr_few<T, O, false>), g, b, 0, s, F);
+        const dim3 g((unsigned)((D.dout + 15) / 16), (unsigned)D.n);
+        const int steps = (int)(((int64_t)D.di * sizeof(T) + 4 * FewOp<T, O>::kBytes - 1) / (4 * FewOp<T, O>::kBytes));
+        auto go = [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            if (al) hipLaunchKernelGGL((k_gr_few<T, O, true, W>), g, dim3(64 * W), 0, s, F);
+            else hipLaunchKernelGGL((k_gr_few<T, O, false, W>), g, dim3(64 * W), 0, s, F);
+        };
+        if (steps <= 16) go(std::integral_constant<int, 4>{});
+        else if (steps <= 64) go(std::integral_constant<int, 8>{});
+        else go(std::integral_constant<int, sizeof(T) == 1 ? 8 : 16>{});   // 8 bits: registers
         return hipGetLastError();
     }
     const bool al = !kWide<T, O> && main_ok<T>(D.X, D.ldx, D.n, D.di, D.W, D.di, D.order);
@@ -1565,11 +1623,12 @@ MainChoice main_choice(int64_t n, int64_t met, int32_t K, int32_t P, int type, b
     const Kind kinds[3] = {{256, 1, {1.65, 7.2, 1.75}, {1.05, 7.0, 1.1}, {3.5, 1.0, 5.5}},
                            {128, 2, {1.15, 3.3, 1.15}, {0.85, 1.7, 0.85}, {2.5, 1.0, 2.2}},
                            {64, 4, {0.96, 1.55, 0.85}, {0.6, 0.6, 0.5}, {2.0, 1.0, 2.0}}};
-    const Kind anywhere{128, 2, {2.4, 4.5, 2.4}, {1.7, 2.6, 1.7}, {3.0, 2.0, 3.0}};
+    const Kind anywhere[2] = {{128, 2, {2.4, 4.5, 2.4}, {1.7, 2.6, 1.7}, {3.0, 2.0, 3.0}},
+                              {64, 4, {1.6, 2.0, 1.6}, {1.1, 1.1, 1.1}, {2.0, 2.0, 2.0}}};
     MainChoice best{128, 1};
     double least = 0;
-    for (int q = 0; q < (main ? 3 : 1); ++q) {
-        const Kind& k = main ? kinds[q] : anywhere;
+    for (int q = 0; q < (main ? 3 : 2); ++q) {
+        const Kind& k = main ? kinds[q] : anywhere[q];
         // A cluster's last tile is half full, and none has less than one.
         double items = (double)n / k.tile + 0.5 * met;
         if (items < met) items = (double)met;
@@ -1611,6 +1670,7 @@ GroupShape group_shape(int64_t n, int32_t di, int32_t dout, int32_t k, int type,
         L.rows.size = main.tile;
         L.splits = main.splits;
         L.any_splits = any.splits;
+        L.any_tile = any.tile;
         const int most = L.splits > L.any_splits ? L.splits : L.any_splits;
         L.off_split = take(most > 1 ? (size_t)most * n * P * 4 : 0);
         L.rows.max_items = group_items(n, k, 64);   // 64: the least size of a tile

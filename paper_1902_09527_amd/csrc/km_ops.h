@@ -186,7 +186,7 @@ struct GroupList {
 };
 struct GroupShape {
     int32_t few, grad_tile;
-    int32_t splits, any_splits;   // parts of the contraction, and at any addresses
+    int32_t splits, any_splits, any_tile;   // parts of the contraction; those and the tile at any addresses
     GroupList rows, cuts;
     size_t off_split, off_part, bytes;
 };
