@@ -24,10 +24,10 @@
  * DEVICE pointers on the current device; a pointer may be NULL where its
  * array is empty.  Rows are `d` contiguous elements, `ld` elements apart
  * (ld >= d) where an argument ld* is given, else d apart.  Outputs must not
- * overlap inputs.  Rows have at most 2^28 elements.  Workspaces are the caller's: device memory of at least
- * the bytes that the *_workspace_bytes function gives, 256-byte aligned,
- * contents on entry of no matter, not to be used by another call until this
- * one's work completes.  Sums, statistics and gradients are formed in
+ * overlap inputs (kmeans_clip_norm may work in place).  Rows have at most 2^28
+ * elements.  Workspaces are the caller's: device memory of at least the bytes
+ * that the *_workspace_bytes function gives, 256-byte aligned, contents on entry
+ * of no matter, not to be used by another call until this one's work completes.  Sums, statistics and gradients are formed in
  * float32 and rounded once to the type of the output; equal inputs give
  * bitwise equal outputs.
  */
@@ -199,7 +199,8 @@ int kmeans_linear_backward(const void* dY, int64_t lddy, const void* X, int64_t 
  * number with a <= 448 2^e), exponents = e + 127 (n x ceil(d / 128) bytes),
  * values = x 2^-e rounded to the nearest e4m3 value, ties to even (n x d
  * bytes); infinities and NaN become NaN.  dequantize: X = values 2^e, rounded to
- * its type.  Requires 0 <= n <= 2^40, d >= 1.
+ * its type.  An exponent byte of 255, which quantize never writes, stands for NaN
+ * in all of its elements.  Requires 0 <= n <= 2^40, d >= 1.
  */
 int kmeans_fp8_quantize(const void* X, int64_t ldx, int64_t n, int32_t d, int32_t type, void* values,
                         uint8_t* exponents, void* hip_stream);

@@ -120,12 +120,13 @@ __global__ __launch_bounds__(256) void k_dequantize(QuantArgs A, T* out) {
         uint32_t w[kEach / 4];
         __builtin_memcpy(w, q, sizeof(w));
         T o[kEach];
+        auto stands = [&](float v) { return from_f32<T>(byte < 255 ? ldexpf(v, byte - 127) : NAN); };
 #pragma unroll
         for (int e = 0; e < kEach / 4; ++e) {
-            o[4 * e] = from_f32<T>(ldexpf(__builtin_amdgcn_cvt_f32_fp8(w[e], 0), byte - 127));
-            o[4 * e + 1] = from_f32<T>(ldexpf(__builtin_amdgcn_cvt_f32_fp8(w[e], 1), byte - 127));
-            o[4 * e + 2] = from_f32<T>(ldexpf(__builtin_amdgcn_cvt_f32_fp8(w[e], 2), byte - 127));
-            o[4 * e + 3] = from_f32<T>(ldexpf(__builtin_amdgcn_cvt_f32_fp8(w[e], 3), byte - 127));
+            o[4 * e] = stands(__builtin_amdgcn_cvt_f32_fp8(w[e], 0));
+            o[4 * e + 1] = stands(__builtin_amdgcn_cvt_f32_fp8(w[e], 1));
+            o[4 * e + 2] = stands(__builtin_amdgcn_cvt_f32_fp8(w[e], 2));
+            o[4 * e + 3] = stands(__builtin_amdgcn_cvt_f32_fp8(w[e], 3));
         }
         row_put(out + row * A.d, c, A.d, o);
     }

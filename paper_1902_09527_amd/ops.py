@@ -475,7 +475,8 @@ class BlockRows:
     """Rows in 8-bit floating point (made by :func:`quantize_blocks`).
 
     ``values`` (float8_e4m3fn [..., d]) and ``exponents`` (uint8 [...,
-    ceil(d / 128)]): 128 elements stand for values * 2^(exponent - 127).
+    ceil(d / 128)]): 128 elements stand for values * 2^(exponent - 127), for
+    NaN where the exponent is 255 (which is never made).
     """
 
     __slots__ = ("values", "exponents")
@@ -653,8 +654,6 @@ def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[
           stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     given, sizes, dtypes = _tensors(tensors, "tensors")
     dev, count = given[0].device, len(given)
-    if torch.is_grad_enabled() and any(map(_grad, given)):
-        _On(dev, stream, tuple(given))   # refuses
     pointers = array.array("Q", map(torch.Tensor.data_ptr, given))
     to = []
     targets = pointers if inplace else None
@@ -663,6 +662,8 @@ def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[
         if to_sizes != sizes or to_dtypes != dtypes or to[0].get_device() != given[0].get_device():
             raise ValueError("out must have the tensors' sizes, types and device")
         targets = array.array("Q", map(torch.Tensor.data_ptr, to))
+    if torch.is_grad_enabled() and (any(map(_grad, given)) or any(map(_grad, to))):
+        _On(dev, stream, tuple(given + to))   # refuses
     kinds = array.array("i", [_TYPES[dtypes[0]]]) * count if len(set(dtypes)) == 1 else \
         array.array("i", [_TYPES[t] for t in dtypes])
     lengths = array.array("q", sizes)
@@ -674,6 +675,8 @@ def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[
         st = lib.kmeans_clip_norm(at(pointers), at(targets), at(lengths), at(kinds), count, limit, _p(norm), _p(ws),
                                   ws.numel(), s)
     N.check(st, "kmeans_clip_norm")
+    if targets is not None:
+        torch.autograd.graph.increment_version(given if inplace else to)
     return norm
 
 
