@@ -37,7 +37,7 @@ from __future__ import annotations
 import array
 import math
 import operator
-from typing import List, Optional, Sequence, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -627,27 +627,29 @@ def cluster_embedding_backward(dY: torch.Tensor, plan: ClusterPlan, scale: float
     return out
 
 
-# A list of many small tensors costs the host more than the GPU: what is asked of
-# each is asked by map over the list.
+# A list of many small tensors costs the host more than the GPU (160 tensors: 100 us
+# a call): what is asked of each is asked by map over the list, and no more than once.
 _dtype, _grad = operator.attrgetter("dtype"), operator.attrgetter("requires_grad")
 
 
-def _tensors(tensors: Sequence[torch.Tensor], name: str) -> Tuple[list, List[int], list]:
-    """Check a list of contiguous tensors of one device; (tensors, sizes, dtypes)."""
+def _tensors(tensors: Sequence[torch.Tensor], name: str) -> Tuple[list, array.array, list]:
+    """Check a list of contiguous tensors; (tensors, sizes, dtypes).  That all are on
+    the first one's device is checked with their addresses, in the call."""
     given = list(tensors)
-    if not set(map(type, given)) <= {torch.Tensor, torch.nn.Parameter} \
-            and not all(isinstance(t, torch.Tensor) for t in given):
-        raise TypeError("%s must be torch.Tensors" % name)
     if not given:
         raise ValueError("%s: at least one is needed" % name)
-    if not all(map(torch.Tensor.is_contiguous, given)):
+    try:
+        dense = all(map(torch.Tensor.is_contiguous, given))
+    except TypeError:
+        raise TypeError("%s must be torch.Tensors" % name) from None
+    if not dense:
         raise ValueError("%s must be contiguous" % name)
-    if len(set(map(torch.Tensor.get_device, given))) > 1 or not given[0].is_cuda:
+    if not given[0].is_cuda:
         raise ValueError("%s must be on one GPU device" % name)
     dtypes = list(map(_dtype, given))
-    if not set(dtypes) <= _TYPES.keys():
+    if dtypes[0] not in _TYPES or (dtypes.count(dtypes[0]) != len(dtypes) and not set(dtypes) <= _TYPES.keys()):
         raise ValueError("%s must be float32, bfloat16 or float16" % name)
-    return given, list(map(torch.Tensor.numel, given)), dtypes
+    return given, array.array("q", map(torch.Tensor.numel, given)), dtypes
 
 
 def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]], inplace: bool,
@@ -655,25 +657,25 @@ def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[
     given, sizes, dtypes = _tensors(tensors, "tensors")
     dev, count = given[0].device, len(given)
     pointers = array.array("Q", map(torch.Tensor.data_ptr, given))
-    to = []
-    targets = pointers if inplace else None
+    to, targets = [], pointers if inplace else None
     if out is not None:
         to, to_sizes, to_dtypes = _tensors(out, "out")
-        if to_sizes != sizes or to_dtypes != dtypes or to[0].get_device() != given[0].get_device():
-            raise ValueError("out must have the tensors' sizes, types and device")
+        if to_sizes != sizes or to_dtypes != dtypes:
+            raise ValueError("out must have the tensors' sizes and types")
         targets = array.array("Q", map(torch.Tensor.data_ptr, to))
     if torch.is_grad_enabled() and (any(map(_grad, given)) or any(map(_grad, to))):
         _On(dev, stream, tuple(given + to))   # refuses
-    kinds = array.array("i", [_TYPES[dtypes[0]]]) * count if len(set(dtypes)) == 1 else \
+    kinds = array.array("i", [_TYPES[dtypes[0]]]) * count if dtypes.count(dtypes[0]) == count else \
         array.array("i", [_TYPES[t] for t in dtypes])
-    lengths = array.array("q", sizes)
     at = lambda a: None if a is None else a.buffer_info()[0]
     lib = N.load()
     with _On(dev, stream, tuple(given + to) if stream is not None else ()) as s:
         norm = torch.empty((), dtype=torch.float32, device=dev)
-        ws = _workspace(lib.kmeans_clip_workspace_bytes(at(lengths), count), dev, "kmeans_clip_workspace_bytes")
-        st = lib.kmeans_clip_norm(at(pointers), at(targets), at(lengths), at(kinds), count, limit, _p(norm), _p(ws),
+        ws = _workspace(lib.kmeans_clip_workspace_bytes(at(sizes), count), dev, "kmeans_clip_workspace_bytes")
+        st = lib.kmeans_clip_norm(at(pointers), at(targets), at(sizes), at(kinds), count, limit, _p(norm), _p(ws),
                                   ws.numel(), s)
+    if st != N.KM_OK and any(t.device != dev for t in given + to):
+        raise ValueError("all tensors must be on %s" % dev)
     N.check(st, "kmeans_clip_norm")
     if targets is not None:
         torch.autograd.graph.increment_version(given if inplace else to)
