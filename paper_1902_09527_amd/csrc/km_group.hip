@@ -118,7 +118,8 @@ struct ListArgs {
     int32_t *first, *num;   // per cluster: first partial slot, items; null: not wanted
 };
 
-// A block a list.  In order of the clusters.
+// A block a list.  In order of the clusters.  3 us for 16 clusters, 5 for 64 and two
+// lists: a launch's own time, that neither the plan nor the host could save.
 __global__ __launch_bounds__(1024) void k_gr_list(ListArgs A0, ListArgs A1) {
     const ListArgs& A = blockIdx.x ? A1 : A0;
     __shared__ int s[2][16];
@@ -381,6 +382,14 @@ constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, 
 // Blocks stay and take tile after tile.  The stages of all of a block's tiles are
 // one sequence: two of them are in LDS, and the next tile's first ones are on their
 // way while the last ones of a tile are multiplied and its results are written.
+//
+// Tiles of 256 x 256 in 8 waves (one block a compute unit: 128 KB of LDS), 128 x 128
+// (two) or 64 x 64 (four): the larger reads less for a product, the smaller has less
+// past a cluster's end (main_choice has the times).  Bound by the matrix cores where
+// clusters are long: four clusters of 4096 rows, 4096 x 4096 bf16, 475 us (1160
+// TFLOP/s; one of them by the library 1459), 8 bits 246 us (2240).  Skewed clusters
+// of 16,384 rows leave tiles part full: 4096 x 4096 f16, 16 clusters 565 us.  By the
+// memory where they are short: 64 clusters, 2048 x 2048 bf16, 193 us, 4.0 TB/s.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
 __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(MainArgs A) {
     using G = Geo<T, O, TM, TN, WR, WC>;
@@ -671,7 +680,8 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
 }
 
 // The same at any address: a tile a block, a stage in registers while the one
-// before it is multiplied.
+// before it is multiplied.  Stages of whole chunks are loaded with no test, the
+// others chunk by chunk to their buffer (both in registers would spill).  Eight clusters of 512 rows, 1001 to 1003 bf16: 37 us, 33 at 1024 to 1024.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
 __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
     using G = Geo<T, O, TM, TN, WR, WC>;
@@ -847,6 +857,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
 }
 
 // The parts of the contraction, added in order: a block a place and 1024 columns.
+// Bound by the parts' bytes, which the last-level cache holds where there are parts.
 template <class O>
 __global__ __launch_bounds__(256) void k_gr_sum(MainArgs A) {
     const int64_t place = blockIdx.x, col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4, step = A.n * A.P;
@@ -883,7 +894,7 @@ struct GradArgs {
     const int32_t *first, *num;
     void* out;               // k x Q x P
     float* part;             // slots x Q x P
-    int32_t k, P, Q, o4;
+    int32_t k, P, Q;
     int32_t tq, tp;          // tiles
 };
 
@@ -923,6 +934,12 @@ __device__ __forceinline__ void grad_put(const GradArgs& A, const GradTile& q,
 // Blocks stay and take tile after tile, two stages of 128 bytes a column being on
 // their way or in LDS, as in k_gr_main: a tile has few stages where clusters are
 // short, and what it starts and ends with is what they would wait for.
+//
+// Bound by its loads' and stores' latency: 16,384 rows in 64 skewed clusters, 2048 x
+// 2048 bf16, 327 us (403 MB read, 537 written, 2.9 TB/s; 219 with no results
+// written); four clusters of 4096, 4096 x 4096, 600 us (915 TFLOP/s).  Tiles of 128
+// x 128, two a compute unit, took 385 us for the 327: twice the reads.  They stay for
+// small weights, whose tiles would not fill the chip.
 template <class T, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad(GradArgs A) {
     constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC, es = sizeof(T);
@@ -1058,7 +1075,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad(GradArgs A) {
 }
 
 // The same at any address: a tile a block, a stage in registers while the one
-// before it is multiplied.
+// before it is multiplied.  Eight clusters of 512 rows, 1001 x 1003 bf16: 53 us, 44
+// at 1024 x 1024 with k_gr_grad.
 template <class T, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
     constexpr int E = Mma<T>::E, KS = 4 * E, BK = 2 * KS, NT = 64 * WR * WC;
@@ -1160,7 +1178,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
 }
 
 // Clusters of no chunk: zeros; of several: the sum of their parts in order.  16
-// bytes a lane, past the caches.
+// bytes a lane, past the caches.  4 us where there is nothing to join.
 template <class T>
 __global__ __launch_bounds__(256) void k_gr_join(GradArgs A) {
     constexpr int E = 16 / (int)sizeof(T);
@@ -1212,7 +1230,9 @@ struct FewArgs {
 
 // 16 columns and the places of one cluster a block, from the place blockIdx.y on
 // if a cluster starts there; its NWAVE waves share the contraction, some four steps
-// each.
+// each.  No list and no workspace: one launch.  48 rows of 4096, 100 clusters, 4096
+// columns in 8 bits: 128 us, the rate of a copy; 32 rows of 1024, 8 clusters, bf16:
+// 7 us.
 template <class T, class O>
 struct FewOp {
     static constexpr int kBytes = 16;   // of a row a lane and step
@@ -1433,11 +1453,6 @@ hipError_t main_go(MainArgs A, const MainPlan& M, bool al, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class T>
-bool rows16(const void* p, int64_t ld, int64_t d) {
-    return rows_vec16(p, ld, d, sizeof(T));
-}
-
 ListArgs list_args(const GroupArgs& D, const GroupList& L, char* ws, bool cut) {
     ListArgs A{};
     A.offsets = D.offsets;
@@ -1463,7 +1478,7 @@ hipError_t lists_go(const GroupArgs& D, const GroupList* rows, const GroupList* 
 template <class T, class O>
 hipError_t forward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStream_t s) {
     if (L.few) {
-        const bool al = rows16<T>(D.X, D.ldx, D.di) && D.di % (16 / (int)sizeof(T)) == 0 && a16(D.W);
+        const bool al = rows_vec16(D.X, D.ldx, D.di, sizeof(T)) && D.di % (16 / (int)sizeof(T)) == 0 && a16(D.W);
         FewArgs F{};
         F.U = D.X;
         F.ldu = D.ldx;
@@ -1584,7 +1599,6 @@ hipError_t backward_t(const GroupArgs& D, char* ws, const GroupShape& L, hipStre
         G.k = D.k;
         G.P = D.di;
         G.Q = D.dout;
-        G.o4 = D.di % 4 == 0 && a16(D.dW);
         if (L.cuts.max_items > 0) {
             const bool whole = grad_ok<T>(D.X, D.ldx, D.n, D.di, D.order, L.cuts.size) &&
                                grad_ok<T>(D.dY, D.lddy, D.n, D.dout, D.order, L.cuts.size);
