@@ -508,7 +508,7 @@ def quantize_blocks(X: torch.Tensor, stream: Optional[torch.cuda.Stream] = None)
     if isinstance(X, torch.Tensor) and X.dim() == 3:
         if not X.is_contiguous():
             raise ValueError("X must be contiguous")
-        rows = X.view(-1, X.shape[2])
+        rows = X.view(X.shape[0] * X.shape[1], X.shape[2])
     else:
         rows = X
     ld = _rows(rows, "X")

@@ -107,7 +107,7 @@ def test_binding_rejects_cpu_tensors():
     w, plan = torch.zeros(2, 8, 8), km.ClusterPlan(i, i, i, torch.zeros(3, dtype=torch.int32), 4, 1, 2)
     q = km.BlockRows(x.to(torch.float8_e4m3fn), torch.ones(4, 1, dtype=torch.uint8))
     for call in (lambda: km.cluster_linear(x, w, plan), lambda: km.cluster_linear_backward(x, x, w, plan),
-                 lambda: km.quantize_blocks(x), lambda: km.dequantize_blocks(q),
+                 lambda: km.quantize_blocks(x), lambda: km.quantize_blocks(torch.zeros(2, 3, 0)), lambda: km.dequantize_blocks(q),
                  lambda: km.cluster_linear_fp8(x, km.BlockRows(w, w), plan), lambda: km.cluster_embedding(i, x),
                  lambda: km.cluster_embedding_backward(x, plan), lambda: km.global_norm([x]),
                  lambda: km.clip_global_norm([x], 1.0)):
