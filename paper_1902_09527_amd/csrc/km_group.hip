@@ -681,7 +681,8 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
 
 // The same at any address: a tile a block, a stage in registers while the one
 // before it is multiplied.  Stages of whole chunks are loaded with no test, the
-// others chunk by chunk to their buffer (both in registers would spill).  Eight clusters of 512 rows, 1001 to 1003 bf16: 37 us, 33 at 1024 to 1024.
+// others chunk by chunk to their buffer (both in registers would spill).  Eight
+// clusters of 512 rows, 1001 to 1003 bf16: 34 us, 33 at 1024 to 1024.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
 __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
     using G = Geo<T, O, TM, TN, WR, WC>;
@@ -1637,8 +1638,12 @@ MainChoice main_choice(int64_t n, int64_t met, int32_t K, int32_t P, int type, b
     const Kind kinds[3] = {{256, 1, {1.65, 7.2, 1.75}, {1.05, 7.0, 1.1}, {3.5, 1.0, 5.5}},
                            {128, 2, {1.15, 3.3, 1.15}, {0.85, 1.7, 0.85}, {2.5, 1.0, 2.2}},
                            {64, 4, {0.96, 1.55, 0.85}, {0.6, 0.6, 0.5}, {2.0, 1.0, 2.0}}};
-    const Kind anywhere[2] = {{128, 2, {2.4, 4.5, 2.4}, {1.7, 2.6, 1.7}, {3.0, 2.0, 3.0}},
-                              {64, 4, {1.6, 2.0, 1.6}, {1.1, 1.1, 1.1}, {2.0, 2.0, 2.0}}};
+    // At any address blocks come as others end: no round is waited for, and a stage's time
+    // grows from `alone` with the tiles that share a compute unit (1001 to 1003 columns
+    // in bf16, 8 clusters of 512: 34 us with tiles of 128, 37 with 64; 2001 to 2003, 4 of
+    // 2000: 131 and 206; 3001 to 301, 100 of 30: 92 and 46).
+    const Kind anywhere[2] = {{128, 2, {1.6, 5.2, 2.1}, {1.55, 2.6, 1.9}, {3.0, 3.0, 3.0}},
+                              {64, 4, {1.4, 1.9, 1.8}, {0.65, 1.1, 1.0}, {3.0, 3.0, 3.0}}};
     MainChoice best{128, 1};
     double least = 0;
     for (int q = 0; q < (main ? 3 : 2); ++q) {
@@ -1650,9 +1655,12 @@ MainChoice main_choice(int64_t n, int64_t met, int32_t K, int32_t P, int type, b
             const int share = part_stages(all, splits, type == kF8);
             if (splits > 1 && share * (splits - 1) >= all) continue;   // no part without a stage
             const double tiles = items * ((P + k.tile - 1) / k.tile) * splits, rounds = tiles / (kCus * k.held);
-            const double stage = tiles <= kCus ? k.alone[i] : k.busy[i];
+            double stage = tiles <= kCus ? k.alone[i] : k.busy[i];
+            if (!main && tiles > kCus && rounds < 1)
+                stage = k.alone[i] + (k.busy[i] - k.alone[i]) * (tiles / kCus - 1) / (k.held - 1);
             // Small tiles make up for each other's waits.
-            double t = (k.tile == 64 && rounds > 1 ? rounds + 0.5 : ceil(rounds)) * stage * (share + k.edge[i]);
+            const bool flows = k.tile == 64 || !main;
+            double t = (flows && rounds > 1 ? rounds + 0.5 : ceil(rounds)) * stage * (share + k.edge[i]);
             if (splits > 1) t += 6 + (double)splits * n * P * 8 / 4e6;   // sums at 4 TB/s, and a launch
             if (least == 0 || t < least) {
                 least = t;
