@@ -368,13 +368,14 @@ struct Tile {
     int c, p0, rows, bn, split, k0;
 };
 // A tile's parts, then down 4 row tiles before the next columns.
-template <int TN>
+template <class T, int TN, int NT, bool TR>
 __device__ __forceinline__ Tile tile_at(const MainArgs& A, int items, int u) {
     const int t = u / A.splits, split = u - t * A.splits;
     const int group = 4 * A.tn, grp = t / group, m0 = grp * 4, in = t - grp * group;
     const int gm = items - m0 < 4 ? items - m0 : 4;
     const GroupItem it = item_at(A.items, m0 + in % gm);
-    return Tile{it.c, it.p0, it.p1 - it.p0, in / gm * TN, split, split * A.share};
+    const int bn = in / gm * TN;
+    return Tile{it.c, it.p0, it.p1 - it.p0, TR ? TrStage<T, TN, NT>::first(bn, A.P) : bn, split, split * A.share};
 }
 
 constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, twice
@@ -419,8 +420,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
         int lk = 0, whole = 0, bn_load = 0;   // that stage, the stages without a chunk past an end, and its columns
         const int uc = swz(tid / 8, tid % 8) * E;   // NT / 8 rows further on the swizzle is the same
         const uint32_t es = sizeof(T), ldub = (uint32_t)A.ldu * es, ldwb = (uint32_t)(TR ? A.P : A.K) * es;
-        constexpr int kDown = NT / CPR;   // TR: rows from one chunk of a thread to its next (16 of them swizzle alike)
-        static_assert(!TR || kDown % 8 == 0, "");
+        using S = TrStage<T, TN, NT>;   // TR
         // The rows of a tile, a thread each, by way of LDS (rows past the last: not stored).
         auto fetch_row = [&](const Tile& q) {
             return tid < TM ? (int32_t)row_of(A.order, q.p0 + (tid < q.rows ? tid : q.rows - 1)) : 0;
@@ -434,8 +434,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
             if constexpr (TR) {
                 wb = W + (int64_t)q.bn * es + (int64_t)q.k0 * BK * ldwb;
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    wo[i] = tid / CPR * ldwb + swz_tr<T, CPR>(i * kDown + tid / CPR, tid % CPR) * E * es;
+                for (int i = 0; i < 2; ++i) wo[i] = S::behind(i, tid, ldwb);
             } else {
                 wb = W + (int64_t)q.bn * ldwb + (int64_t)q.k0 * 128;
                 const int last = A.P - 1 - q.bn;   // columns past it: not stored
@@ -447,7 +446,8 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
             }
             bn_load = q.bn;
             lk = q.k0;
-            whole = !TR || A.P >= TN ? A.K / BK : 0;
+            if constexpr (TR) whole = S::whole(A.K, A.P);
+            else whole = A.K / BK;
         };
         // Chunk i (of NU + NW a thread) of the next stage to LDS; guard: it may lie past an end.
         auto load = [&](int i, char* buf, bool guard) {
@@ -458,9 +458,8 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
                 src = ub + uo[i];
                 if (guard) in = lk * BK + uc < A.K;
             } else if constexpr (TR) {
-                const int x = (i - NU) * NT + tid, kk = x / CPR;
-                src = wb + (uint64_t)((i - NU) * kDown) * ldwb + wo[(i - NU) % 2];
-                if (guard) in = lk * BK + kk < A.K && bn_load + swz_tr<T, CPR>(kk, x % CPR) * E < A.P;
+                src = wb + S::above(i - NU, ldwb) + wo[(i - NU) % 2];
+                if (guard) in = S::in(i - NU, tid, lk, bn_load, A.K, A.P);
             } else {
                 src = wb + wo[i - NU];
                 if (guard) in = lk * BK + uc < A.K;
@@ -508,7 +507,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
                 if (tid < TM + TN) __builtin_memcpy(s_scale + (b * (TM + TN) + tid) * kWindow, sv, 8);
         };
 
-        Tile cur = tile_at<TN>(A, items, t);
+        Tile cur = tile_at<T, TN, NT, TR>(A, items, t);
         {
             const int32_t row = fetch_row(cur);
             if (tid < TM) s_rows[tid] = row;
@@ -626,7 +625,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
             Tile next = cur;
             int32_t row = 0;
             if (more) {
-                next = tile_at<TN>(A, items, t + step);
+                next = tile_at<T, TN, NT, TR>(A, items, t + step);
                 row = fetch_row(next);
             }
             live = (cur.rows + kTurn - 1) / kTurn;
@@ -699,10 +698,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
     const int tiles = items * A.tn * A.splits, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if ((int)(blockIdx.x / 8) < per && t < tiles) {
-        Tile q = tile_at<TN>(A, items, t);
-        // The last tile of a width that TN does not divide moves left until it is whole:
-        // it and its neighbour then write the same values.
-        if (TR && A.P >= TN && q.bn > A.P - TN) q.bn = A.P - TN;
+        const Tile q = tile_at<T, TN, NT, TR>(A, items, t);
         const int all = (A.K + BK - 1) / BK, end = q.k0 + A.share < all ? q.k0 + A.share : all;
         const int live = (q.rows + kTurn - 1) / kTurn;
         const int64_t ldw = TR ? A.P : A.K;
@@ -730,7 +726,9 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
             }
         }
         // Stages without a chunk past the contraction's end or the last column.
-        const int whole = !TR || A.P >= TN ? A.K / BK : 0;
+        int whole;
+        if constexpr (TR) whole = TrStage<T, TN, NT>::whole(A.K, A.P);
+        else whole = A.K / BK;
         typedef u32x4 __attribute__((aligned(1))) any4;
         u32x4 v[NU + NW];
         bool held = false;   // the stage is in v, else in its buffer already

@@ -1,10 +1,12 @@
 // Tiles of rows for the matrix cores (km_adapter.hip, km_group.hip): operand
-// chunks, their moves to LDS and the transposing reads from it.
+// chunks, their moves to LDS and the transposing reads from it (km_places.h: where
+// they lie).
 #pragma once
 
 #include <type_traits>
 
 #include "km_ops.h"
+#include "km_places.h"
 
 namespace km {
 
@@ -124,20 +126,6 @@ __device__ __forceinline__ void load_lds16(const void* src, char* wave_base) {
 }
 
 __device__ __forceinline__ int64_t row_of(const int32_t* order, int64_t place) { return order ? order[place] : place; }
-
-// Chunk position of a stage's rows in LDS: rows are 128 bytes, so 16 rows read
-// at one chunk index fall on all 64 banks once.
-__device__ __forceinline__ int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
-
-__device__ __forceinline__ int swz4(int row, int c) { return c ^ ((row >> 2) & 3); }   // rows of 64 bytes
-
-// The same for tiles that hold the contraction along their rows (TR): 16-bit
-// tiles are read 4 rows x 16 columns at a time, float32 by columns.
-template <class T, int CPR>
-__device__ __forceinline__ int swz_tr(int k, int c) {
-    const int m = sizeof(T) == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2;
-    return c ^ (m & (CPR - 1));
-}
 
 // Operand of 16 columns c0 .. along rows k0 + 0 .. of a tile whose rows are the
 // contraction (CPR chunks a row).  The swizzle is the same k0 rows further (a
