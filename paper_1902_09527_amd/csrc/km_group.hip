@@ -71,9 +71,9 @@ struct Op<uint8_t, O> {
     static __device__ __forceinline__ int run(int j, int lane) { return j * 8 + (lane >> 5) * 4; }
 };
 
-// Eight e4m3 values times 2^(byte - 127) as bfloat16, which holds them exactly.
+// Eight e4m3 values as bfloat16, which holds them exactly; NaN under a byte of 255.
 __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, int byte) {
-    const float scale = __builtin_bit_cast(float, byte > 0 ? (uint32_t)byte << 23 : 0x400000u);
+    const float scale = byte == 255 ? INFINITY : 1.0f;
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     struct Four {
         bf16x2 v[4];
@@ -84,7 +84,9 @@ __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, int byte) {
     return __builtin_bit_cast(u32x4, o);
 }
 // e4m3 values with float32 results: widened to bfloat16, whose products and sums
-// keep float32.  A chunk is the operand of two steps.
+// keep float32.  A chunk is the operand of two steps.  The powers of two go to the
+// sums of a block (add_scaled): values times theirs may lie outside of bfloat16, the
+// products' being in range, and its matrix steps lose what lies below 2^-126.
 template <>
 struct Op<uint8_t, float> {
     static constexpr int R = 16, E = 16;
@@ -96,15 +98,29 @@ struct Op<uint8_t, float> {
     static __device__ __forceinline__ Frag read(const char* buf, int at) {
         return {*reinterpret_cast<const u32x4*>(buf + at)};
     }
-    static __device__ __forceinline__ Acc mma(const Frag& a, const Frag& b, Acc c, int sa, int sb) {
+    struct Wide {
+        u32x4 v[2];
+    };
+    static __device__ __forceinline__ Wide wide(const Frag& a, int byte) {
+        return {{widen(a.v[0], a.v[1], byte), widen(a.v[2], a.v[3], byte)}};
+    }
+    static __device__ __forceinline__ Acc mma(const Wide& a, const Wide& b, Acc c) {
+        return Mma<__bf16>::mma(a.v[1], b.v[1], Mma<__bf16>::mma(a.v[0], b.v[0], c));
+    }
+    // v times the powers of its first operand's rows (bytes a) and its second's (b).
+    static __device__ __forceinline__ void add_scaled(Acc& c, const Acc& v, const int (&a)[4], int b) {
 #pragma unroll
-        for (int i = 0; i < 4; i += 2)
-            c = Mma<__bf16>::mma(widen(a.v[i], a.v[i + 1], sa), widen(b.v[i], b.v[i + 1], sb), c);
-        return c;
+        for (int i = 0; i < 4; ++i) c[i] += __builtin_ldexpf(v[i], a[i] + b - 254);
     }
     static constexpr int kRuns = 1;
     static __device__ __forceinline__ int run(int, int lane) { return (lane >> 4) * 4; }
 };
+
+// 8 bits with float32 results: widened operands take the registers of the larger
+// tiles, so there is one form at any address (16,380 rows, 10 clusters, 4096 to 8192:
+// 1.44 to 1.51 ms; four clusters of 2000 rows, 2001 to 2003: 123 us).
+template <class T, class O>
+constexpr bool kWide = sizeof(T) == 1 && sizeof(O) == 4;
 
 // --------------------------------------------------------------------------
 // Lists of row tiles and of chunks.
@@ -683,7 +699,7 @@ __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(Main
 // others chunk by chunk to their buffer (both in registers would spill).  Eight
 // clusters of 512 rows, 1001 to 1003 bf16: 34 us, 33 at 1024 to 1024.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
-__global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
+__global__ __launch_bounds__(64 * WR * WC, (kWide<T, O> && TM == 64 ? 4 : 1)) void k_gr_any(MainArgs A) {
     using G = Geo<T, O, TM, TN, WR, WC>;
     using P = typename G::P;
     constexpr bool F8 = sizeof(T) == 1;
@@ -802,35 +818,64 @@ __global__ __launch_bounds__(64 * WR * WC) void k_gr_any(MainArgs A) {
             if (kt + 1 < end) fetch(kt + 1, s_tiles + (at ^ 1) * kStage);
             int sa[F8 ? FC : 1], sb[F8 ? FR : 1];
             if constexpr (F8) {
+                const uint8_t* cols = s_scale + (TM + wc * (TN / WC)) * kScales + (kt - q.k0) % kScales;
 #pragma unroll
-                for (int h = 0; h < FC; ++h)
-                    sa[h] = s_scale[(TM + wc * (TN / WC) + h * R + li) * kScales + (kt - q.k0) % kScales];
+                for (int h = 0; h < FC; ++h) sa[h] = cols[(h * R + li) * kScales];
 #pragma unroll
                 for (int f = 0; f < FR; ++f) sb[f] = s_scale[(G::row(f, wr) + li) * kScales + (kt - q.k0) % kScales];
-            }
+                if constexpr (kWide<T, O>) {   // a stage is a block
+                    typename P::Wide a[2][FC];
+                    int sr[FC][4];   // of the columns of a lane's results
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                typename P::Frag b[FR], a[FC];
+                    for (int h = 0; h < FC; ++h) {
 #pragma unroll
-                for (int f = 0; f < FR; ++f) b[f] = P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128);
-                if constexpr (TR) {
-                    u32x4 x[FC];
-                    if (s == 0) read_tr_wait<T, CPR, 0>(x, buf, wa);
-                    else read_tr_wait<T, CPR, KS>(x, buf, wa);
+                        for (int s = 0; s < 2; ++s)
+                            a[s][h] = P::wide(P::read(buf, (wa[0] ^ (s * 64)) + h * (R * 128)), sa[h]);
 #pragma unroll
-                    for (int h = 0; h < FC; ++h) a[h].v = x[h];
-                } else {
+                        for (int i = 0; i < 4; ++i) sr[h][i] = cols[(h * R + P::run(0, lane) + i) * kScales];
+                    }
 #pragma unroll
-                    for (int h = 0; h < FC; ++h) a[h] = P::read(buf, (wa[0] ^ (s * 64)) + h * (R * 128));
+                    for (int f = 0; f < FR; ++f) {
+                        if (f / FP >= live) continue;
+                        typename P::Wide b[2];
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            b[s] = P::wide(P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128), sb[f]);
+#pragma unroll
+                        for (int h = 0; h < FC; ++h) {
+                            typename P::Acc v{0, 0, 0, 0};
+#pragma unroll
+                            for (int s = 0; s < 2; ++s) v = P::mma(a[s][h], b[s], v);
+                            P::add_scaled(acc[f][h], v, sr[h], sb[f]);
+                        }
+                    }
                 }
+            }
+            if constexpr (!kWide<T, O>) {
 #pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    if (p >= live) continue;
+                for (int s = 0; s < 2; ++s) {
+                    typename P::Frag b[FR], a[FC];
 #pragma unroll
-                    for (int f = p * FP; f < (p + 1) * FP; ++f)
+                    for (int f = 0; f < FR; ++f) b[f] = P::read(buf, (ua ^ (s * 64)) + (f / FP * kTurn + f % FP * R) * 128);
+                    if constexpr (TR) {
+                        u32x4 x[FC];
+                        if (s == 0) read_tr_wait<T, CPR, 0>(x, buf, wa);
+                        else read_tr_wait<T, CPR, KS>(x, buf, wa);
 #pragma unroll
-                        for (int h = 0; h < FC; ++h)
-                            acc[f][h] = P::mma(a[h], b[f], acc[f][h], sa[F8 ? h : 0], sb[F8 ? f : 0]);
+                        for (int h = 0; h < FC; ++h) a[h].v = x[h];
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < FC; ++h) a[h] = P::read(buf, (wa[0] ^ (s * 64)) + h * (R * 128));
+                    }
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p) {
+                        if (p >= live) continue;
+#pragma unroll
+                        for (int f = p * FP; f < (p + 1) * FP; ++f)
+#pragma unroll
+                            for (int h = 0; h < FC; ++h)
+                                acc[f][h] = P::mma(a[h], b[f], acc[f][h], sa[F8 ? h : 0], sb[F8 ? f : 0]);
+                    }
                 }
             }
             if (F8 && (kt + 1 - q.k0) % kScales == 0 && kt + 1 < end) {
@@ -1252,9 +1297,18 @@ struct FewOp<uint8_t, O> {
 template <>
 struct FewOp<uint8_t, float> {
     static constexpr int kBytes = 16;
-    using Frag = Op<uint8_t, float>::Frag;
-    static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, int sa, int sb) {
-        return Op<uint8_t, float>::mma(a, b, c, sa, sb);
+    using Q = Op<uint8_t, float>;
+    using Frag = Q::Frag;
+    // The products of B steps of one block, with the bytes of the lane's column and row.
+    template <int B>
+    static __device__ __forceinline__ void add(f32x4& c, const Frag* a, const Frag (&b)[B], int sa, int sb) {
+        f32x4 v{0, 0, 0, 0};
+#pragma unroll
+        for (int z = 0; z < B; ++z) v = Q::mma(Q::wide(a[z], sa), Q::wide(b[z], sb), v);
+        int cols[4];   // the lane's results are of four other columns
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cols[i] = __shfl(sa, (threadIdx.x & 48) + Q::run(0, threadIdx.x & 63) + i);
+        Q::add_scaled(c, v, cols, sb);
     }
 };
 
@@ -1313,10 +1367,23 @@ __device__ __forceinline__ void few_block(const FewArgs& A, int c, int p0, int r
             }
         }
         __builtin_amdgcn_sched_barrier(0);   // all of them are issued before the first is waited for
+        if constexpr (kWide<T, O>) {
+            constexpr int B = UN % 2 == 0 ? 2 : 1;   // two steps are a block
 #pragma unroll
-        for (int y = 0; y < UN; ++y)
+            for (int y = 0; y < UN; y += B)
 #pragma unroll
-            for (int f = 0; f < RF; ++f) acc[f] = P::mma(a[y], b[y][f], acc[f], F8 ? sa[y] : 0, F8 ? sb[y][f] : 0);
+                for (int f = 0; f < RF; ++f) {
+                    typename P::Frag rows[B];
+#pragma unroll
+                    for (int z = 0; z < B; ++z) rows[z] = b[y + z][f];
+                    P::add(acc[f], a + y, rows, sa[y], sb[y][f]);
+                }
+        } else {
+#pragma unroll
+            for (int y = 0; y < UN; ++y)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) acc[f] = P::mma(a[y], b[y][f], acc[f], F8 ? sa[y] : 0, F8 ? sb[y][f] : 0);
+        }
     }
     // The waves' sums: the upper half's to the lower half, then in order.
     constexpr int H = NWAVE / 2;
@@ -1411,11 +1478,6 @@ bool main_ok(const void* U, int64_t ld, int64_t n, int64_t K, const void* W, int
     return rows_vec16(U, ld, K, es) && w * es % 16 == 0 && a16(W) && (order ? n : 256) * ld * es < most &&
            256 * w * es < most;
 }
-
-// 8 bits with float32 results: widened operands take the registers of the larger
-// tiles, so there is one form at any address.
-template <class T, class O>
-constexpr bool kWide = sizeof(T) == 1 && sizeof(O) == 4;
 
 // A product's tiles and parts as the launch takes them: those of any addresses where
 // rows or weights cannot be read 16 bytes at a time.
