@@ -27,9 +27,10 @@
  * overlap inputs (kmeans_clip_norm may work in place).  Rows have at most 2^28
  * elements.  Workspaces are the caller's: device memory of at least the bytes
  * that the *_workspace_bytes function gives, 256-byte aligned, contents on entry
- * of no matter, not to be used by another call until this one's work completes.  Sums, statistics and gradients are formed in
- * float32 and rounded once to the type of the output; equal inputs give
- * bitwise equal outputs.
+ * of no matter, not to be used by another call until this one's work completes.
+ * Sums, statistics and gradients are formed in float32 and rounded once to the type
+ * of the output (kmeans_fp8_forward says what its results of 16 bits keep); equal
+ * inputs give bitwise equal outputs.
  */
 #ifndef KMEANS_OPS_H
 #define KMEANS_OPS_H
@@ -209,8 +210,15 @@ int kmeans_fp8_dequantize(const void* values, const uint8_t* exponents, int64_t 
 
 /*
  * kmeans_linear_forward with both operands in 8 bits: y = sum of the products of
- * the values that they stand for, in float32, rounded to y_type (KM_F32, KM_BF16
- * or KM_F16).  W: k x dout x din values with k x dout x ceil(din / 128)
+ * the values that they stand for, rounded to y_type (KM_F32, KM_BF16 or KM_F16).
+ * Sums: for KM_F32 all float32.  For KM_BF16 and KM_F16 the products of each 8
+ * consecutive elements (from a multiple of 8 on) are aligned to the one of the
+ * largest exponent, and what lies more than 13 bits below it is dropped: less than
+ * 2^-10 2^m of the 8 together, m being the largest sum of two values' exponents
+ * (their powers of two counted; an e4m3 value below 2^-6 has that exponent); these sums
+ * of 8 are added in float32.  That is below a bfloat16 result's own rounding where
+ * products do not cancel, but may be two of a float16 one's: for float32 sums take
+ * KM_F32 and round its results.  W: k x dout x din values with k x dout x ceil(din / 128)
  * exponents.  X: of type KM_E4M3 with its exponents (n x ceil(din / 128) bytes),
  * or of another type with exponents = NULL: quantised in the workspace.
  */

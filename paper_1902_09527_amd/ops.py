@@ -539,13 +539,19 @@ def dequantize_blocks(Q: BlockRows, dtype: torch.dtype = torch.float32,
 def cluster_linear_fp8(X, W: BlockRows, plan: ClusterPlan, sorted_rows: bool = False,
                        dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None
                        ) -> torch.Tensor:
-    """:func:`cluster_linear` with both operands in 8 bits (kmeans_fp8_forward);
-    sums are float32.
+    """:func:`cluster_linear` with both operands in 8 bits (kmeans_fp8_forward).
 
     W: [k, dout, din], quantised once.  X: rows [n, din], quantised in the call
     as :func:`quantize_blocks` does, or :class:`BlockRows`.  ``dtype``: of the
     results (default: X's type, bfloat16 for BlockRows).  For serving: the
     gradients of such a layer are those of :func:`cluster_linear`.
+
+    float32 results have float32 sums.  For bfloat16 and float16 the matrix cores
+    drop, of the products of each 8 consecutive elements, what lies more than 13
+    bits below the largest one's exponent m (less than 2^-10 2^m of the 8 together)
+    and add these sums in float32: 1.3e-5 of the norm for normal values, but up to
+    two roundings of a float16 result where one product of 8 is far larger than the
+    rest.  Where that counts, take float32 results and round them.
     """
     _blocks(W, "W", (3,))
     k, dout, din = W.shape
