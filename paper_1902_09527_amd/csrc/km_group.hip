@@ -338,12 +338,16 @@ struct MainArgs {
     float* part;              // splits x n x P, by place
 };
 
+// A block's place among all of a grid's: a launch has fewer than 2^32 threads in a
+// dimension, so grids of a block a tile may have two (many_blocks).
+__device__ __forceinline__ uint32_t block_at() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Rows of no cluster: zeros, by all blocks, a wave a row.
 template <class O>
 __device__ __forceinline__ void zero_rows(const MainArgs& A, int waves) {
     constexpr int E = 16 / (int)sizeof(O);
-    const int64_t step = (int64_t)gridDim.x * waves;
-    for (int64_t p = A.used[0] + (int64_t)blockIdx.x * waves + (threadIdx.x >> 6); p < A.n; p += step) {
+    const int64_t step = (int64_t)gridDim.x * gridDim.y * waves;
+    for (int64_t p = A.used[0] + (int64_t)block_at() * waves + (threadIdx.x >> 6); p < A.n; p += step) {
         O* y = static_cast<O*>(A.Y) + row_of(A.order, p) * A.P;
         for (int64_t col = (threadIdx.x & 63) * E; col < A.P; col += 64 * E) {
             const u32x4 zero{0, 0, 0, 0};
@@ -716,9 +720,10 @@ __global__ __launch_bounds__(64 * WR * WC, (kWide<T, O> && TM == 64 ? 4 : 1)) vo
     const int tid = threadIdx.x, lane = tid & 63, li = lane % R;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int items = __builtin_amdgcn_readfirstlane(A.count[0]);
-    const int tiles = items * A.tn * A.splits, per = (tiles + 7) / 8, t = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if ((int)(blockIdx.x / 8) < per && t < tiles) {
-        const Tile q = tile_at<T, TN, NT, TR>(A, items, t);
+    const uint32_t block = block_at();
+    const int64_t tiles = (int64_t)items * A.tn * A.splits, per = (tiles + 7) / 8, t = block % 8 * per + block / 8;
+    if (block / 8 < per && t < tiles) {
+        const Tile q = tile_at<T, TN, NT, TR>(A, items, (int)t);
         const int all = (A.K + BK - 1) / BK, end = q.k0 + A.share < all ? q.k0 + A.share : all;
         const int live = (q.rows + kTurn - 1) / kTurn;
         const int64_t ldw = TR ? A.P : A.K;
@@ -962,7 +967,7 @@ __device__ __forceinline__ GradTile grad_tile_at(const GradArgs& A, int64_t t) {
 }
 // The j-th tile of an XCD: eight consecutive ones go to one, the next eight to the
 // next, so that all share the tiles of a long cluster.
-__device__ __forceinline__ int64_t grad_index(int64_t j) { return (j / 8 * 8 + blockIdx.x % 8) * 8 + j % 8; }
+__device__ __forceinline__ int64_t grad_index(int64_t j, uint32_t block) { return (j / 8 * 8 + block % 8) * 8 + j % 8; }
 
 template <class T, int TM, int TN, int WR, int WC>
 __device__ __forceinline__ void grad_put(const GradArgs& A, const GradTile& q,
@@ -1001,10 +1006,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad(GradArgs A) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp, step = gridDim.x / 8;
     int64_t j = blockIdx.x / 8;
-    if (grad_index(j) >= tiles) return;
+    if (grad_index(j, blockIdx.x) >= tiles) return;
     // This tile and the three after it (of no places where there are none).
     auto tile = [&](int64_t x) {
-        const int64_t t = grad_index(x);
+        const int64_t t = grad_index(x, blockIdx.x);
         return t < tiles ? grad_tile_at<TM, TN>(A, t) : GradTile{0, 0, 0, 0, 0, 0};
     };
     GradTile q0 = tile(j), q1 = tile(j + step), q2 = tile(j + 2 * step), q3 = tile(j + 3 * step);
@@ -1135,7 +1140,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_gr_grad_any(GradArgs A) {
     extern __shared__ __align__(16) char s_tiles[];   // two stages: V, then U
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
-    const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp, t = grad_index(blockIdx.x / 8);
+    const uint32_t block = block_at();
+    const int64_t tiles = (int64_t)__builtin_amdgcn_readfirstlane(A.count[0]) * A.tq * A.tp;
+    const int64_t t = grad_index(block / 8, block);
     if (t >= tiles) return;
     GradTile q = grad_tile_at<TM, TN>(A, t);
     // The last tile of a width that TM does not divide moves left until it is whole: it and
@@ -1437,6 +1444,14 @@ hipError_t raise_lds(K* kernel, int bytes) {
 
 constexpr int kCus = 256;
 
+// A grid of at least `blocks` blocks, which block_at numbers; of 2^20 in the first
+// dimension where they are more (512 threads of a block: 2^29).
+dim3 many_blocks(int64_t blocks) {
+    constexpr int64_t kMost = 1 << 20;
+    if (blocks <= kMost) return dim3((unsigned)blocks);
+    return dim3((unsigned)kMost, (unsigned)((blocks + kMost - 1) / kMost));
+}
+
 // Stages of one of `splits` parts of `all` stages: whole windows of scales in 8 bits.
 int part_stages(int all, int splits, bool f8) {
     const int share = (all + splits - 1) / splits;
@@ -1469,7 +1484,7 @@ hipError_t any_tile(MainArgs A, int64_t max_items, hipStream_t s) {
         const hipError_t e = raise_lds(k_gr_any<T, O, TM, TN, WR, WC, TR>, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_gr_any<T, O, TM, TN, WR, WC, TR>), dim3((unsigned)((max_items * A.tn * A.splits + 7) / 8 * 8)),
+    hipLaunchKernelGGL((k_gr_any<T, O, TM, TN, WR, WC, TR>), many_blocks((max_items * A.tn * A.splits + 7) / 8 * 8),
                        dim3(64 * WR * WC), lds, s, A);
     return hipGetLastError();
 }
@@ -1609,7 +1624,7 @@ hipError_t grad_tile(GradArgs A, int64_t max_items, bool al, hipStream_t s) {
         hipLaunchKernelGGL((k_gr_grad<T, TILE, TILE, 2, WC>), dim3((unsigned)(tiles < most ? tiles : most)),
                            dim3(128 * WC), lds, s, A);
     } else {
-        hipLaunchKernelGGL((k_gr_grad_any<T, 128, 128, 2, 2>), dim3((unsigned)tiles), dim3(256), 2 * 2 * 128 * 128, s, A);
+        hipLaunchKernelGGL((k_gr_grad_any<T, 128, 128, 2, 2>), many_blocks(tiles), dim3(256), 2 * 2 * 128 * 128, s, A);
     }
     return hipGetLastError();
 }
