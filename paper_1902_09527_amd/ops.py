@@ -45,6 +45,15 @@ from . import _native as N
 
 _TYPES = {torch.float32: N.KM_F32, torch.bfloat16: N.KM_BF16, torch.float16: N.KM_F16}
 
+# Sizes go to the library as 32-bit numbers (rows as 64-bit ones), and ctypes keeps a
+# larger one's low bits without an error: they are checked here.
+_MOST = 2 ** 31 - 1
+_MOST_COLUMNS = 2 ** 28
+
+
+def _too_large(what: str, most: str) -> N.KMError:
+    return N.KMError(N.KM_ERR_INVALID_ARG, what, "at most %s" % most)
+
 
 def _gpu(t: torch.Tensor, name: str, device: Optional[torch.device] = None) -> None:
     if not isinstance(t, torch.Tensor):
@@ -68,6 +77,8 @@ def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None, n: Op
     rows, cols = t.shape
     if cols < 1:
         raise ValueError("%s must have at least one column" % name)
+    if cols > _MOST_COLUMNS:
+        raise _too_large("columns of %s" % name, "2^28")
     if n is not None and rows != n:
         raise ValueError("%s must have %d rows, got %d" % (name, n, rows))
     if d is not None and cols != d:
@@ -319,6 +330,8 @@ def _adapters(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor
     _array(W, "W", X.dtype, (dout, din), X.device)
     _array(A, "A", X.dtype, (k, r, din), X.device)
     _array(B, "B", X.dtype, (k, dout, r), X.device)
+    if max(dout, k, r) > _MOST:
+        raise _too_large("sizes of W, A and B", "2^31 - 1")
     if scale is not None:
         _array(scale, "scale", torch.float32, (k,), X.device)
     return din, dout, k, r
@@ -411,6 +424,8 @@ def _experts(X: torch.Tensor, W: torch.Tensor) -> Tuple[int, int, int]:
     if X.shape[1] != din:
         raise ValueError("X must have %d columns" % din)
     _array(W, "W", X.dtype, (k, dout, din), X.device)
+    if max(dout, k) > _MOST:
+        raise _too_large("sizes of W", "2^31 - 1")
     return din, dout, k
 
 
@@ -496,6 +511,8 @@ def _blocks(q: BlockRows, name: str, dims: Tuple[int, ...], device: Optional[tor
     if q.values.dim() not in dims or q.values.shape[-1] < 1:
         raise ValueError("%s must have %s dimensions and at least one column" % (name, " or ".join(map(str, dims))))
     shape = tuple(q.values.shape)
+    if shape[-1] > _MOST_COLUMNS:
+        raise _too_large("columns of %s" % name, "2^28")
     _array(q.values, name + ".values", _E4M3, shape, q.values.device)
     _array(q.exponents, name + ".exponents", torch.uint8, shape[:-1] + ((shape[-1] + 127) // 128,), q.values.device)
 
@@ -566,6 +583,8 @@ def cluster_linear_fp8(X, W: BlockRows, plan: ClusterPlan, sorted_rows: bool = F
     n = rows.shape[0]
     if rows.shape[1] != din or k < 1 or dout < 1:
         raise ValueError("X must have %d columns, and W weights" % din)
+    if max(dout, k) > _MOST:
+        raise _too_large("sizes of W", "2^31 - 1")
     dtype = dtype if dtype is not None else torch.bfloat16 if exps is not None else X.dtype
     if dtype not in _TYPES:
         raise ValueError("dtype must be float32, bfloat16 or float16, got %s" % dtype)
@@ -602,6 +621,8 @@ def cluster_embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0
     _gpu(ids, "ids", table.device)
     if k < 1:
         raise ValueError("table must have at least one row")
+    if k > _MOST:
+        raise _too_large("rows of table", "2^31 - 1")
     _array(ids, "ids", torch.int32, tuple(ids.shape), table.device)
     scale = _scale(scale)
     with _On(table.device, stream, (ids, table)) as s:
