@@ -29,7 +29,7 @@ Nothing synchronizes.
 
 Gradients are calls of their own (``*_backward``); autograd records none of
 these calls, so a tensor that requires a gradient is refused while grad mode is
-on.  Call them under ``torch.no_grad()``, or in the forward and backward of a
+on, and one with a forward-mode tangent wherever its tangent would be lost.  Call them under ``torch.no_grad()``, or in the forward and backward of a
 ``torch.autograd.Function``, which run without it.
 """
 from __future__ import annotations
@@ -40,6 +40,7 @@ import operator
 from typing import Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _native as N
 
@@ -109,20 +110,31 @@ def _p(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _not_followed(inputs: Sequence[Optional[torch.Tensor]]) -> None:
+    """Refuse inputs that autograd would follow, backward or forward (whose tangents
+    no_grad leaves, and the forward of an autograd.Function hides)."""
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                raise ValueError("an input requires a gradient, and autograd does not follow this call: use "
+                                 "torch.no_grad() or a torch.autograd.Function, and the *_backward functions")
+    if getattr(forward_ad, "_current_level", 0) >= 0:   # a level is open
+        for t in inputs:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("an input has a forward-mode tangent, and autograd does not follow this call: use "
+                                 "a torch.autograd.Function with a jvp of its own")
+
+
 class _On:
     """The device and stream of one call: results and workspaces are allocated
     on that stream, and inputs made on another one are kept until it has
-    used them.  Inputs that autograd would follow are refused: it cannot."""
+    used them.  Inputs that autograd would follow are refused."""
 
     __slots__ = ("device", "stream", "inputs", "ctx")
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream],
                  inputs: Tuple[Optional[torch.Tensor], ...]):
-        if torch.is_grad_enabled():
-            for t in inputs:
-                if t is not None and t.requires_grad:
-                    raise ValueError("an input requires a gradient, and autograd does not follow this call: use "
-                                     "torch.no_grad() or a torch.autograd.Function, and the *_backward functions")
+        _not_followed(inputs)
         self.device, self.stream, self.inputs, self.ctx = device, stream, inputs, None
 
     def __enter__(self) -> int:
@@ -690,8 +702,9 @@ def _clip(tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[
         if to_sizes != sizes or to_dtypes != dtypes:
             raise ValueError("out must have the tensors' sizes and types")
         targets = array.array("Q", map(torch.Tensor.data_ptr, to))
-    if torch.is_grad_enabled() and (any(map(_grad, given)) or any(map(_grad, to))):
-        _On(dev, stream, tuple(given + to))   # refuses
+    if (torch.is_grad_enabled() and (any(map(_grad, given)) or any(map(_grad, to)))) or \
+            getattr(forward_ad, "_current_level", 0) >= 0:
+        _not_followed(given + to)
     kinds = array.array("i", [_TYPES[dtypes[0]]]) * count if dtypes.count(dtypes[0]) == count else \
         array.array("i", [_TYPES[t] for t in dtypes])
     at = lambda a: None if a is None else a.buffer_info()[0]
