@@ -250,7 +250,8 @@ int kmeans_table_backward(const void* dY, int64_t lddy, int64_t n, int32_t k, in
  * The norm g over `count` tensors: the square root of the sum of all squares,
  * formed in float64, to *norm (device, float32; infinity beyond its range).  With
  * out, not NULL, out[i] = tensors[i] f rounded once, f = min(1, limit / g) in
- * float32; a norm that is not finite leaves the values as they are.  tensors, out, sizes (elements)
+ * float32; where g is infinite or NaN, as it is if an input is, out[i] = tensors[i]
+ * (beyond float32's range g is not: values are scaled).  tensors, out, sizes (elements)
  * and types are HOST arrays, read before the call returns; out[i] is tensors[i]
  * (in place) or does not overlap any tensor.  Requires at most 2^40 elements in
  * all and a positive limit.

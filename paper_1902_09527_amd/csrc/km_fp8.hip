@@ -8,7 +8,8 @@
 //
 // 16 lanes share a block, 8 elements each (the maximum over a row of 16 lanes is four
 // cross-lane moves), four blocks of a lane in flight.  Bound by the memory's rate:
-// 16,383 x 4100 bf16, 41 us, 5.1 TB/s.
+// 16,383 x 4100 bf16, 41 us, 5.1 TB/s.  Back from 8 bits a lane takes one block at a
+// time: to bf16 37 us (5.5 TB/s), to float32 95 (3.5).
 #include <math.h>
 
 #include "km_tile.h"

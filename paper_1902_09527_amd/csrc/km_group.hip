@@ -139,7 +139,9 @@ struct ListArgs {
 };
 
 // A block a list.  In order of the clusters.  3 us for 16 clusters, 5 for 64 and two
-// lists: a launch's own time, that neither the plan nor the host could save.
+// lists: a launch's own time, that neither the plan nor the host could save.  A
+// cluster's items are written by one lane: 20 us for 100,000 rows in one cluster, 650
+// for a million rows of 64 columns in one (15,625 items).
 __global__ __launch_bounds__(1024) void k_gr_list(ListArgs A0, ListArgs A1) {
     const ListArgs& A = blockIdx.x ? A1 : A0;
     __shared__ int s[2][16];
@@ -412,8 +414,8 @@ constexpr int kWindow = 8;   // 8 bits: stages whose scales are in LDS at once, 
 // (two) or 64 x 64 (four): the larger reads less for a product, the smaller has less
 // past a cluster's end (main_choice has the times).  Bound by the matrix cores where
 // clusters are long: four clusters of 4096 rows, 4096 x 4096 bf16, 475 us (1160
-// TFLOP/s; one of them by the library 1459), 8 bits 246 us (2240).  Skewed clusters
-// of 16,384 rows leave tiles part full: 4096 x 4096 f16, 16 clusters 565 us.  By the
+// TFLOP/s; one of them by the library 1459), 8 bits 246 us (2240).  16 skewed clusters
+// of 16,384 rows, 4096 x 4096 f16, are 4.4 rounds of tiles for 4, and take 565 to 585 us.  By the
 // memory where they are short: 64 clusters, 2048 x 2048 bf16, 193 us, 4.0 TB/s.
 template <class T, class O, int TM, int TN, int WR, int WC, bool TR>
 __global__ __launch_bounds__(64 * WR * WC, TM == 64 ? 4 : 2) void k_gr_main(MainArgs A) {
@@ -1286,8 +1288,9 @@ struct FewArgs {
 // 16 columns and the places of one cluster a block, from the place blockIdx.y on
 // if a cluster starts there; its NWAVE waves share the contraction, some four steps
 // each.  No list and no workspace: one launch.  48 rows of 4096, 100 clusters, 4096
-// columns in 8 bits: 128 us, the rate of a copy; 32 rows of 1024, 8 clusters, bf16:
-// 7 us.
+// columns in 8 bits: 128 us, the rate of a copy; 48 rows of 48 such clusters f16 296 us
+// (5.4 TB/s), float32 620 (5.2), 8 bits 171 and with float32 results 191; 32 rows of
+// 1024, 8 clusters, bf16: 7 us.
 template <class T, class O>
 struct FewOp {
     static constexpr int kBytes = 16;   // of a row a lane and step
@@ -1709,7 +1712,8 @@ MainChoice main_choice(int64_t n, int64_t met, int32_t K, int32_t P, int type, b
     // A compute unit holds `held` tiles at once.  A stage of as many takes `busy` us on
     // a chip at work, and no stage less than `alone`; measured with 64 to 16,384 rows
     // of 256 to 4096 (16-bit, float32 and 8-bit rows).  A tile starts and ends in the
-    // time of `edge` stages.
+    // time of `edge` stages (too little for float32 tiles of 64 with few stages: 100,003
+    // rows of 256 to 256 are estimated at 94 us and take 142).
     struct Kind {
         int tile, held;
         double busy[3], alone[3], edge[3];

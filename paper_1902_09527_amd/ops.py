@@ -353,7 +353,7 @@ def _places(plan: ClusterPlan, n: int, k: int, device: torch.device, sorted_rows
     """Check a plan for n rows; its order, or None where the rows are in it already."""
     _plan(plan, device)
     if plan.k != k:
-        raise ValueError("plan has %d clusters, A has %d" % (plan.k, k))
+        raise ValueError("plan has %d clusters, the weights have %d" % (plan.k, k))
     if plan.m != 1 and not sorted_rows:
         raise ValueError("a plan of m = %d slots a row needs sorted rows (cluster_gather)" % plan.m)
     if plan.n * plan.m != n:
@@ -734,7 +734,9 @@ def clip_global_norm(tensors: Sequence[torch.Tensor], limit: float, out: Optiona
     """Scale tensors so that their :func:`global_norm` is at most ``limit``
     (kmeans_clip_norm): each times min(1, limit / norm), in place, or to ``out``
     (tensors of the same sizes and types that overlap none of them).  Returns the
-    norm before.  A norm that is not finite leaves the values as they are."""
+    norm before.  Where an input is infinite or NaN, the norm shows it and the values
+    stay as they are; a norm beyond float32's range is returned as infinity and the
+    values are scaled by the one in float64."""
     limit = float(limit)
     if not limit > 0:
         raise ValueError("limit must be positive")
